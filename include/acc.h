@@ -258,6 +258,71 @@ int acc_linear_fwd_rsvd(const acc_linear_desc* desc, const void* X, const void* 
 int acc_linear_bwd_rsvd(const acc_linear_desc* desc, const void* dY, const void* W, const void* U, const void* V,
                         void* dX, void* Gr, void* dW, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- 8-bit checkpoints of activations ------------------------------------------------------------------
+ * A third way to keep an activation between forward and backward, for what the factored compressors do not fit (weight
+ * gradients that have to stay close to the dense ones; element-wise operators, whose backward pass needs every element):
+ * X [n, c] -> one byte per element and one power-of-two scale for every ACC_ACT8_BLOCK consecutive tokens of a channel.
+ *   Q [n, c]                         the bytes, dense
+ *   E [ceil(n / ACC_ACT8_BLOCK), c]  uint8, dense: e + 127 of the block's scale 2^e, e the least whole number >= -100 with
+ *                                    max |x| <= T 2^e over the block's finite elements, T = 448 (e4m3) or 127 (int8)
+ *   q = x / 2^e, rounded to nearest even, as OCP fp8 e4m3 or as a two's complement integer of [-127, 127];
+ *   x^ = q 2^e, exact in bfloat16 and in float.
+ * An element that is not finite is stored as the format's code for it (0x7F; 0x80) and comes back as NaN; it does not count
+ * for the scale.  Finite magnitudes above 1.875 2^127 are kept as that.  A block of zeros has e = -100.
+ * Relative to X (2-norm, normal data) x^ is off by 2.6 % in e4m3, whatever the spread of magnitudes inside a block, and by
+ * 0.7 % in int8 where a channel's tokens are of one size.  Kept: 1 + 1 / 32 bytes per element.
+ * All pointers 16-byte aligned.                                                                        */
+#define ACC_ACT8_BLOCK 32
+typedef enum { ACC_ACT8_E4M3 = 0, ACC_ACT8_INT8 = 1 } acc_act8_format;
+
+typedef struct acc_act8_desc {
+  int64_t n;         /* tokens, 1 .. 2^30                                                    */
+  int64_t c;         /* channels, a multiple of 8, at most 2^21                              */
+  int64_t ldx;       /* row stride of X in elements, a multiple of 8; 0 = c                  */
+  int32_t io_dtype;  /* acc_dtype of X                                                       */
+  int32_t format;    /* acc_act8_format                                                      */
+} acc_act8_desc;
+
+/* Q and E from X [n, ldx]. */
+int acc_act8_pack(const acc_act8_desc* desc, const void* X, void* Q, void* E, void* stream);
+/* X [n, ldx] (columns 0 .. c-1 of each row) = the values that Q and E stand for. */
+int acc_act8_unpack(const acc_act8_desc* desc, const void* Q, const void* E, void* X, void* stream);
+
+/* The linear layer with an 8-bit checkpoint of its input: Y = X.W exact, then Q and E of X [n, d_in] as above
+ * (ACC_FLAG_SKIP_SKETCH: linears that share an input keep one checkpoint; Q and E are left alone and may be NULL).
+ * Of desc, r, seed, row_offset, ldf and factor_dtype have no meaning here (they must be valid); ACC_FLAG_ONE_LAUNCH is
+ * ignored.  No workspace. */
+int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, const void* W, void* Y, void* Q, void* E,
+                        void* stream);
+
+/* Its backward pass: dX = dY.W^T exact, and dW [d_in, d_out] = X^^T.dY of dw_dtype ([d_out, d_in] = dY^T.X^ with
+ * ACC_FLAG_W_OUT_IN; += with ACC_FLAG_DW_ACCUMULATE), a full gradient, not a factored one.  The products are accumulated in
+ * float and rounded once (where X^ or dY takes more than 4 GiB once per 4 GiB of tokens).  dX (W is then not read and may be
+ * NULL) or dW (Q, E and the workspace likewise) may be NULL, not both.  ACC_FLAG_SKIP_SKETCH is refused.
+ * workspace: ws_bytes >= acc_linear_act8_workspace_bytes(desc) for dW. */
+size_t acc_linear_act8_workspace_bytes(const acc_linear_desc* desc);
+int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY, const void* W, const void* Q, const void* E,
+                        void* dX, void* dW, void* workspace, size_t ws_bytes, void* stream);
+
+/* The gated activation of an MLP with 8-bit checkpoints of its two inputs, the largest activations of a layer:
+ *   H = silu(G) o U,  silu(g) = g / (1 + exp(-g));  Qg, Eg and Qu, Eu are the checkpoints of G and U [n, f]
+ *   dU = dH o silu(G^);  dG = dH o U^ o s (1 + G^ (1 - s)),  s = 1 / (1 + exp(-G^))
+ * and, where H != NULL in the backward call, H = silu(G^) o U^ again: the input of the product behind it, whose weight gradient
+ * then needs nothing kept of its own.  G, U, dG and dU [n, ldg] may be two halves of the rows of one matrix (ldg = 2 f);
+ * H and dH are [n, ldh].  Outputs overlap no inputs.  Float arithmetic, one rounding. */
+typedef struct acc_gated_desc {
+  int64_t n;         /* tokens, 1 .. 2^30                                                    */
+  int64_t f;         /* channels, a multiple of 8, at most 2^21                              */
+  int64_t ldg;       /* row stride of G, U, dG and dU in elements, a multiple of 8; 0 = f    */
+  int64_t ldh;       /* row stride of H and dH in elements, a multiple of 8; 0 = f           */
+  int32_t io_dtype;  /* acc_dtype of G, U, H, dH, dG and dU                                  */
+  int32_t format;    /* acc_act8_format                                                      */
+} acc_gated_desc;
+int acc_gated_fwd_act8(const acc_gated_desc* desc, const void* G, const void* U, void* H, void* Qg, void* Eg, void* Qu,
+                       void* Eu, void* stream);
+int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Qg, const void* Eg, const void* Qu,
+                       const void* Eu, void* dG, void* dU, void* H, void* stream);
+
 /* Test hook: the Philox integer stream behind S.  out is a device array of
  * ceil(n/4) * r * 4 uint32 laid out [token group q][column j][word w]. */
 int acc_philox_dump_u32(uint64_t seed, uint64_t row_offset, int64_t n, int64_t r, uint32_t* out,

@@ -21,12 +21,16 @@ ACC_FLAG_RSVD_POWER_SHIFT = 8   # flags bits 8..9: rounds of subspace iteration 
 
 ACC_STATIC_SCRATCH_BYTES = 32 << 20
 ACC_FP8_E4M3, ACC_FP8_E5M2 = 0, 1
+ACC_ACT8_BLOCK = 32
+ACC_ACT8_E4M3, ACC_ACT8_INT8 = 0, 1
 
 EXPORTS = ("acc_linear_workspace_bytes", "acc_linear_fwd", "acc_linear_fwd_static", "acc_linear_bwd", "acc_linear_dw",
            "acc_linear_fwd_fp8", "acc_linear_bwd_fp8",
            "acc_linear_bias_grad",
            "acc_rsvd_workspace_bytes", "acc_linear_fwd_rsvd", "acc_linear_bwd_rsvd", "acc_lowrank_workspace_bytes",
            "acc_lowrank_projector", "acc_lowrank_adamw_step",
+           "acc_act8_pack", "acc_act8_unpack", "acc_linear_fwd_act8", "acc_linear_act8_workspace_bytes",
+           "acc_linear_bwd_act8", "acc_gated_fwd_act8", "acc_gated_bwd_act8",
            "acc_philox_dump_u32", "acc_probe_mfma",
            "acc_sketch_dump", "acc_status_string", "acc_version")
 
@@ -45,6 +49,18 @@ class AccAdamwHyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
                 ("step", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class AccAct8Desc(ctypes.Structure):
+    """Mirror of `acc_act8_desc`."""
+    _fields_ = [("n", ctypes.c_int64), ("c", ctypes.c_int64), ("ldx", ctypes.c_int64), ("io_dtype", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
+class AccGatedDesc(ctypes.Structure):
+    """Mirror of `acc_gated_desc`."""
+    _fields_ = [("n", ctypes.c_int64), ("f", ctypes.c_int64), ("ldg", ctypes.c_int64), ("ldh", ctypes.c_int64),
+                ("io_dtype", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
 class AccError(RuntimeError):
@@ -92,6 +108,21 @@ _lib.acc_lowrank_workspace_bytes.restype = _sz
 _lib.acc_lowrank_workspace_bytes.argtypes = [_dp, ctypes.c_int64]
 _lib.acc_lowrank_projector.restype = ctypes.c_int
 _lib.acc_lowrank_projector.argtypes = [_dp, ctypes.c_int64, _vp, _vp, _vp, _vp, _sz, _vp]
+_adp, _gdp = ctypes.POINTER(AccAct8Desc), ctypes.POINTER(AccGatedDesc)
+_lib.acc_act8_pack.restype = ctypes.c_int
+_lib.acc_act8_pack.argtypes = [_adp, _vp, _vp, _vp, _vp]
+_lib.acc_act8_unpack.restype = ctypes.c_int
+_lib.acc_act8_unpack.argtypes = [_adp, _vp, _vp, _vp, _vp]
+_lib.acc_linear_fwd_act8.restype = ctypes.c_int
+_lib.acc_linear_fwd_act8.argtypes = [_dp, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.acc_linear_act8_workspace_bytes.restype = _sz
+_lib.acc_linear_act8_workspace_bytes.argtypes = [_dp]
+_lib.acc_linear_bwd_act8.restype = ctypes.c_int
+_lib.acc_linear_bwd_act8.argtypes = [_dp, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.acc_gated_fwd_act8.restype = ctypes.c_int
+_lib.acc_gated_fwd_act8.argtypes = [_gdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.acc_gated_bwd_act8.restype = ctypes.c_int
+_lib.acc_gated_bwd_act8.argtypes = [_gdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.acc_philox_dump_u32.restype = ctypes.c_int
 _lib.acc_philox_dump_u32.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, _vp, _vp]
 _lib.acc_sketch_dump.restype = ctypes.c_int
@@ -265,6 +296,66 @@ def acc_lowrank_adamw_step(desc, hyper, P, k, left, Gr, M, V, W, workspace, stre
 def alloc_lowrank_workspace(desc, k: int, device="cuda:0"):
     import torch
     return torch.empty(max(acc_lowrank_workspace_bytes(desc, k), 16), dtype=torch.uint8, device=device)
+
+
+def make_act8_desc(n, c, ldx=0, io_dtype=ACC_BF16, format=ACC_ACT8_E4M3) -> AccAct8Desc:
+    return AccAct8Desc(n, c, ldx, io_dtype, format)
+
+
+def alloc_act8(desc: AccAct8Desc, device="cuda:0"):
+    """The two buffers of a checkpoint: its bytes [n, c] and its blocks' exponents (uint8 tensors)."""
+    return (torch.empty(desc.n, desc.c, dtype=torch.uint8, device=device),
+            torch.empty((desc.n + ACC_ACT8_BLOCK - 1) // ACC_ACT8_BLOCK, desc.c, dtype=torch.uint8, device=device))
+
+
+def acc_act8_pack(desc, X, Q, E, stream=None):
+    """Enqueue Q, E = the 8-bit checkpoint of X."""
+    _check(_lib.acc_act8_pack(ctypes.byref(desc), _ptr(X), _ptr(Q), _ptr(E), _stream(stream)))
+
+
+def acc_act8_unpack(desc, Q, E, X, stream=None):
+    """Enqueue X = the values that the checkpoint stands for."""
+    _check(_lib.acc_act8_unpack(ctypes.byref(desc), _ptr(Q), _ptr(E), _ptr(X), _stream(stream)))
+
+
+def acc_linear_fwd_act8(desc, format, X, W, Y, Q, E, stream=None):
+    """Enqueue Y = X.W and the 8-bit checkpoint of X."""
+    _check(_lib.acc_linear_fwd_act8(ctypes.byref(desc), int(format), _ptr(X), _ptr(W), _ptr(Y), _ptr(Q), _ptr(E),
+                                    _stream(stream)))
+
+
+def acc_linear_act8_workspace_bytes(desc: AccLinearDesc) -> int:
+    return int(_lib.acc_linear_act8_workspace_bytes(ctypes.byref(desc)))
+
+
+def acc_linear_bwd_act8(desc, format, dY, W, Q, E, dX, dW, workspace, stream=None, ws_bytes=None):
+    """Enqueue dX = dY.W^T (dX is not None) and dW = X^^T.dY from the checkpoint (dW is not None)."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_linear_bwd_act8(ctypes.byref(desc), int(format), _ptr(dY), _ptr(W), _ptr(Q), _ptr(E), _ptr(dX),
+                                    _ptr(dW), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def make_gated_desc(n, f, ldg=0, ldh=0, io_dtype=ACC_BF16, format=ACC_ACT8_E4M3) -> AccGatedDesc:
+    return AccGatedDesc(n, f, ldg, ldh, io_dtype, format)
+
+
+def alloc_gated_act8(desc: AccGatedDesc, device="cuda:0"):
+    """Qg, Eg, Qu, Eu of acc_gated_fwd_act8."""
+    one = make_act8_desc(desc.n, desc.f, io_dtype=desc.io_dtype, format=desc.format)
+    return (*alloc_act8(one, device), *alloc_act8(one, device))
+
+
+def acc_gated_fwd_act8(desc, G, U, H, Qg, Eg, Qu, Eu, stream=None):
+    """Enqueue H = silu(G) o U and the 8-bit checkpoints of G and U."""
+    _check(_lib.acc_gated_fwd_act8(ctypes.byref(desc), _ptr(G), _ptr(U), _ptr(H), _ptr(Qg), _ptr(Eg), _ptr(Qu), _ptr(Eu),
+                                   _stream(stream)))
+
+
+def acc_gated_bwd_act8(desc, dH, Qg, Eg, Qu, Eu, dG, dU, H=None, stream=None):
+    """Enqueue dG and dU from the checkpoints and (H is not None) the activation again."""
+    _check(_lib.acc_gated_bwd_act8(ctypes.byref(desc), _ptr(dH), _ptr(Qg), _ptr(Eg), _ptr(Qu), _ptr(Eu), _ptr(dG),
+                                   _ptr(dU), _ptr(H), _stream(stream)))
 
 
 def acc_philox_dump_u32(seed, row_offset, n, r, out, stream=None):

@@ -1,9 +1,11 @@
 """Compile csrc/ into libacc.so for gfx950 with hipcc (in-tree, no JIT cache)."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -20,9 +22,7 @@ def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
 
 
-def build(verbose: bool = True, extra_flags=()) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, *sources(), "-o", LIB]
+def _run(cmd, verbose=False):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -30,8 +30,20 @@ def build(verbose: bool = True, extra_flags=()) -> str:
                     if "packed-fp32-ops" not in l and "is not a recognized feature" not in l)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    return out
+
+
+def build(verbose: bool = True, extra_flags=()) -> str:
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:   # one compiler per source, side by side
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in sources()]
+        cmds = [[hipcc, *flags, *extra_flags, "-c", src, "-o", obj] for src, obj in zip(sources(), objects)]
+        with concurrent.futures.ThreadPoolExecutor(len(cmds)) as pool:
+            outs = list(pool.map(lambda cmd: _run(cmd, verbose), cmds))
+        outs.append(_run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB], verbose))
+    if verbose:
+        print("\n".join(out for out in outs if out.strip()))
     return LIB
 
 
@@ -92,33 +104,36 @@ def kernel_resources() -> dict:
     restores scalar registers it had parked in vector lanes): the hardware needs five wait states there, and without
     them the transfer uses the register's old value."""
     import re
-    import tempfile
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in HIPCC_FLAGS if f not in ("-fPIC", "-shared")]
     out = {}
     with tempfile.TemporaryDirectory() as tmp:
-        asm_path = os.path.join(tmp, "dev.s")
-        cmd = [hipcc, *flags, "--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage", *sources(),
-               "-o", asm_path]
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        if res.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + res.stderr)
-        name = None
-        for line in res.stderr.splitlines():
-            m = re.search(r"remark: Function Name: (\S+)", line)
-            if m:
-                name = m.group(1)
-                out[name] = {}
-                continue
-            m = re.search(r"remark:\s+ScratchSize \[bytes/lane\]: (\d+)", line)
-            if m and name:
-                out[name]["scratch"] = int(m.group(1))
-            m = re.search(r"remark:\s+VGPRs Spill: (\d+)", line)
-            if m and name:
-                out[name]["vgpr_spill"] = int(m.group(1))
-        with open(asm_path) as f:
-            for name, found in scan_assembly(f, set(out)).items():
-                out[name].update(found)
+        def compiled(src):
+            asm_path = os.path.join(tmp, os.path.basename(src) + ".s")
+            cmd = [hipcc, *flags, "--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage", src, "-o", asm_path]
+            return asm_path, subprocess.run(cmd, capture_output=True, text=True)
+        with concurrent.futures.ThreadPoolExecutor(len(sources())) as pool:
+            results = list(pool.map(compiled, sources()))
+        for asm_path, res in results:
+            if res.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + res.stderr)
+            name, found = None, {}
+            for line in res.stderr.splitlines():
+                m = re.search(r"remark: Function Name: (\S+)", line)
+                if m:
+                    name = m.group(1)
+                    found[name] = {}
+                    continue
+                m = re.search(r"remark:\s+ScratchSize \[bytes/lane\]: (\d+)", line)
+                if m and name:
+                    found[name]["scratch"] = int(m.group(1))
+                m = re.search(r"remark:\s+VGPRs Spill: (\d+)", line)
+                if m and name:
+                    found[name]["vgpr_spill"] = int(m.group(1))
+            with open(asm_path) as f:
+                for name, scanned in scan_assembly(f, set(found)).items():
+                    found[name].update(scanned)
+            out.update(found)
     return out
 
 

@@ -1,0 +1,293 @@
+// 8-bit checkpoints of activations: X [n, c] -> one byte per element and one power-of-two scale 2^e for every 32 consecutive tokens
+// of a channel, and back.
+//
+//   e = the least whole number >= -100 with max |x| <= T 2^e over the block's finite elements, T = 448 (e4m3) or 127 (int8);
+//   q = x / 2^e rounded to nearest even; what is not finite gets the format's code for it (0x7F, -128) and reads back as NaN.
+//   Magnitudes above 1.875 2^127 are kept as that, so that no finite value reads back as infinite.
+//
+// Why blocks along the tokens: the large magnitudes of a trained model's activations sit in few channels, which a block along the
+// channels would share with their neighbours and flush those.  Why powers of two: a byte times its scale is then a bfloat16 number
+// exactly (e4m3 has four significant bits, int8 seven), so a product of the checkpoint on the matrix instructions rounds nothing
+// that the quantisation did not; and the exponent is one byte.  e >= -100 keeps every value that is read back a normal number.
+//
+// All kernels here are bound by HBM.  One wave takes 32 tokens x 128 channels: lane = 8 channels (16 bytes of bfloat16) of 8 tokens,
+// all its loads requested at once, so a block's maximum needs two exchanges between lanes and no LDS, and rows are read in pieces of
+// 256 bytes.
+#pragma once
+#include "acc_common.h"
+
+namespace acc {
+
+constexpr int kActBlock = ACC_ACT8_BLOCK;
+constexpr int kActTokens = 8;               // tokens of a lane; four lanes hold a block
+constexpr int kActChannels = 128;           // channels of a wave
+constexpr uint32_t kActTop = 0x7F700000u;   // 1.875 2^127, as float bits
+constexpr uint32_t kInf = 0x7F800000u;
+static_assert(kActBlock == 4 * kActTokens, "a wave's rows are one block");
+
+// Eight consecutive elements as float; p is 16-byte aligned.
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const f32x4 lo = *(const f32x4*)p, hi = *(const f32x4*)(p + 4);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    v[t] = lo[t];
+    v[4 + t] = hi[t];
+  }
+}
+__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
+  const bf16x8 x = *(const bf16x8*)p;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) v[t] = (float)x[t];
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
+  bf16x8 x;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) x[t] = (bf16)v[t];
+  *(bf16x8*)p = x;
+}
+
+// e + 127 of a block whose largest finite magnitude has these float bits.
+template <int FORMAT> __device__ __forceinline__ uint32_t act_exponent(uint32_t largest) {
+  if (largest > kActTop) largest = kActTop;
+  // 448 = 1.75 2^8, 127 = 1.984375 2^6
+  constexpr uint32_t FRAC = FORMAT == ACC_ACT8_E4M3 ? 0x600000u : 0x7E0000u;
+  constexpr int SHIFT = FORMAT == ACC_ACT8_E4M3 ? 8 : 6;
+  const int e = (int)(largest >> 23) - SHIFT + ((largest & 0x7FFFFFu) > FRAC ? 1 : 0);
+  return (uint32_t)(e < 27 ? 27 : e);
+}
+__device__ __forceinline__ float act_scale(uint32_t e) { return __uint_as_float(e << 23); }                 // 2^e
+__device__ __forceinline__ float act_inverse_scale(uint32_t e) { return __uint_as_float((254u - e) << 23); }  // 2^-e
+
+// Four elements over their scales, |y| <= T, as four bytes.
+template <int FORMAT> __device__ __forceinline__ uint32_t act_bytes(float y0, float y1, float y2, float y3) {
+  if constexpr (FORMAT == ACC_ACT8_E4M3) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y2, y3, w, true);
+  } else {
+    // 1.5 2^23 + y: the sum's last place is 1, so it is rounded to a whole number whose low byte is y in two's complement
+    const uint32_t b0 = __float_as_uint(y0 + 12582912.f), b1 = __float_as_uint(y1 + 12582912.f);
+    const uint32_t b2 = __float_as_uint(y2 + 12582912.f), b3 = __float_as_uint(y3 + 12582912.f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, 0x0C0C0400u), __builtin_amdgcn_perm(b1, b0, 0x0C0C0400u), 0x05040100u);
+  }
+}
+template <int FORMAT> constexpr uint32_t kActNotFinite = FORMAT == ACC_ACT8_E4M3 ? 0x7Fu : 0x80u;
+
+// Element t of four bytes as float, without its scale.
+template <int FORMAT, int T> __device__ __forceinline__ float act_element(uint32_t w) {
+  if constexpr (FORMAT == ACC_ACT8_E4M3) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)w, T);
+  } else {
+    const int q = (int)(w << (24 - 8 * T)) >> 24;
+    return q == -128 ? __uint_as_float(0x7FC00000u) : (float)q;
+  }
+}
+// Eight bytes times their scales.
+template <int FORMAT> __device__ __forceinline__ void act_values(u32x2 q, u32x2 e, float (&v)[8]) {
+  static_for<0, 8>([&](auto t) {
+    constexpr int T = decltype(t)::value;
+    v[T] = act_element<FORMAT, T % 4>(q[T / 4]) * act_scale((e[T / 4] >> (8 * (T % 4))) & 0xFFu);
+  });
+}
+
+// A wave's tile: 8 channels from `c`, tokens row .. row + 7 of block `block`.
+struct ActLane {
+  int64_t block, row, c;
+  int rows;       // tokens of this lane that exist (0: none, or its channels do not)
+  int group;      // which quarter of the block
+};
+__device__ __forceinline__ ActLane act_lane(int64_t n, int64_t c) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
+  const int64_t across = (c + kActChannels - 1) / kActChannels;
+  ActLane l;
+  l.block = wave / across;
+  l.group = lane >> 4;
+  l.c = (wave - l.block * across) * kActChannels + (lane & 15) * 8;
+  l.row = l.block * kActBlock + l.group * kActTokens;
+  const int64_t left = n - l.row;
+  l.rows = l.c >= c || left <= 0 ? 0 : (int)(left < kActTokens ? left : kActTokens);
+  return l;
+}
+inline __host__ int64_t act_work_groups(int64_t n, int64_t c) {  // of 256 lanes
+  return ceil_div(ceil_div(n, kActBlock) * ceil_div(c, kActChannels), 4);
+}
+
+// This lane's eight tokens of eight channels, x[token][channel] (0 where a token does not exist), into the checkpoint [n, c].
+template <int FORMAT>
+__device__ __forceinline__ void act_keep(const ActLane& l, int64_t c, float (&x)[kActTokens][8], uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
+  uint32_t largest[8], any = 0;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < kActTokens; ++k) {
+      const uint32_t a = __float_as_uint(x[k][t]) & 0x7FFFFFFFu;
+      m = a > m ? a : m;
+    }
+    largest[t] = m;
+    any = m > any ? m : any;
+  }
+  uint64_t odd = 0;   // bit 8 k + t: element [k][t] is not finite
+  if (__any(any > kActTop)) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < kActTokens; ++k) {
+        const uint32_t bits = __float_as_uint(x[k][t]), a = bits & 0x7FFFFFFFu;
+        if (a >= kInf) {
+          odd |= (uint64_t)1 << (8 * k + t);
+          x[k][t] = 0.f;
+        } else {
+          const uint32_t kept = a < kActTop ? a : kActTop;
+          m = kept > m ? kept : m;
+          x[k][t] = __uint_as_float((bits & 0x80000000u) | kept);
+        }
+      }
+      largest[t] = m;
+    }
+  }
+  uint32_t e[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    uint32_t m = largest[t], o = (uint32_t)__shfl_xor((int)m, 16);
+    m = o > m ? o : m;
+    o = (uint32_t)__shfl_xor((int)m, 32);
+    e[t] = act_exponent<FORMAT>(o > m ? o : m);
+  }
+  if (l.rows == 0) return;
+  if (l.group == 0) {
+    const u32x2 packed = {e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24};
+    *(u32x2*)(E + l.block * c + l.c) = packed;
+  }
+  float inv[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) inv[t] = act_inverse_scale(e[t]);
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) {
+    if (k >= l.rows) break;
+    u32x2 q;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w = act_bytes<FORMAT>(x[k][4 * h] * inv[4 * h], x[k][4 * h + 1] * inv[4 * h + 1], x[k][4 * h + 2] * inv[4 * h + 2],
+                                     x[k][4 * h + 3] * inv[4 * h + 3]);
+      if (odd) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (odd >> (8 * k + 4 * h + t) & 1) w = (w & ~(0xFFu << (8 * t))) | kActNotFinite<FORMAT> << (8 * t);
+      }
+      q[h] = w;
+    }
+    *(u32x2*)(Q + (l.row + k) * c + l.c) = q;
+  }
+}
+
+template <typename T> __device__ __forceinline__ void act_load(const ActLane& l, const T* __restrict__ X, int64_t ld, float (&x)[kActTokens][8]) {
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) {
+    if (k < l.rows) {
+      load8(X + (l.row + k) * ld + l.c, x[k]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[k][t] = 0.f;
+    }
+  }
+}
+
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void act8_pack_kernel(const T* __restrict__ X, int64_t n, int64_t c, int64_t ld, uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
+  const ActLane l = act_lane(n, c);
+  float x[kActTokens][8];
+  act_load(l, X, ld, x);
+  act_keep<FORMAT>(l, c, x, Q, E);
+}
+
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void act8_unpack_kernel(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ E, int64_t n, int64_t c, int64_t ld, T* __restrict__ X) {
+  const ActLane l = act_lane(n, c);
+  if (l.rows == 0) return;
+  const u32x2 e = *(const u32x2*)(E + l.block * c + l.c);
+  u32x2 q[kActTokens];
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k)
+    if (k < l.rows) q[k] = *(const u32x2*)(Q + (l.row + k) * c + l.c);
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) {
+    if (k >= l.rows) break;
+    float v[8];
+    act_values<FORMAT>(q[k], e, v);
+    store8(X + (l.row + k) * ld + l.c, v);
+  }
+}
+
+// 1 / (1 + exp(-x)); 0 and 1 at the ends, as exp overflows to infinity or vanishes.  bfloat16 results take the hardware's
+// exponential and reciprocal (a few 2^-23 of the value, under the rounding of 2^-9), float32 ones the library's.
+template <typename T> __device__ __forceinline__ float sigmoid(float x) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-x));
+  else return 1.f / (1.f + expf(-x));
+}
+
+// H = silu(G) o U, and G and U into their checkpoints.
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void gated_fwd_kernel(const T* __restrict__ G, const T* __restrict__ U, int64_t n, int64_t f, int64_t ldg, int64_t ldh,
+                                                        T* __restrict__ H, uint8_t* __restrict__ Qg, uint8_t* __restrict__ Eg, uint8_t* __restrict__ Qu,
+                                                        uint8_t* __restrict__ Eu) {
+  const ActLane l = act_lane(n, f);
+  float g[kActTokens][8], u[kActTokens][8];
+  act_load(l, G, ldg, g);
+  act_load(l, U, ldg, u);
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) {
+    if (k >= l.rows) break;
+    float h[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) h[t] = g[k][t] * sigmoid<T>(g[k][t]) * u[k][t];
+    store8(H + (l.row + k) * ldh + l.c, h);
+  }
+  act_keep<FORMAT>(l, f, g, Qg, Eg);
+  act_keep<FORMAT>(l, f, u, Qu, Eu);
+}
+
+// With s = sigmoid(G^):  dU = dH o G^ s,  dG = dH o U^ s (1 + G^ (1 - s)),  and on request H = G^ s o U^ again.
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void gated_bwd_kernel(const T* __restrict__ dH, const uint8_t* __restrict__ Qg, const uint8_t* __restrict__ Eg,
+                                                        const uint8_t* __restrict__ Qu, const uint8_t* __restrict__ Eu, int64_t n, int64_t f, int64_t ldg,
+                                                        int64_t ldh, T* __restrict__ dG, T* __restrict__ dU, T* __restrict__ H) {
+  const ActLane l = act_lane(n, f);
+  if (l.rows == 0) return;
+  const u32x2 eg = *(const u32x2*)(Eg + l.block * f + l.c), eu = *(const u32x2*)(Eu + l.block * f + l.c);
+  u32x2 qg[kActTokens], qu[kActTokens];
+  float dh[kActTokens][8];
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k)
+    if (k < l.rows) {
+      const int64_t row = l.row + k;
+      qg[k] = *(const u32x2*)(Qg + row * f + l.c);
+      qu[k] = *(const u32x2*)(Qu + row * f + l.c);
+      load8(dH + row * ldh + l.c, dh[k]);
+    }
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) {
+    if (k >= l.rows) break;
+    const int64_t row = l.row + k;
+    float g[8], u[8], dg[8], du[8], h[8];
+    act_values<FORMAT>(qg[k], eg, g);
+    act_values<FORMAT>(qu[k], eu, u);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const float s = sigmoid<T>(g[t]), a = g[t] * s;
+      du[t] = dh[k][t] * a;
+      dg[t] = dh[k][t] * u[t] * (s + a * (1.f - s));
+      h[t] = a * u[t];
+    }
+    store8(dG + row * ldg + l.c, dg);
+    store8(dU + row * ldg + l.c, du);
+    if (H) store8(H + row * ldh + l.c, h);
+  }
+}
+
+}  // namespace acc

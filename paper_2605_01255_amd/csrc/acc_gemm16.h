@@ -1,7 +1,8 @@
 // bf16 GEMM on the 16x16x32 matrix instruction for shapes that fill rounds of the chip with 256 x 256 tiles
 // (steps F1, B1; pick_gemm_tile decides):  C[M, N] = A[M, K] . B, fp32 accumulate, bf16 output.
 //
-//   A is row-major with K contiguous (X, dY).
+//   A_KMAJOR = true : A[M, K], K contiguous                 (X, dY).
+//   A_KMAJOR = false: A is given transposed, At[K, M], M contiguous (products over the tokens), read like such a B.
 //   B_KMAJOR = true : B is given as Bt[N, K], K contiguous      (dX = dY . W^T reads W as is)
 //   B_KMAJOR = false: B is given as  B[K, N], N contiguous      (Y = X . W); the operand is formed with
 //                     transposing LDS reads (ds_read_b64_tr_b16).
@@ -74,7 +75,7 @@ __device__ __forceinline__ int swz_n16(int krow) { return ((krow & 3) << 2) | ((
 // RAGGED_K: K % 64 != 0 (K % 8 == 0).  The 16-byte chunks of the last K tile past K are sent out of the buffer's range and
 // read as zero; a lane's chunk is the same in all its wave-loads, so that is one select per K tile and one OR per
 // transfer, which an instantiation of its own keeps out of the slots of the K % 64 == 0 form.
-template <bool B_KMAJOR, bool RAGGED_K = false, int N1 = 12, int S1 = 4, int S0 = 4>
+template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, int N1 = 12, int S1 = 4, int S0 = 4>
 __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, int n_slots) {
   // schedule of k-step 1: the barrier sits before its slot BAR_Q; N1 wave-loads go out after it, one every S1
   // slots, the other 16 - N1 in the next K tile's k-step 0, one every S0 slots from slot 2
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   constexpr int BM = 256, BN = 256, BK = 64;
   constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES;
   constexpr int A_LOADS = A_BYTES / 1024 / NW, B_LOADS = B_BYTES / 1024 / NW, NG = A_LOADS + B_LOADS;
-  constexpr int BN_CHUNKS = BN / 8;
+  constexpr int BN_CHUNKS = BN / 8;   // of a row of either kind of transposed tile
   constexpr int REGION = 16 * 256;  // one staged block row: 16 rows x 128 bf16
   static_assert(NG == 16, "the slot program places sixteen wave-loads per K tile");
 
@@ -100,8 +101,13 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   uint32_t a_src[A_LOADS], b_src[B_LOADS];
 #pragma unroll
   for (int t = 0; t < A_LOADS; ++t) {
-    const int row = (t * NW + wave) * 8 + (lane >> 3);
-    a_src[t] = (uint32_t)(row * p.lda * 2 + (((lane & 7) ^ swz(row)) << 4));
+    if (A_KMAJOR) {
+      const int row = (t * NW + wave) * 8 + (lane >> 3);
+      a_src[t] = (uint32_t)(row * p.lda * 2 + (((lane & 7) ^ swz(row)) << 4));
+    } else {
+      const int krow = (t * NW + wave) * (64 / BN_CHUNKS) + lane / BN_CHUNKS;
+      a_src[t] = (uint32_t)(krow * p.lda * 2 + (((lane % BN_CHUNKS) ^ swz_n16(krow)) << 4));
+    }
   }
 #pragma unroll
   for (int t = 0; t < B_LOADS; ++t) {
@@ -117,6 +123,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   // this lane's chunk of the last K tile lies past K (rows a multiple of 32 apart share their swizzle)
   const uint32_t tail = RAGGED_K && (((lane & 7) ^ swz(wave * 8 + (lane >> 3))) * 8 >= p.K - (int64_t)(KT - 1) * BK) ? 0xFFFFFFF0u : 0u;
   auto past_k = [&](int kt) -> uint32_t { return RAGGED_K && kt == KT - 1 ? tail : 0u; };
+  const uint32_t a_kstep = A_KMAJOR ? BK * 2 : (uint32_t)(BK * p.lda * 2);
   const uint32_t b_kstep = B_KMAJOR ? BK * 2 : (uint32_t)(BK * p.ldb * 2);
   const uint32_t smem_lds = (uint32_t)(uintptr_t)smem;
 
@@ -130,13 +137,14 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     TileRef r;
     r.m0 = (int64_t)tm * BM;
     r.n0 = (int64_t)tn * BN;
-    r.a_rsrc = make_rsrc(p.A + r.m0 * p.lda, ((p.M - r.m0 - 1) * p.lda + p.K) * 2);
+    r.a_rsrc = A_KMAJOR ? make_rsrc(p.A + r.m0 * p.lda, ((p.M - r.m0 - 1) * p.lda + p.K) * 2)
+                        : make_rsrc(p.A + r.m0, ((p.K - 1) * p.lda + ((p.M - r.m0 + 7) & ~(int64_t)7)) * 2);
     r.b_rsrc = B_KMAJOR ? make_rsrc(p.B + r.n0 * p.ldb, ((p.N - r.n0 - 1) * p.ldb + p.K) * 2)
                         : make_rsrc(p.B + r.n0, ((p.K - 1) * p.ldb + (p.N - r.n0)) * 2);
     return r;
   };
   auto issue_one = [&](const TileRef& r, int g, int kt, uint32_t stage) {
-    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, a_src[g], (uint32_t)kt * (BK * 2), stage + (g * NW + wave) * 1024);
+    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, a_src[g], (uint32_t)kt * a_kstep, stage + (g * NW + wave) * 1024);
     else buffer_to_lds_b128(r.b_rsrc, b_src[g - A_LOADS], (uint32_t)kt * b_kstep,
                             stage + A_BYTES + ((g - A_LOADS) * NW + wave) * 1024);
   };
@@ -152,7 +160,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   };
   auto issue_at_m0 = [&](const TileRef& r, int g, int kt, uint32_t oob) {  // oob: past_k(kt)
     if (g < A_LOADS)
-      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K ? a_src[g] | oob : a_src[g]), "s"(r.a_rsrc), "s"((uint32_t)kt * (BK * 2)), "{m0}"(m0_token) : "memory");
+      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K && A_KMAJOR ? a_src[g] | oob : a_src[g]), "s"(r.a_rsrc), "s"((uint32_t)kt * a_kstep), "{m0}"(m0_token) : "memory");
     else
       asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K && B_KMAJOR ? b_src[g - A_LOADS] | oob : b_src[g - A_LOADS]), "s"(r.b_rsrc), "s"((uint32_t)kt * b_kstep), "{m0}"(m0_token) : "memory");
   };
@@ -163,7 +171,24 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   int kc[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s) kc[s] = ((4 * s + g4) ^ rswz) << 4;
-  auto read_a = [&](const char* st, int s, int i) -> bf16x8 { return lds_read_b128(st, a_row + i * 2048 + kc[s]); };
+  int a_rd[A_KMAJOR ? 1 : TB];
+  if constexpr (!A_KMAJOR) {
+#pragma unroll
+    for (int i = 0; i < TB; ++i) {
+      const int m_off = (wm * TB + i) * 16 + 4 * (l16 & 3);
+      const int krow = 8 * g4 + (l16 >> 2);
+      a_rd[i] = krow * (BM * 2) + (((m_off >> 3) ^ swz_n16(krow)) << 4) + (m_off & 7) * 2;
+    }
+  }
+  auto read_a = [&](const char* st, int s, int i) -> bf16x8 {
+    if constexpr (A_KMAJOR) {
+      return lds_read_b128(st, a_row + i * 2048 + kc[s]);
+    } else {
+      const s16x4 lo = lds_read_tr16_b64(st, a_rd[i] + 32 * s * (BM * 2));
+      const s16x4 hi = lds_read_tr16_b64(st, a_rd[i] + (32 * s + 4) * (BM * 2));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
   int b_rd[TB];
 #pragma unroll
   for (int j = 0; j < TB; ++j) {

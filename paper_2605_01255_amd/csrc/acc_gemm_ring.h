@@ -1,7 +1,7 @@
 // bf16 GEMM on a ring of LDS stages, for products that do not fill whole rounds of the chip with 256 x 256 tiles (steps F1, B1, B3):
 // C[M, N] = A[M, K] . B, fp32 accumulate, bf16 or fp32 output, optionally C = beta C + alpha (A . B).
 //
-//   A is row-major with K contiguous.  B_KMAJOR = true: Bt[N, K];  false: B[K, N], N contiguous.
+//   A_KMAJOR = true: A[M, K];  false: A is given transposed, At[K, M], M contiguous.  B_KMAJOR = true: Bt[N, K];  false: B[K, N], N contiguous.
 //
 // With one tile of 128 x 128 (or 64 x 64) per compute unit a work-group's time is the latency of its transfers: a K
 // tile multiplies for 0.2 us and a transfer takes one to two.  So NS stages are kept in flight (NS - 1 of them while one
@@ -14,7 +14,8 @@
 //   wait       K tile kt + 1 has landed (at most the NS - 2 tiles after it are outstanding), barrier
 //   k-step 1   the operands of K tile kt + 1's k-step 0 are read; K tile kt + NS goes into the stage just released
 // Any K % 8 == 0: in the last K tile the 16-byte chunks past K (and the rows of an N-contiguous B past K) are sent out
-// of the buffer's range and read as zero on both sides.  M, N as in gemm_bf16_tile; operands below 4 GiB.
+// of the buffer's range and read as zero on both sides.  M, N as in gemm_bf16_tile; operands below 4 GiB.  With both operands
+// transposed (products over the tokens) any K, and any M whose rows of At are stored M rounded up to 8 apart or more.
 #pragma once
 #include <type_traits>
 
@@ -23,7 +24,8 @@
 namespace acc {
 
 // Swizzles of an N-contiguous B tile (see swz_n16): the 4 k rows x 2 groups that 32 lanes of a transposing read touch
-// fall on 8 different 32-byte bank groups.  A 64-column row covers half the banks, rows alternate between the halves.
+// fall on 8 different 32-byte bank groups.  A 64-column row covers half the banks, rows alternate between the halves.  The same
+// for an M-contiguous A tile.
 template <int BN> __device__ __forceinline__ int swz_ring(int krow) {
   // (so do the 384-byte rows of 192 columns, whose chunks stay inside an aligned group of eight)
   if constexpr (BN == 64 || BN == 192) return (((krow >> 1) & 1) << 1) | (((krow >> 3) & 1) << 2);
@@ -52,15 +54,16 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_
 // result is (error of a [16384, 3072] x [3072, 64] product: 6.3e-7 with one sum per split of 1536, 6.0e-7 so, 6.1e-7 with
 // the four splits of 768 that the two-stage kernel took; the time is the same).
 // SUM: C = beta C + alpha (A . B).  A form of its own: behind a branch its registers cost the plain one occupancy.
-template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, bool SPLIT = false, bool SUM = false>
+template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, bool SPLIT = false, bool SUM = false, bool A_KMAJOR = true>
 __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int NW = 4, WN = 2;
   constexpr int BM = 2 * TM * 16, BN = 2 * TN * 16, BK = 64;
   constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES;
   constexpr int A_LOADS = A_BYTES / 1024 / NW, B_LOADS = B_BYTES / 1024 / NW, NG = A_LOADS + B_LOADS;
-  constexpr int BN_CHUNKS = BN / 8;
+  constexpr int BM_CHUNKS = BM / 8, BN_CHUNKS = BN / 8;
   static_assert(BN == 64 || BN == 128 || BN == 192, "N-contiguous swizzle");
+  static_assert(A_KMAJOR || BM == 64 || BM == 128 || BM == 192 || BM == 256, "M-contiguous swizzle");
   static_assert((NS - 1) * NG <= 63, "vmcnt range");
 
   int tm, tn;
@@ -78,13 +81,22 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   const int KT = (int)((kn + BK - 1) / BK);
 
   // ---- global -> LDS: wave-load t of wave w fills LDS bytes [(t * NW + w) * 1024, +1024) of the operand tile ----
-  const u32x4 a_rsrc = make_rsrc(p.A + m0 * p.lda + k0, ((p.M - m0 - 1) * p.lda + kn) * 2);
+  const u32x4 a_rsrc = A_KMAJOR ? make_rsrc(p.A + m0 * p.lda + k0, ((p.M - m0 - 1) * p.lda + kn) * 2)
+                                : make_rsrc(p.A + k0 * p.lda + m0, ((kn - 1) * p.lda + ((p.M - m0 + 7) & ~(int64_t)7)) * 2);
   const u32x4 b_rsrc = B_KMAJOR ? make_rsrc(p.B + n0 * p.ldb + k0, ((p.N - n0 - 1) * p.ldb + kn) * 2)
                                 : make_rsrc(p.B + k0 * p.ldb + n0, kb > 0 ? ((kb - 1) * p.ldb + (p.N - n0)) * 2 : 0);
   uint32_t a_src[A_LOADS], b_src[B_LOADS];
   const int kchunk = (lane & 7) ^ swz(wave * 8 + (lane >> 3));  // the same for every wave-load: rows 32 apart share swz
 #pragma unroll
-  for (int t = 0; t < A_LOADS; ++t) a_src[t] = (uint32_t)(((t * NW + wave) * 8 + (lane >> 3)) * p.lda * 2 + (kchunk << 4));
+  for (int t = 0; t < A_LOADS; ++t) {
+    if (A_KMAJOR) {
+      a_src[t] = (uint32_t)(((t * NW + wave) * 8 + (lane >> 3)) * p.lda * 2 + (kchunk << 4));
+    } else {
+      const int c = (t * NW + wave) * 64 + lane;
+      const int krow = c / BM_CHUNKS;
+      a_src[t] = (uint32_t)(krow * p.lda * 2 + (((c % BM_CHUNKS) ^ swz_ring<BM>(krow)) << 4));
+    }
+  }
 #pragma unroll
   for (int t = 0; t < B_LOADS; ++t) {
     if (B_KMAJOR) {
@@ -97,11 +109,11 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   }
   // last K tile: this lane's chunk lies past K (whole chunks: K % 8 == 0)
   const uint32_t tail = kchunk * 8 >= kn - (int64_t)(KT - 1) * BK ? 0xFFFFFFF0u : 0u;
-  const uint32_t b_kstep = B_KMAJOR ? BK * 2 : (uint32_t)(BK * p.ldb * 2);
+  const uint32_t a_kstep = A_KMAJOR ? BK * 2 : (uint32_t)(BK * p.lda * 2), b_kstep = B_KMAJOR ? BK * 2 : (uint32_t)(BK * p.ldb * 2);
   const uint32_t smem_lds = (uint32_t)(uintptr_t)smem;
   auto issue_one = [&](int g, int kt, uint32_t stage) {
     const uint32_t oob = kt == KT - 1 ? tail : 0u;
-    if (g < A_LOADS) buffer_to_lds_b128(a_rsrc, a_src[g] | oob, (uint32_t)kt * (BK * 2), stage + (g * NW + wave) * 1024);
+    if (g < A_LOADS) buffer_to_lds_b128(a_rsrc, A_KMAJOR ? a_src[g] | oob : a_src[g], (uint32_t)kt * a_kstep, stage + (g * NW + wave) * 1024);
     else buffer_to_lds_b128(b_rsrc, B_KMAJOR ? b_src[g - A_LOADS] | oob : b_src[g - A_LOADS], (uint32_t)kt * b_kstep,
                             stage + A_BYTES + ((g - A_LOADS) * NW + wave) * 1024);
   };
@@ -112,7 +124,15 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   int kc[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s) kc[s] = ((4 * s + g4) ^ rswz) << 4;
-  int b_rd[TN];
+  int a_rd[A_KMAJOR ? 1 : TM], b_rd[TN];
+  if constexpr (!A_KMAJOR) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m_off = (wm * TM + i) * 16 + 4 * (l16 & 3);
+      const int krow = 8 * g4 + (l16 >> 2);
+      a_rd[i] = krow * (BM * 2) + (((m_off >> 3) ^ swz_ring<BM>(krow)) << 4) + (m_off & 7) * 2;
+    }
+  }
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
     if (B_KMAJOR) {
@@ -126,7 +146,13 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   bf16x8 a[2][TM], b[2][TN];
   auto read_one = [&](const char* st, int s, int r) {  // r-th operand of k-step s: A operands first
     if (r < TM) {
-      a[s][r] = lds_read_b128(st, a_row + r * 2048 + kc[s]);
+      if constexpr (A_KMAJOR) {
+        a[s][r] = lds_read_b128(st, a_row + r * 2048 + kc[s]);
+      } else {
+        const s16x4 lo = lds_read_tr16_b64(st, a_rd[r] + 32 * s * (BM * 2));
+        const s16x4 hi = lds_read_tr16_b64(st, a_rd[r] + (32 * s + 4) * (BM * 2));
+        a[s][r] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
     } else if (B_KMAJOR) {
       b[s][r - TM] = lds_read_b128(st, b_rd[r - TM] + kc[s]);
     } else {  // k rows + 32 s and + 4: the row bits the swizzle uses do not change

@@ -1,0 +1,239 @@
+// Host side of the operators beside the compressed linear layer: 8-bit checkpoints of activations and what reads them.
+// As in acc_api.hip nothing is allocated and nothing synchronised: every entry point only enqueues on the caller's stream.
+#include "acc_act8.h"
+#include "acc_gemm16.h"
+#include "acc_gemm_ring.h"
+#include "acc_host.h"
+
+namespace acc {
+namespace {
+
+// ---- 8-bit checkpoints ------------------------------------------------------------------------------
+bool valid_format(int32_t f) { return f == ACC_ACT8_E4M3 || f == ACC_ACT8_INT8; }
+
+// Sizes and strides that the calls without an acc_linear_desc share: rows of `c` elements, `ld` apart (0: dense).
+int validate_rows(int64_t n, int64_t c, int64_t* ld) {
+  if (n <= 0 || n > (int64_t)1 << 30 || c <= 0 || c > (1 << 21) || c % 8) return ACC_ERR_SHAPE;
+  if (!*ld) *ld = c;
+  return *ld < c || *ld % 8 || *ld > ((int64_t)1 << 24) ? ACC_ERR_SHAPE : ACC_OK;
+}
+
+// f(a value of the element type, the format as a constant)
+template <typename F> void with_act8(int32_t dtype, int32_t format, F&& f) {
+  auto typed = [&](auto value) {
+    if (format == ACC_ACT8_E4M3) f(value, std::integral_constant<int, ACC_ACT8_E4M3>{});
+    else f(value, std::integral_constant<int, ACC_ACT8_INT8>{});
+  };
+  if (dtype == ACC_BF16) typed(bf16{});
+  else typed(float{});
+}
+
+void act8_pack(int32_t dtype, int32_t format, const void* X, int64_t n, int64_t c, int64_t ld, void* Q, void* E, Launcher& L) {
+  with_act8(dtype, format, [&](auto value, auto fmt) {
+    using T = decltype(value);
+    L(act8_pack_kernel<T, decltype(fmt)::value>, dim3((unsigned)act_work_groups(n, c)), dim3(256), (const T*)X, n, c, ld, (uint8_t*)Q, (uint8_t*)E);
+  });
+}
+
+void act8_unpack(int32_t dtype, int32_t format, const void* Q, const void* E, int64_t n, int64_t c, int64_t ld, void* X, Launcher& L) {
+  with_act8(dtype, format, [&](auto value, auto fmt) {
+    using T = decltype(value);
+    L(act8_unpack_kernel<T, decltype(fmt)::value>, dim3((unsigned)act_work_groups(n, c)), dim3(256), (const uint8_t*)Q, (const uint8_t*)E, n, c, ld, (T*)X);
+  });
+}
+
+// ---- products over the tokens -------------------------------------------------------------------------
+// C[M, N] (op)= At^T . B with At [K, M] and B [K, N]: both operands of the ring kernel by transposing reads.
+template <int TM, int TN, int NS, typename TC, bool SUM>
+void ring_token_gemm(FastGemmParams& p, Launcher& L) {
+  const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
+  p.red_stride = (int64_t)grid * 256 * 4;
+  L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, TC, false, SUM, false>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+}
+
+template <typename TC, bool SUM>
+void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, Launcher& L) {
+  FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, nullptr, 1.f, 1.f);
+  const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
+  const GemmChoice c = pick_gemm_tile(M, N, K, persist_ok);
+  switch (c.tile) {
+    case GemmTile::k256:
+      if constexpr (sizeof(TC) == 2 && !SUM) {
+        const unsigned slots = gemm_bf16_plan(p, 256, 256);
+        p.red_stride = (int64_t)256 * 256 * 4;
+        L.launch_lds(gemm16_persist_kernel<false, true, false>, dim3(256), dim3(256), (size_t)160 * 1024, p, (int)slots);
+      }
+      break;
+    case GemmTile::k256x192:
+    case GemmTile::k192x128:
+      if (c.one_round) ring_token_gemm<6, 4, 3, TC, SUM>(p, L);
+      else ring_token_gemm<6, 4, 2, TC, SUM>(p, L);
+      break;
+    case GemmTile::k128:
+      if (c.one_round) ring_token_gemm<4, 4, 3, TC, SUM>(p, L);
+      else ring_token_gemm<4, 4, 2, TC, SUM>(p, L);
+      break;
+    case GemmTile::k128x64: ring_token_gemm<4, 2, 3, TC, SUM>(p, L); break;
+    case GemmTile::k64: ring_token_gemm<2, 2, 3, TC, SUM>(p, L); break;
+  }
+}
+
+// C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.
+void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t M,
+                   int64_t N, int64_t K, bool accumulate, Launcher& L) {
+  if (io == ACC_BF16) {
+    auto typed = [&](auto type) {
+      using TC = decltype(type);
+      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L);
+      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L);
+    };
+    if (dtype == ACC_BF16) typed(bf16{});
+    else typed(float{});
+    return;
+  }
+  f32_product(F32Operand{A, lda, false, false}, F32Operand{B, ldb, false, false}, C, dtype, ldc, M, N, K, accumulate, L);
+}
+
+// Tokens of one such product: a buffer resource has to reach over the wider operand.  A multiple of 64, so of a block too.
+int64_t token_chunk(int64_t n, int64_t ld, int32_t io) {
+  const int64_t most = kMaxOperandBytes / (ld * (int64_t)dtype_size(io)) - 64;
+  return n <= most ? n : most / 64 * 64;
+}
+
+size_t act8_workspace_bytes(const acc_linear_desc* d, const Shape& s) {
+  return (size_t)token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, d->io_dtype) * (size_t)s.d_in * dtype_size(d->io_dtype);
+}
+
+int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
+  if (!d) return ACC_ERR_INVALID_ARG;
+  if (!valid_dtype(d->io_dtype) || !valid_format(d->format)) return ACC_ERR_DTYPE;
+  *ldg = d->ldg;
+  *ldh = d->ldh;
+  const int rc = validate_rows(d->n, d->f, ldg);
+  return rc != ACC_OK ? rc : validate_rows(d->n, d->f, ldh);
+}
+
+}  // namespace
+}  // namespace acc
+
+using namespace acc;
+
+extern "C" {
+
+int acc_act8_pack(const acc_act8_desc* desc, const void* X, void* Q, void* E, void* stream) {
+  if (!desc) return ACC_ERR_INVALID_ARG;
+  if (!valid_dtype(desc->io_dtype) || !valid_format(desc->format)) return ACC_ERR_DTYPE;
+  int64_t ld = desc->ldx;
+  int rc = validate_rows(desc->n, desc->c, &ld);
+  if (rc != ACC_OK) return rc;
+  if (!X || !Q || !E) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(X) || !aligned16(Q) || !aligned16(E)) return ACC_ERR_ALIGN;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  act8_pack(desc->io_dtype, desc->format, X, desc->n, desc->c, ld, Q, E, L);
+  return L.status();
+}
+
+int acc_act8_unpack(const acc_act8_desc* desc, const void* Q, const void* E, void* X, void* stream) {
+  if (!desc) return ACC_ERR_INVALID_ARG;
+  if (!valid_dtype(desc->io_dtype) || !valid_format(desc->format)) return ACC_ERR_DTYPE;
+  int64_t ld = desc->ldx;
+  int rc = validate_rows(desc->n, desc->c, &ld);
+  if (rc != ACC_OK) return rc;
+  if (!X || !Q || !E) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(X) || !aligned16(Q) || !aligned16(E)) return ACC_ERR_ALIGN;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  act8_unpack(desc->io_dtype, desc->format, Q, E, desc->n, desc->c, ld, X, L);
+  return L.status();
+}
+
+int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, const void* W, void* Y, void* Q, void* E,
+                        void* stream) {
+  Shape s;
+  int rc = validate_desc(desc, &s);
+  if (rc != ACC_OK) return rc;
+  if (!valid_format(format)) return ACC_ERR_DTYPE;
+  const bool keep = !(desc->flags & ACC_FLAG_SKIP_SKETCH);
+  if (!X || !W || !Y || (keep && (!Q || !E))) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Q) || !aligned16(E)) return ACC_ERR_ALIGN;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  // the checkpoint first: it leaves X in the memory-side cache for the product, as the sketch does
+  if (keep) act8_pack(desc->io_dtype, format, X, s.n, s.d_in, s.ldx, Q, E, L);
+  exact_forward_gemm(desc, s, X, W, Y, L);
+  return L.status();
+}
+
+size_t acc_linear_act8_workspace_bytes(const acc_linear_desc* desc) {
+  Shape s;
+  if (validate_desc(desc, &s) != ACC_OK) return 0;
+  return act8_workspace_bytes(desc, s);
+}
+
+int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY, const void* W, const void* Q, const void* E,
+                        void* dX, void* dW, void* workspace, size_t ws_bytes, void* stream) {
+  Shape s;
+  int rc = validate_desc(desc, &s);
+  if (rc != ACC_OK) return rc;
+  if (!valid_format(format)) return ACC_ERR_DTYPE;
+  if (desc->flags & ACC_FLAG_SKIP_SKETCH) return ACC_ERR_INVALID_ARG;
+  if (!dY || (!dX && !dW) || (dX && !W) || (dW && (!Q || !E))) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(dY) || !aligned16(W) || !aligned16(Q) || !aligned16(E) || !aligned16(dX) || !aligned16(dW) || !aligned16(workspace))
+    return ACC_ERR_ALIGN;
+  if (dW && (!workspace || ws_bytes < act8_workspace_bytes(desc, s))) return ACC_ERR_WORKSPACE;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  if (dX) exact_backward_gemm(desc, s, dY, W, dX, L);
+  if (dW) {
+    const bool w_oi = (desc->flags & ACC_FLAG_W_OUT_IN) != 0;
+    const int64_t chunk = token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, desc->io_dtype);
+    for (int64_t t0 = 0; t0 < s.n; t0 += chunk) {
+      const int64_t nt = s.n - t0 < chunk ? s.n - t0 : chunk;
+      const char* dy = (const char*)dY + (size_t)t0 * s.ldy * dtype_size(desc->io_dtype);
+      act8_unpack(desc->io_dtype, format, (const char*)Q + t0 * s.d_in, (const char*)E + t0 / kActBlock * s.d_in, nt, s.d_in, s.d_in, workspace, L);
+      const bool add = t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
+      if (w_oi) token_product(desc->io_dtype, desc->dw_dtype, dy, s.ldy, workspace, s.d_in, dW, s.d_in, s.d_out, s.d_in, nt, add, L);
+      else token_product(desc->io_dtype, desc->dw_dtype, workspace, s.d_in, dy, s.ldy, dW, s.d_out, s.d_in, s.d_out, nt, add, L);
+    }
+  }
+  return L.status();
+}
+
+int acc_gated_fwd_act8(const acc_gated_desc* desc, const void* G, const void* U, void* H, void* Qg, void* Eg, void* Qu,
+                       void* Eu, void* stream) {
+  int64_t ldg, ldh;
+  int rc = validate_gated(desc, &ldg, &ldh);
+  if (rc != ACC_OK) return rc;
+  if (!G || !U || !H || !Qg || !Eg || !Qu || !Eu) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(G) || !aligned16(U) || !aligned16(H) || !aligned16(Qg) || !aligned16(Eg) || !aligned16(Qu) || !aligned16(Eu))
+    return ACC_ERR_ALIGN;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  with_act8(desc->io_dtype, desc->format, [&](auto value, auto fmt) {
+    using T = decltype(value);
+    L(gated_fwd_kernel<T, decltype(fmt)::value>, dim3((unsigned)act_work_groups(desc->n, desc->f)), dim3(256), (const T*)G, (const T*)U, desc->n, desc->f,
+      ldg, ldh, (T*)H, (uint8_t*)Qg, (uint8_t*)Eg, (uint8_t*)Qu, (uint8_t*)Eu);
+  });
+  return L.status();
+}
+
+int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Qg, const void* Eg, const void* Qu,
+                       const void* Eu, void* dG, void* dU, void* H, void* stream) {
+  int64_t ldg, ldh;
+  int rc = validate_gated(desc, &ldg, &ldh);
+  if (rc != ACC_OK) return rc;
+  if (!dH || !Qg || !Eg || !Qu || !Eu || !dG || !dU) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(dH) || !aligned16(Qg) || !aligned16(Eg) || !aligned16(Qu) || !aligned16(Eu) || !aligned16(dG) || !aligned16(dU) || !aligned16(H))
+    return ACC_ERR_ALIGN;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  Launcher L{(hipStream_t)stream};
+  with_act8(desc->io_dtype, desc->format, [&](auto value, auto fmt) {
+    using T = decltype(value);
+    L(gated_bwd_kernel<T, decltype(fmt)::value>, dim3((unsigned)act_work_groups(desc->n, desc->f)), dim3(256), (const T*)dH, (const uint8_t*)Qg,
+      (const uint8_t*)Eg, (const uint8_t*)Qu, (const uint8_t*)Eu, desc->n, desc->f, ldg, ldh, (T*)dG, (T*)dU, (T*)H);
+  });
+  return L.status();
+}
+
+}  // extern "C"

@@ -1,0 +1,103 @@
+"""Refusals of the 8-bit checkpoint calls, before anything touches a GPU, and the mirrors of their descriptors."""
+import ctypes
+import os
+import re
+
+import pytest
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "acc.h")
+acc = pytest.importorskip("paper_2605_01255_amd.binding", reason="libacc.so not built")
+FINE = (0, -6)   # passed validation (without a GPU the device check refuses)
+
+
+@pytest.mark.parametrize("name,mirror,size", [("acc_act8_desc", "AccAct8Desc", 32), ("acc_gated_desc", "AccGatedDesc", 40)])
+def test_descriptors_match_the_header(name, mirror, size):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (name, name), text, flags=re.S).group(1)
+    ctype = {"int64_t": ctypes.c_int64, "int32_t": ctypes.c_int32, "uint32_t": ctypes.c_uint32}
+    fields = [(n, ctype[t]) for t, n in re.findall(r"\b(int64_t|int32_t|uint32_t)\s+(\w+)\s*;", body)]
+    assert fields == list(getattr(acc, mirror)._fields_) and ctypes.sizeof(getattr(acc, mirror)) == size
+
+
+def test_constants_match_the_header():
+    text = open(HEADER).read()
+    assert "ACC_ACT8_E4M3 = 0, ACC_ACT8_INT8 = 1" in text and (acc.ACC_ACT8_E4M3, acc.ACC_ACT8_INT8) == (0, 1)
+    assert int(re.search(r"#define ACC_ACT8_BLOCK (\d+)", text).group(1)) == acc.ACC_ACT8_BLOCK == 32
+
+
+BAD_ROWS = [dict(n=0), dict(n=-1), dict(n=(1 << 30) + 1), dict(w=0), dict(w=12), dict(w=(1 << 21) + 8), dict(ld=56), dict(ld=68), dict(ld=(1 << 24) + 8)]
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS, ids=str)
+def test_sizes_and_strides_are_refused(bad):
+    kw = {**dict(n=100, w=64, ld=0), **bad}
+    d = acc.make_act8_desc(kw["n"], kw["w"], ldx=kw["ld"])
+    assert acc._lib.acc_act8_pack(ctypes.byref(d), 0x1000, 0x2000, 0x3000, None) == -2
+    assert acc._lib.acc_act8_unpack(ctypes.byref(d), 0x1000, 0x2000, 0x3000, None) == -2
+    for g in (acc.make_gated_desc(kw["n"], kw["w"], ldg=kw["ld"]), acc.make_gated_desc(kw["n"], kw["w"], ldh=kw["ld"])):
+        assert acc._lib.acc_gated_fwd_act8(ctypes.byref(g), *range(0x1000, 0x8000, 0x1000), None) == -2
+        assert acc._lib.acc_gated_bwd_act8(ctypes.byref(g), *range(0x1000, 0x9000, 0x1000), None) == -2
+
+
+def _each_pointer(call, count, optional=()):
+    ptrs = [0x1000 * (k + 1) for k in range(count)]
+    assert call(*ptrs) in FINE
+    for k in range(count):
+        bad = list(ptrs)
+        bad[k] = None
+        assert (call(*bad) in FINE) if k in optional else call(*bad) == -1, k
+        bad[k] = ptrs[k] + 8
+        assert call(*bad) == -3, k
+
+
+def test_pointers_formats_and_types_are_refused():
+    lib = acc._lib
+    for fn in (lib.acc_act8_pack, lib.acc_act8_unpack):
+        _each_pointer(lambda *p: fn(ctypes.byref(acc.make_act8_desc(33, 64)), *p, None), 3)
+        assert fn(None, 0x1000, 0x2000, 0x3000, None) == -1
+        assert fn(ctypes.byref(acc.make_act8_desc(33, 64, format=2)), 0x1000, 0x2000, 0x3000, None) == -4
+        assert fn(ctypes.byref(acc.make_act8_desc(33, 64, io_dtype=2)), 0x1000, 0x2000, 0x3000, None) == -4
+    g = acc.make_gated_desc(33, 64)
+    _each_pointer(lambda *p: lib.acc_gated_fwd_act8(ctypes.byref(g), *p, None), 7)
+    _each_pointer(lambda *p: lib.acc_gated_bwd_act8(ctypes.byref(g), *p, None), 8, optional=(7,))
+    for bad in (dict(format=-1), dict(io_dtype=5)):
+        assert lib.acc_gated_fwd_act8(ctypes.byref(acc.make_gated_desc(33, 64, **bad)), *range(0x1000, 0x8000, 0x1000), None) == -4
+    assert lib.acc_gated_fwd_act8(None, *range(0x1000, 0x8000, 0x1000), None) == -1
+    assert lib.acc_gated_bwd_act8(None, *range(0x1000, 0x9000, 0x1000), None) == -1
+
+
+def test_the_linear_layers_calls_are_refused():
+    lib = acc._lib
+    d = acc.make_desc(100, 64, 128, 8)
+
+    def fwd(*p, desc=d, fmt=0):
+        return lib.acc_linear_fwd_act8(ctypes.byref(desc), fmt, *p, None)
+
+    ptrs = (0x1000, 0x2000, 0x3000, 0x4000, 0x5000)
+    _each_pointer(fwd, 5)
+    assert fwd(*ptrs, fmt=2) == -4 and lib.acc_linear_fwd_act8(None, 0, *ptrs, None) == -1
+    skip = acc.make_desc(100, 64, 128, 8, flags=acc.ACC_FLAG_SKIP_SKETCH)
+    assert fwd(0x1000, 0x2000, 0x3000, None, None, desc=skip) in FINE       # a shared input keeps one checkpoint
+    assert fwd(*ptrs, desc=acc.make_desc(0, 64, 128, 8)) == -2
+    assert fwd(*ptrs, desc=acc.make_desc(100, 64, 128, 8, flags=1 << 8)) == -1
+
+    need = acc.acc_linear_act8_workspace_bytes(d)
+    assert need == 100 * 64 * 2 and acc.acc_linear_act8_workspace_bytes(acc.make_desc(100, 60, 128, 8)) == 0
+
+    def bwd(dY=0x1000, W=0x2000, Q=0x3000, E=0x4000, dX=0x5000, dW=0x6000, ws=0x7000, size=need, desc=d, fmt=1):
+        return lib.acc_linear_bwd_act8(ctypes.byref(desc), fmt, dY, W, Q, E, dX, dW, ws, size, None)
+
+    assert bwd() in FINE and bwd(fmt=2) == -4 and bwd(desc=skip) == -1
+    assert bwd(dY=None) == -1 and bwd(W=None) == -1 and bwd(Q=None) == -1 and bwd(E=None) == -1
+    assert bwd(dX=None, dW=None) == -1
+    assert bwd(dX=None, W=None) in FINE and bwd(dW=None, Q=None, E=None, ws=None, size=0) in FINE
+    assert bwd(ws=None) == -5 and bwd(size=need - 1) == -5
+    for name in ("dY", "W", "Q", "E", "dX", "dW", "ws"):
+        assert bwd(**{name: 0x9008}) == -3, name
+    assert lib.acc_linear_bwd_act8(None, 0, *range(0x1000, 0x8000, 0x1000), need, None) == -1
+
+
+def test_the_workspace_of_long_inputs_is_that_of_a_part():
+    # an operand of a product reaches over 4 GiB at most: more tokens take several products through one workspace
+    part = acc.acc_linear_act8_workspace_bytes(acc.make_desc(1 << 20, 4096, 4096, 8))
+    assert part <= 1 << 32 and acc.acc_linear_act8_workspace_bytes(acc.make_desc(1 << 21, 4096, 4096, 8)) == part
