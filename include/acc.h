@@ -323,6 +323,44 @@ int acc_gated_fwd_act8(const acc_gated_desc* desc, const void* G, const void* U,
 int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Qg, const void* Eg, const void* Qu,
                        const void* Eu, void* dG, void* dU, void* H, void* stream);
 
+/* ---- Softmax cross entropy of a product with the vocabulary's matrix -----------------------------------
+ * The last product of a language model and its loss, without the logits: pieces of the vocabulary pass through the workspace
+ * and nothing of the size [n, v] is kept, forward or backward.  W is in the layout of an embedding table and of
+ * torch.nn.Linear, [v, d].
+ *   z = X.W^T;  lse_i = log sum_v exp z_iv;  loss_i = lse_i - z_i,target          (float)
+ *   dz_iv = dloss_i (exp(z_iv - lse_i) - [v = target_i]);  dX = dz.W;  dW = dz^T.X
+ * The backward call forms the logits again, piece by piece.  bfloat16: products of bfloat16 operands accumulated in float, dz
+ * rounded to bfloat16 as their operand, dX and dW rounded once.  float: float throughout.
+ *   targets [n]  int64, device.  Negative: the token has no loss (loss and stats 0, a zero row of dX, no part in dW, and what its row
+ *                of X holds, infinities and NaN included, is not read into any sum).  v and above: loss NaN, no gradient.
+ *   loss [n]     float;  stats [2, n] float: lse, then the target's logit, which the backward call reads.
+ *   dloss [n]    float, the gradient of every token's loss (1 / tokens with a loss for their mean).
+ * n above 2^18, or X of more than 2 GiB, is worked off in runs of tokens, and a bfloat16 dW is then rounded once per run.
+ * A row of logits of which none is finite gives what the formulas give (infinities, NaN). */
+typedef struct acc_ce_desc {
+  int64_t n;         /* tokens, 1 .. 2^30                                                    */
+  int64_t d;         /* features, a multiple of 8, at most 2^16                              */
+  int64_t v;         /* vocabulary, 1 .. 2^21, any size                                      */
+  int64_t ldx;       /* row stride of X and dX in elements, a multiple of 8, at most 2^18; 0 = d */
+  int64_t ldw;       /* row stride of W (and not of dW, which is dense), likewise; 0 = d     */
+  int64_t piece;     /* columns of a piece, a multiple of 256; 0 = as many as keep a piece within 512 MiB */
+  int32_t io_dtype;  /* acc_dtype of X, W and dX                                             */
+  int32_t dw_dtype;  /* acc_dtype of dW                                                      */
+  uint32_t flags;    /* ACC_FLAG_DW_ACCUMULATE: dW += (acc_linear_ce_bwd)                    */
+  uint32_t reserved; /* 0                                                                    */
+} acc_ce_desc;
+
+/* Bytes of device workspace of the forward (is_backward == 0) or backward call, the latter never less; 0 = invalid. */
+size_t acc_linear_ce_workspace_bytes(const acc_ce_desc* desc, int is_backward);
+
+/* loss and stats are overwritten. */
+int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, const int64_t* targets, float* loss, float* stats,
+                      void* workspace, size_t ws_bytes, void* stream);
+/* stats as acc_linear_ce_fwd left them for the same X, W and targets.  dX [n, ldx] and dW [v, d] (dense); one of them may be
+ * NULL. */
+int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* stats,
+                      const float* dloss, void* dX, void* dW, void* workspace, size_t ws_bytes, void* stream);
+
 /* Test hook: the Philox integer stream behind S.  out is a device array of
  * ceil(n/4) * r * 4 uint32 laid out [token group q][column j][word w]. */
 int acc_philox_dump_u32(uint64_t seed, uint64_t row_offset, int64_t n, int64_t r, uint32_t* out,

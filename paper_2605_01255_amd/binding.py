@@ -31,6 +31,7 @@ EXPORTS = ("acc_linear_workspace_bytes", "acc_linear_fwd", "acc_linear_fwd_stati
            "acc_lowrank_projector", "acc_lowrank_adamw_step",
            "acc_act8_pack", "acc_act8_unpack", "acc_linear_fwd_act8", "acc_linear_act8_workspace_bytes",
            "acc_linear_bwd_act8", "acc_gated_fwd_act8", "acc_gated_bwd_act8",
+           "acc_linear_ce_workspace_bytes", "acc_linear_ce_fwd", "acc_linear_ce_bwd",
            "acc_philox_dump_u32", "acc_probe_mfma",
            "acc_sketch_dump", "acc_status_string", "acc_version")
 
@@ -61,6 +62,13 @@ class AccGatedDesc(ctypes.Structure):
     """Mirror of `acc_gated_desc`."""
     _fields_ = [("n", ctypes.c_int64), ("f", ctypes.c_int64), ("ldg", ctypes.c_int64), ("ldh", ctypes.c_int64),
                 ("io_dtype", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class AccCeDesc(ctypes.Structure):
+    """Mirror of `acc_ce_desc`."""
+    _fields_ = [("n", ctypes.c_int64), ("d", ctypes.c_int64), ("v", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("ldw", ctypes.c_int64), ("piece", ctypes.c_int64), ("io_dtype", ctypes.c_int32),
+                ("dw_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 class AccError(RuntimeError):
@@ -123,6 +131,13 @@ _lib.acc_gated_fwd_act8.restype = ctypes.c_int
 _lib.acc_gated_fwd_act8.argtypes = [_gdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.acc_gated_bwd_act8.restype = ctypes.c_int
 _lib.acc_gated_bwd_act8.argtypes = [_gdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_cdp = ctypes.POINTER(AccCeDesc)
+_lib.acc_linear_ce_workspace_bytes.restype = _sz
+_lib.acc_linear_ce_workspace_bytes.argtypes = [_cdp, ctypes.c_int]
+_lib.acc_linear_ce_fwd.restype = ctypes.c_int
+_lib.acc_linear_ce_fwd.argtypes = [_cdp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.acc_linear_ce_bwd.restype = ctypes.c_int
+_lib.acc_linear_ce_bwd.argtypes = [_cdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.acc_philox_dump_u32.restype = ctypes.c_int
 _lib.acc_philox_dump_u32.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, _vp, _vp]
 _lib.acc_sketch_dump.restype = ctypes.c_int
@@ -356,6 +371,30 @@ def acc_gated_bwd_act8(desc, dH, Qg, Eg, Qu, Eu, dG, dU, H=None, stream=None):
     """Enqueue dG and dU from the checkpoints and (H is not None) the activation again."""
     _check(_lib.acc_gated_bwd_act8(ctypes.byref(desc), _ptr(dH), _ptr(Qg), _ptr(Eg), _ptr(Qu), _ptr(Eu), _ptr(dG),
                                    _ptr(dU), _ptr(H), _stream(stream)))
+
+
+def make_ce_desc(n, d, v, ldx=0, ldw=0, piece=0, io_dtype=ACC_BF16, dw_dtype=None, flags=0) -> AccCeDesc:
+    return AccCeDesc(n, d, v, ldx, ldw, piece, io_dtype, io_dtype if dw_dtype is None else dw_dtype, flags, 0)
+
+
+def acc_linear_ce_workspace_bytes(desc: AccCeDesc, is_backward: bool) -> int:
+    return int(_lib.acc_linear_ce_workspace_bytes(ctypes.byref(desc), 1 if is_backward else 0))
+
+
+def acc_linear_ce_fwd(desc, X, W, targets, loss, stats, workspace, stream=None, ws_bytes=None):
+    """Enqueue the per-token losses of X.W^T against `targets` (int64) and what the backward call reads of them."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_linear_ce_fwd(ctypes.byref(desc), _ptr(X), _ptr(W), _ptr(targets), _ptr(loss), _ptr(stats),
+                                  _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def acc_linear_ce_bwd(desc, X, W, targets, stats, dloss, dX, dW, workspace, stream=None, ws_bytes=None):
+    """Enqueue dX and dW of sum(dloss * loss); either may be None."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_linear_ce_bwd(ctypes.byref(desc), _ptr(X), _ptr(W), _ptr(targets), _ptr(stats), _ptr(dloss),
+                                  _ptr(dX), _ptr(dW), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def acc_philox_dump_u32(seed, row_offset, n, r, out, stream=None):

@@ -91,8 +91,9 @@ F32GemmParams f32_params(const F32Operand& a, const F32Operand& b, void* C, int6
 template <typename TC>
 void f32_gemm(const F32Operand& a, const F32Operand& b, void* C, int64_t ldc, int64_t M, int64_t N, int64_t K, Launcher& L,
               bool accumulate = false, float alpha = 1.f, float beta = 1.f, int64_t k_per_split = 0,
-              int64_t c_split_stride = 0, int sum_tiles = 8) {
+              int64_t c_split_stride = 0, int sum_tiles = 8, int64_t kb_rows = 0) {
   F32GemmParams p = f32_params(a, b, C, ldc, M, N, K);
+  p.kb_rows = kb_rows;
   p.accumulate = accumulate ? 1 : 0; p.alpha = alpha; p.beta = beta;
   if (k_per_split) p.k_per_split = k_per_split;
   p.c_split_stride = c_split_stride;
@@ -316,8 +317,9 @@ bool factor_gemm(FastGemmParams& p, Launcher& L) {
 template <bool KMAJ, typename TC, bool SUM = false>
 void fast_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda,
                int64_t ldb, int64_t ldc, Launcher& L, const ReduceJob* job = nullptr, float alpha = 1.f,
-               float beta = 1.f) {
+               float beta = 1.f, int64_t kb_rows = 0) {
   FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, job, alpha, beta);
+  p.kb_rows = kb_rows;
   const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
   if (!SUM && K <= 128 && ceil_div(M, 256) * ceil_div(N, 256) >= 192) {
     factor_gemm<KMAJ, TC, SUM>(p, L);
@@ -831,7 +833,14 @@ void exact_backward_gemm(const acc_linear_desc* desc, const Shape& s, const void
 }
 
 void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtype, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                 bool accumulate, Launcher& L) {
+                 bool accumulate, Launcher& L, bool padded) {
+  if (padded && dtype == ACC_F32) {
+    const int64_t kp = a.kmajor ? round_up(K, 4) : K;
+    if (f32_gemm_ok(a, b, M, round_up(N, 4), kp, C, ldc)) {
+      f32_gemm<float>(a, b, C, ldc, M, N, kp, L, accumulate, 1.f, 1.f, 0, 0, 8, K);
+      return;
+    }
+  }
   GemmParams p{};
   p.A = a.ptr; p.B = b.ptr; p.C = C;
   p.M = M; p.N = N; p.K = K;
@@ -843,6 +852,16 @@ void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtyp
   p.alpha = p.beta = 1.f;
   if (dtype == ACC_BF16) launch_generic<float, float, bf16, float, false, true>(p, 1, L);
   else launch_generic<float, float, float, float, false, true>(p, 1, L);
+}
+
+void bf16_logits(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, Launcher& L) {
+  fast_gemm<true, float>(A, B, C, M, N, K, lda, ldb, ldc, L);
+}
+
+void bf16_input_gradient(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K,
+                         bool accumulate, Launcher& L) {
+  if (accumulate) fast_gemm<false, float, true>(A, B, C, M, N, round_up(K, 8), lda, ldb, ldc, L, nullptr, 1.f, 1.f, K);
+  else fast_gemm<false, float>(A, B, C, M, N, round_up(K, 8), lda, ldb, ldc, L, nullptr, 1.f, 1.f, K);
 }
 
 namespace {

@@ -1,0 +1,213 @@
+// The vocabulary's product and its softmax cross entropy without the logits:  z = X . W^T in pieces of the vocabulary,
+//   lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_i,target;   dz_iv = g_i (exp(z_iv - lse_i) - [v = target_i]),
+//   dX = dz . W,  dW = dz^T . X.
+//
+// Tokens without a loss (negative targets) take no part: the others are gathered into a dense matrix first, so that products cost what
+// the tokens with a loss cost, and infinities or NaN in a padded token's row reach no sum (0 times NaN is NaN).
+#pragma once
+#include "acc_common.h"
+
+namespace acc {
+
+// What a call knows of its tokens after the selection.  `order` lists the tokens with a loss in their order, then the others.
+struct CeTokens {
+  const int64_t* targets;   // [n]
+  int n;
+  int* order;               // [n]
+  int* count;               // tokens with a loss
+};
+
+// One work-group of 1024 threads, eight tokens of a thread at a time.
+__global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t) {
+  constexpr int PER = 8;
+  __shared__ int wave_kept[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int kept = 0;   // so far
+  for (int first = 0; first < t.n; first += 1024 * PER) {
+    const int i0 = first + tid * PER;
+    bool keep[PER];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      keep[k] = i0 + k < t.n && t.targets[i0 + k] >= 0;
+      mine += keep[k] ? 1 : 0;
+    }
+    int before = mine;   // inclusive scan over the wave
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(before, d);
+      before += lane >= d ? o : 0;
+    }
+    if (lane == 63) wave_kept[wave] = before;
+    __syncthreads();
+    int total = 0, waves_before = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      waves_before += w < wave ? wave_kept[w] : 0;
+      total += wave_kept[w];
+    }
+    __syncthreads();
+    int at = kept + waves_before + before - mine;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (keep[k]) t.order[at++] = i0 + k;
+    kept += total;
+  }
+  if (tid == 0) *t.count = kept;
+  // the others from the end of the list: token i without a loss is the (i - kept ones before it)-th of them
+  int others = 0;
+  for (int first = 0; first < t.n; first += 1024 * PER) {
+    const int i0 = first + tid * PER;
+    bool keep[PER];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      keep[k] = i0 + k < t.n && t.targets[i0 + k] < 0;
+      mine += keep[k] ? 1 : 0;
+    }
+    int before = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(before, d);
+      before += lane >= d ? o : 0;
+    }
+    if (lane == 63) wave_kept[wave] = before;
+    __syncthreads();
+    int total = 0, waves_before = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      waves_before += w < wave ? wave_kept[w] : 0;
+      total += wave_kept[w];
+    }
+    __syncthreads();
+    int at = kept + others + waves_before + before - mine;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (keep[k]) t.order[at++] = i0 + k;
+    others += total;
+  }
+}
+
+// What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero.
+// `rows` of them are written (>= n).
+template <typename T>
+__global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc,
+                                                        const float* __restrict__ stats, const float* __restrict__ dloss, int64_t stats_stride,
+                                                        float* __restrict__ per_row) {
+  constexpr int VEC = 16 / sizeof(T);
+  typedef T vecT __attribute__((ext_vector_type(VEC)));
+  const int64_t r = blockIdx.x;
+  const int count = *t.count;
+  const bool lives = r < count;
+  const int i = lives ? t.order[r] : 0;
+  for (int c = (int)threadIdx.x * VEC; c < d; c += 256 * VEC) {
+    vecT v = {};
+    if (lives) v = *(const vecT*)(X + (int64_t)i * ldx + c);
+    *(vecT*)(Xc + r * d + c) = v;
+  }
+  if (per_row && threadIdx.x == 0) {   // backward: lse, the target's logit, the incoming gradient
+    per_row[r] = lives ? stats[i] : 0.f;
+    per_row[rows + r] = lives ? stats[stats_stride + i] : 0.f;
+    per_row[2 * rows + r] = lives ? dloss[i] : 0.f;
+  }
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// A sum of exponentials as (m, s) = s exp(m); the sum of two of them.  m = -infinity: nothing yet.
+struct ExpSum {
+  float m, s;
+};
+__device__ __forceinline__ ExpSum operator+(ExpSum a, ExpSum b) {
+  const float m = fmaxf(a.m, b.m), z = isinf(m) ? 0.f : m;   // exponentials of what is infinite are 0 or infinite, never NaN
+  return ExpSum{z, a.s * expf((isinf(a.m) ? 0.f : a.m) - z) + b.s * expf((isinf(b.m) ? 0.f : b.m) - z)};
+}
+
+// Losses and statistics, one work-group per token, from the logits of one piece [rows, vp]; running sums between the pieces.
+__global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const float* __restrict__ Z, int64_t ldz, int64_t v0, int vp, bool first,
+                                                             bool last, int64_t V, float* __restrict__ run_m, float* __restrict__ run_s,
+                                                             float* __restrict__ run_z, float* __restrict__ loss, float* __restrict__ stats,
+                                                             int64_t stats_stride) {
+  __shared__ float red[8];
+  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+  const int i = t.order[r];
+  if (r >= *t.count) {
+    if (last && tid == 0) loss[i] = stats[i] = stats[stats_stride + i] = 0.f;
+    return;
+  }
+  const float* z = Z + (int64_t)r * ldz;
+  float m = -INFINITY;
+  bool nan = false;
+  for (int c = tid; c < vp; c += 256) {
+    m = fmaxf(m, z[c]);
+    nan |= z[c] != z[c];
+  }
+  m = wave_max(m);
+  if ((tid & 63) == 0) red[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if (isinf(m)) m = 0.f;
+  float s = 0.f;
+  for (int c = tid; c < vp; c += 256) s += expf(z[c] - m);
+  if (nan) s = NAN;
+  s = wave_sum(s);
+  if ((tid & 63) == 0) red[4 + wave] = s;
+  __syncthreads();
+  if (tid) return;
+  ExpSum sum{m, red[4] + red[5] + red[6] + red[7]};
+  if (!first) sum = sum + ExpSum{run_m[r], run_s[r]};
+  const int64_t target = t.targets[i];
+  if (target >= v0 && target < v0 + vp) run_z[r] = z[target - v0];
+  if (last) {
+    const float lse = sum.m + logf(sum.s), zt = target < V ? run_z[r] : NAN;
+    loss[i] = lse - zt;
+    stats[i] = lse;
+    stats[stats_stride + i] = zt;
+  } else {
+    run_m[r] = sum.m;
+    run_s[r] = sum.s;
+  }
+}
+
+// dz of one piece from its logits, one work-group per row; rows without a token and columns from vp to ldz are zero.  A target beyond
+// the vocabulary has no gradient.  TO = float: in place.
+template <typename TO>
+__global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, const float* Z, int64_t ldz, int64_t v0, int vp, int64_t V, int64_t rows,
+                                                            const float* __restrict__ per_row, TO* dZ) {
+  const int64_t r = blockIdx.x;
+  const bool lives = r < *t.count;
+  const int64_t target = lives ? t.targets[t.order[r]] : -1;
+  const bool counts = lives && target < V;
+  const float lse = per_row[r], zt = per_row[rows + r], g = per_row[2 * rows + r];
+  for (int64_t c = threadIdx.x; c < ldz; c += 256) {
+    float dz = 0.f;
+    if (counts && c < vp) dz = v0 + c == target ? g * expm1f(zt - lse) : g * expf(Z[r * ldz + c] - lse);
+    dZ[r * ldz + c] = from_f32<TO>(dz);
+  }
+}
+
+// dX [n, ldx] from the dense rows; tokens without a loss get zeros.  One work-group per row of the list.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_scatter_kernel(CeTokens t, const float* __restrict__ dXf, int d, T* __restrict__ dX, int64_t ldx) {
+  const int64_t r = blockIdx.x;
+  const bool lives = r < *t.count;
+  const int i = t.order[r];
+  for (int c = (int)threadIdx.x * 4; c < d; c += 1024) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (lives) v = *(const f32x4*)(dXf + r * d + c);
+    T* dst = dX + (int64_t)i * ldx + c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) dst[k] = from_f32<T>(v[k]);
+  }
+}
+
+}  // namespace acc

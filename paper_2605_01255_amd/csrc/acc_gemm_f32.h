@@ -36,6 +36,7 @@ struct F32GemmParams {
   int64_t k_per_split;     // multiple of 32; split s writes its partial product at C + s * c_split_stride
   int64_t c_split_stride;
   int sum_tiles;           // K tiles of one running sum, a power of two
+  int64_t kb_rows;         // N-contiguous B only: rows of B that exist (0 = K); K may exceed it when A is zero-padded along K
 };
 
 // One operand of the kernel: R rows of the output dimension (BM or BN) per tile, K_MAJOR its memory order.
@@ -133,15 +134,16 @@ __device__ __forceinline__ void gemm_f32_block(const F32GemmParams& p, const Out
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
   const int64_t k0 = (int64_t)split * p.k_per_split;
   const int64_t kn = k0 + p.k_per_split < p.K ? p.k_per_split : p.K - k0;   // this split's K range
+  const int64_t kb = p.kb_rows && p.kb_rows < k0 + kn ? p.kb_rows - k0 : kn;  // rows of an N-contiguous B in it
   const int KT = (int)((kn + BK - 1) / BK);
 
-  // ---- global -> LDS ----
-  auto rsrc_of = [&](const auto* X, int64_t x0, int64_t X_total, int64_t ld, bool kmajor) {
-    constexpr int64_t ES = sizeof(*X);
+  // ---- global -> LDS (rows of an operand that is not K-contiguous end with a whole chunk) ----
+  auto rsrc_of = [&](const auto* X, int64_t x0, int64_t X_total, int64_t ld, bool kmajor, int64_t rows) {
+    constexpr int64_t ES = sizeof(*X), CHUNK = 16 / ES;
     return kmajor ? make_rsrc(X + x0 * ld + k0, ((X_total - x0 - 1) * ld + kn) * ES)
-                  : make_rsrc(X + k0 * ld + x0, ((kn - 1) * ld + (X_total - x0)) * ES);
+                  : make_rsrc(X + k0 * ld + x0, rows > 0 ? ((rows - 1) * ld + ((X_total - x0 + CHUNK - 1) & ~(CHUNK - 1))) * ES : 0);
   };
-  const u32x4 a_rsrc = rsrc_of((const TA*)p.A, m0, p.M, p.lda, A_KMAJOR), b_rsrc = rsrc_of((const TB*)p.B, n0, p.N, p.ldb, B_KMAJOR);
+  const u32x4 a_rsrc = rsrc_of((const TA*)p.A, m0, p.M, p.lda, A_KMAJOR, kn), b_rsrc = rsrc_of((const TB*)p.B, n0, p.N, p.ldb, B_KMAJOR, kb);
   uint32_t a_src[A_LOADS], b_src[B_LOADS];
 #pragma unroll
   for (int t = 0; t < A_LOADS; ++t) a_src[t] = TileA::source(t, wave, lane, p.lda);

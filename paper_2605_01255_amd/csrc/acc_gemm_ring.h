@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   const int64_t m0 = has_tile ? (int64_t)tm * BM : 0, n0 = has_tile ? (int64_t)tn * BN : 0;
   const int64_t k0 = SPLIT ? (int64_t)split * p.k_per_split : 0;
   const int64_t kn = SPLIT && k0 + p.k_per_split < p.K ? p.k_per_split : p.K - k0;   // this work-group's K range
-  const int64_t kb = SPLIT && p.kb_rows && p.kb_rows < k0 + kn ? p.kb_rows - k0 : kn;  // rows of an N-contiguous B in it
+  const int64_t kb = p.kb_rows && p.kb_rows < k0 + kn ? p.kb_rows - k0 : kn;  // rows of an N-contiguous B in it
   const int KT = (int)((kn + BK - 1) / BK);
 
   // ---- global -> LDS: wave-load t of wave w fills LDS bytes [(t * NW + w) * 1024, +1024) of the operand tile ----

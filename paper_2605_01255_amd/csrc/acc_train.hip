@@ -1,6 +1,7 @@
 // Host side of the operators beside the compressed linear layer: 8-bit checkpoints of activations and what reads them.
 // As in acc_api.hip nothing is allocated and nothing synchronised: every entry point only enqueues on the caller's stream.
 #include "acc_act8.h"
+#include "acc_ce.h"
 #include "acc_gemm16.h"
 #include "acc_gemm_ring.h"
 #include "acc_host.h"
@@ -111,6 +112,106 @@ int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
   *ldh = d->ldh;
   const int rc = validate_rows(d->n, d->f, ldg);
   return rc != ACC_OK ? rc : validate_rows(d->n, d->f, ldh);
+}
+
+// ---- the vocabulary's cross entropy --------------------------------------------------------------------
+constexpr int64_t kCePieceBytes = (int64_t)512 << 20;
+
+struct CePlan {
+  int64_t n, d, v, ldx, ldw;
+  int64_t run;      // tokens of a run
+  int64_t rows;     // of the dense matrices: a run, and 256 at least
+  int64_t vp, ldz;  // columns of a piece, their row stride
+  size_t order, count, x, z, dz, per_row, dx;   // offsets into the workspace
+  size_t forward, backward;                      // its bytes
+};
+
+int plan_ce(const acc_ce_desc* d, CePlan* p) {
+  if (!d || (d->flags & ~(uint32_t)ACC_FLAG_DW_ACCUMULATE) || d->reserved) return ACC_ERR_INVALID_ARG;
+  if (!valid_dtype(d->io_dtype) || !valid_dtype(d->dw_dtype)) return ACC_ERR_DTYPE;
+  if (d->n <= 0 || d->n > (int64_t)1 << 30 || d->d <= 0 || d->d % 8 || d->d > (1 << 16) || d->v <= 0 || d->v > (1 << 21)) return ACC_ERR_SHAPE;
+  if (d->piece < 0 || d->piece % 256 || d->piece > (1 << 22)) return ACC_ERR_SHAPE;
+  p->n = d->n; p->d = d->d; p->v = d->v;
+  p->ldx = d->ldx ? d->ldx : d->d;
+  p->ldw = d->ldw ? d->ldw : d->d;
+  for (int64_t ld : {p->ldx, p->ldw})
+    if (ld < p->d || ld % 8 || ld > (1 << 18)) return ACC_ERR_SHAPE;
+  const int64_t es = (int64_t)dtype_size(d->io_dtype);
+  p->run = ((int64_t)2 << 30) / (p->d * es) / 256 * 256;
+  if (p->run > 1 << 18) p->run = 1 << 18;
+  if (p->run > p->n) p->run = p->n;
+  p->rows = p->run < 256 ? 256 : p->run;
+  // a piece: at most kCePieceBytes of dz, and of W what a buffer resource reaches
+  int64_t vp = d->piece ? d->piece : kCePieceBytes / (p->rows * es) / 256 * 256;
+  const int64_t most = ((int64_t)2 << 30) / (p->ldw * es) / 256 * 256;
+  const int64_t most_z = ((int64_t)2 << 30) / (p->rows * 4) / 256 * 256;
+  if (vp > most) vp = most;
+  if (vp > most_z) vp = most_z;
+  if (vp < 256) vp = 256;
+  if (vp > p->v) vp = p->v;
+  p->vp = vp;
+  p->ldz = round_up(vp, 8);
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t from = at;
+    at += (size_t)round_up(bytes, 256);
+    return from;
+  };
+  p->order = take(p->run * 4);
+  p->count = take(4);
+  p->per_row = take(3 * p->rows * 4);
+  p->x = take(p->rows * p->d * es);
+  p->z = take(p->rows * p->ldz * 4);
+  p->forward = at;
+  p->dz = d->io_dtype == ACC_F32 ? p->z : take(p->rows * p->ldz * 2);
+  p->dx = take(p->rows * p->d * 4);
+  p->backward = at;
+  return ACC_OK;
+}
+
+// A run of tokens t0 .. t0 + n - 1 and the workspace of its call.
+struct CeRun {
+  const acc_ce_desc* desc;
+  CePlan p;
+  char* ws;
+  int64_t t0, n;
+  CeTokens tokens;
+  size_t es() const { return dtype_size(desc->io_dtype); }
+  const void* w_piece(const void* W, int64_t v0) const { return (const char*)W + (size_t)v0 * p.ldw * es(); }
+  int64_t piece(int64_t v0) const { return p.v - v0 < p.vp ? p.v - v0 : p.vp; }
+};
+
+template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, const int64_t* targets, void* workspace, hipStream_t stream, F&& f) {
+  Launcher L{stream};
+  char* ws = (char*)workspace;
+  for (int64_t t0 = 0; t0 < p.n; t0 += p.run) {
+    const int64_t n = p.n - t0 < p.run ? p.n - t0 : p.run;
+    const CeRun run{desc, p, ws, t0, n, CeTokens{targets + t0, (int)n, (int*)(ws + p.order), (int*)(ws + p.count)}};
+    L(ce_select_kernel, dim3(1), dim3(1024), run.tokens);
+    f(run, L);
+  }
+  return L.status();
+}
+
+void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
+  const dim3 grid((unsigned)r.p.rows);
+  float* per_row = stats ? (float*)(r.ws + r.p.per_row) : nullptr;
+  auto typed = [&](auto value) {
+    using T = decltype(value);
+    L(ce_gather_kernel<T>, grid, dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows, (T*)(r.ws + r.p.x),
+      stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, per_row);
+  };
+  if (r.desc->io_dtype == ACC_BF16) typed(bf16{});
+  else typed(float{});
+}
+
+// Z [rows, piece] = X . W_piece^T, float.
+void ce_logits(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
+  const void* w = r.w_piece(W, v0);
+  float* z = (float*)(r.ws + r.p.z);
+  const int64_t vp = r.piece(v0);
+  if (r.desc->io_dtype == ACC_BF16) bf16_logits(r.ws + r.p.x, r.p.d, w, r.p.ldw, z, r.p.ldz, r.n, vp, r.p.d, L);
+  else f32_product(F32Operand{r.ws + r.p.x, r.p.d, true, false}, F32Operand{w, r.p.ldw, true, false}, z, ACC_F32, r.p.ldz, r.n, vp, r.p.d, false, L, true);
 }
 
 }  // namespace
@@ -234,6 +335,76 @@ int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Q
       (const uint8_t*)Eg, (const uint8_t*)Qu, (const uint8_t*)Eu, desc->n, desc->f, ldg, ldh, (T*)dG, (T*)dU, (T*)H);
   });
   return L.status();
+}
+
+size_t acc_linear_ce_workspace_bytes(const acc_ce_desc* desc, int is_backward) {
+  CePlan p;
+  if (plan_ce(desc, &p) != ACC_OK) return 0;
+  return is_backward ? p.backward : p.forward;
+}
+
+int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, const int64_t* targets, float* loss, float* stats,
+                      void* workspace, size_t ws_bytes, void* stream) {
+  CePlan p;
+  int rc = plan_ce(desc, &p);
+  if (rc != ACC_OK) return rc;
+  if (!X || !W || !targets || !loss || !stats) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(X) || !aligned16(W) || !aligned16(targets) || !aligned16(loss) || !aligned16(stats) || !aligned16(workspace)) return ACC_ERR_ALIGN;
+  if (!workspace || ws_bytes < p.forward) return ACC_ERR_WORKSPACE;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
+    ce_gather(r, X, nullptr, nullptr, L);
+    float* run = (float*)(r.ws + r.p.per_row);
+    for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
+      const int64_t vp = r.piece(v0);
+      ce_logits(r, W, v0, L);
+      L(ce_piece_stats_kernel, dim3((unsigned)r.n), dim3(256), r.tokens, (const float*)(r.ws + r.p.z), r.p.ldz, v0, (int)vp, v0 == 0, v0 + vp == r.p.v,
+        r.p.v, run, run + r.p.rows, run + 2 * r.p.rows, loss + r.t0, stats + r.t0, r.p.n);
+    }
+  });
+}
+
+int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* stats,
+                      const float* dloss, void* dX, void* dW, void* workspace, size_t ws_bytes, void* stream) {
+  CePlan p;
+  int rc = plan_ce(desc, &p);
+  if (rc != ACC_OK) return rc;
+  if (!X || !W || !targets || !stats || !dloss || (!dX && !dW)) return ACC_ERR_INVALID_ARG;
+  if (!aligned16(X) || !aligned16(W) || !aligned16(targets) || !aligned16(stats) || !aligned16(dloss) || !aligned16(dX) || !aligned16(dW) ||
+      !aligned16(workspace))
+    return ACC_ERR_ALIGN;
+  if (!workspace || ws_bytes < p.backward) return ACC_ERR_WORKSPACE;
+  if ((rc = check_device()) != ACC_OK) return rc;
+  const bool b16 = desc->io_dtype == ACC_BF16;
+  return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
+    ce_gather(r, X, stats, dloss, L);
+    const float* per_row = (const float*)(r.ws + r.p.per_row);
+    float* z = (float*)(r.ws + r.p.z);
+    float* dxf = (float*)(r.ws + r.p.dx);
+    char* dz = r.ws + r.p.dz;
+    for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
+      const int64_t vp = r.piece(v0);
+      ce_logits(r, W, v0, L);
+      const dim3 grid((unsigned)r.p.rows);
+      if (b16) L(ce_piece_grad_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)z, r.p.ldz, v0, (int)vp, r.p.v, r.p.rows, per_row, (bf16*)dz);
+      else L(ce_piece_grad_kernel<float>, grid, dim3(256), r.tokens, (const float*)z, r.p.ldz, v0, (int)vp, r.p.v, r.p.rows, per_row, (float*)dz);
+      if (dX) {
+        const void* w = r.w_piece(W, v0);
+        if (b16) bf16_input_gradient(dz, r.p.ldz, w, r.p.ldw, dxf, r.p.d, r.n, r.p.d, vp, v0 > 0, L);
+        else f32_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{w, r.p.ldw, false, false}, dxf, ACC_F32, r.p.d, r.n, r.p.d, vp, v0 > 0, L, true);
+      }
+      if (dW) {
+        char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
+        const bool add = r.t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
+        token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, r.n, add, L);
+      }
+    }
+    if (dX) {
+      const dim3 grid((unsigned)r.n);
+      if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)dxf, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
+      else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, (const float*)dxf, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
+    }
+  });
 }
 
 }  // extern "C"
