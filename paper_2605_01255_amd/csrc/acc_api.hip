@@ -317,9 +317,8 @@ bool factor_gemm(FastGemmParams& p, Launcher& L) {
 template <bool KMAJ, typename TC, bool SUM = false>
 void fast_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda,
                int64_t ldb, int64_t ldc, Launcher& L, const ReduceJob* job = nullptr, float alpha = 1.f,
-               float beta = 1.f, int64_t kb_rows = 0) {
+               float beta = 1.f) {
   FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, job, alpha, beta);
-  p.kb_rows = kb_rows;
   const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
   if (!SUM && K <= 128 && ceil_div(M, 256) * ceil_div(N, 256) >= 192) {
     factor_gemm<KMAJ, TC, SUM>(p, L);
@@ -852,16 +851,6 @@ void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtyp
   p.alpha = p.beta = 1.f;
   if (dtype == ACC_BF16) launch_generic<float, float, bf16, float, false, true>(p, 1, L);
   else launch_generic<float, float, float, float, false, true>(p, 1, L);
-}
-
-void bf16_logits(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, Launcher& L) {
-  fast_gemm<true, float>(A, B, C, M, N, K, lda, ldb, ldc, L);
-}
-
-void bf16_input_gradient(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                         bool accumulate, Launcher& L) {
-  if (accumulate) fast_gemm<false, float, true>(A, B, C, M, N, round_up(K, 8), lda, ldb, ldc, L, nullptr, 1.f, 1.f, K);
-  else fast_gemm<false, float>(A, B, C, M, N, round_up(K, 8), lda, ldb, ldc, L, nullptr, 1.f, 1.f, K);
 }
 
 namespace {

@@ -88,10 +88,11 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t) {
   }
 }
 
-// What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero.
-// `rows` of them are written (>= n).
+// What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero, up to
+// 256 of them for the products' least rows.  per_row: target (as int; -1: no gradient), and in a backward call lse, the target's
+// logit and the incoming gradient, `rows` of each.
 template <typename T>
-__global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc,
+__global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc, int64_t V,
                                                         const float* __restrict__ stats, const float* __restrict__ dloss, int64_t stats_stride,
                                                         float* __restrict__ per_row) {
   constexpr int VEC = 16 / sizeof(T);
@@ -100,15 +101,20 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
   const int count = *t.count;
   const bool lives = r < count;
   const int i = lives ? t.order[r] : 0;
+  if (threadIdx.x == 0) {
+    const int64_t target = lives ? t.targets[i] : -1;
+    ((int*)per_row)[r] = target < V ? (int)target : -1;
+    if (stats) {
+      per_row[rows + r] = lives ? stats[i] : 0.f;
+      per_row[2 * rows + r] = lives ? stats[stats_stride + i] : 0.f;
+      per_row[3 * rows + r] = lives && target < V ? dloss[i] : 0.f;
+    }
+  }
+  if (sizeof(T) == 2 && !lives && r >= 256) return;   // the float32 products read every row
   for (int c = (int)threadIdx.x * VEC; c < d; c += 256 * VEC) {
     vecT v = {};
     if (lives) v = *(const vecT*)(X + (int64_t)i * ldx + c);
     *(vecT*)(Xc + r * d + c) = v;
-  }
-  if (per_row && threadIdx.x == 0) {   // backward: lse, the target's logit, the incoming gradient
-    per_row[r] = lives ? stats[i] : 0.f;
-    per_row[rows + r] = lives ? stats[stats_stride + i] : 0.f;
-    per_row[2 * rows + r] = lives ? dloss[i] : 0.f;
   }
 }
 
@@ -123,13 +129,15 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// A sum of exponentials as (m, s) = s exp(m); the sum of two of them.  m = -infinity: nothing yet.
+// A sum of exponentials as (m, s) = s exp(m), m finite; s = 0: nothing.
 struct ExpSum {
   float m, s;
 };
 __device__ __forceinline__ ExpSum operator+(ExpSum a, ExpSum b) {
-  const float m = fmaxf(a.m, b.m), z = isinf(m) ? 0.f : m;   // exponentials of what is infinite are 0 or infinite, never NaN
-  return ExpSum{z, a.s * expf((isinf(a.m) ? 0.f : a.m) - z) + b.s * expf((isinf(b.m) ? 0.f : b.m) - z)};
+  if (a.s == 0.f) return b;
+  if (b.s == 0.f) return a;
+  const float m = fmaxf(a.m, b.m);
+  return ExpSum{m, a.s * expf(a.m - m) + b.s * expf(b.m - m)};
 }
 
 // Losses and statistics, one work-group per token, from the logits of one piece [rows, vp]; running sums between the pieces.
@@ -138,13 +146,14 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const f
                                                              float* __restrict__ run_z, float* __restrict__ loss, float* __restrict__ stats,
                                                              int64_t stats_stride) {
   __shared__ float red[8];
-  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, wave = tid >> 6;
   const int i = t.order[r];
   if (r >= *t.count) {
     if (last && tid == 0) loss[i] = stats[i] = stats[stats_stride + i] = 0.f;
     return;
   }
-  const float* z = Z + (int64_t)r * ldz;
+  const float* z = Z + r * ldz;
   float m = -INFINITY;
   bool nan = false;
   for (int c = tid; c < vp; c += 256) {
@@ -178,21 +187,64 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const f
   }
 }
 
-// dz of one piece from its logits, one work-group per row; rows without a token and columns from vp to ldz are zero.  A target beyond
-// the vocabulary has no gradient.  TO = float: in place.
-template <typename TO>
-__global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, const float* Z, int64_t ldz, int64_t v0, int vp, int64_t V, int64_t rows,
-                                                            const float* __restrict__ per_row, TO* dZ) {
+// dz of one piece from its logits, in place, one work-group per row; rows without a token and columns from vp to ldz are zero.  A
+// target beyond the vocabulary has no gradient.
+__global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, float* __restrict__ Z, int64_t ldz, int64_t v0, int vp, int64_t rows,
+                                                            const float* __restrict__ per_row) {
   const int64_t r = blockIdx.x;
-  const bool lives = r < *t.count;
-  const int64_t target = lives ? t.targets[t.order[r]] : -1;
-  const bool counts = lives && target < V;
-  const float lse = per_row[r], zt = per_row[rows + r], g = per_row[2 * rows + r];
+  const int target = ((const int*)per_row)[r];   // -1 where there is no token or no gradient
+  const float lse = per_row[rows + r], zt = per_row[2 * rows + r], g = per_row[3 * rows + r];
   for (int64_t c = threadIdx.x; c < ldz; c += 256) {
     float dz = 0.f;
-    if (counts && c < vp) dz = v0 + c == target ? g * expm1f(zt - lse) : g * expf(Z[r * ldz + c] - lse);
-    dZ[r * ldz + c] = from_f32<TO>(dz);
+    if (target >= 0 && c < vp) dz = v0 + c == target ? g * expm1f(zt - lse) : g * expf(Z[r * ldz + c] - lse);
+    Z[r * ldz + c] = dz;
   }
+}
+
+// What the product that forms dz leaves to do: the targets' elements, g (exp(z - lse) - 1), and zeros from column vp to ldz (rows end
+// with whole 16 bytes).  One thread per row.
+__global__ __launch_bounds__(256) void ce_target_kernel(const int* __restrict__ live, int64_t ldz, int64_t v0, int vp, int64_t rows,
+                                                        const float* __restrict__ per_row, bf16* __restrict__ dZ) {
+  const int r = (int)(blockIdx.x * 256 + threadIdx.x);
+  const int count = *live;
+  if (r >= rows || r >= (count < 256 ? 256 : count)) return;
+  for (int64_t c = vp; c < ldz; ++c) dZ[r * ldz + c] = (bf16)0.f;
+  const int64_t at = ((const int*)per_row)[r] - v0;
+  if (at >= 0 && at < vp) dZ[r * ldz + at] = (bf16)(per_row[3 * rows + r] * expm1f(per_row[2 * rows + r] - per_row[rows + r]));
+}
+
+// Losses and statistics from the strips' sums.  A work-group takes `across` rows (a power of two up to 32); the threads of a row
+// share its strips.
+__global__ __launch_bounds__(256) void ce_finish_kernel(CeTokens t, const f32x2* __restrict__ part, int strips, int64_t rows, int across, int64_t V,
+                                                        const float* __restrict__ target_logit, float* __restrict__ loss,
+                                                        float* __restrict__ stats, int64_t stats_stride) {
+  __shared__ ExpSum sums[256];
+  const int tid = threadIdx.x, mine = tid & (across - 1), first = tid / across, step = 256 / across;
+  const int r = (int)blockIdx.x * across + mine;
+  const bool lives = r < *t.count;
+  ExpSum sum{0.f, 0.f};
+  if (lives) {
+    for (int k = first; k < strips; k += step) {
+      const f32x2 v = part[k * rows + r];
+      sum = sum + ExpSum{v[0], v[1]};
+    }
+  }
+  sums[tid] = sum;
+  __syncthreads();
+  for (int half = step / 2; half; half /= 2) {
+    if (first < half) sums[tid] = sums[tid] + sums[tid + half * across];
+    __syncthreads();
+  }
+  if (first || r >= t.n) return;
+  const int i = t.order[r];
+  float lse = 0.f, zt = 0.f;
+  if (lives) {
+    lse = sums[tid].m + logf(sums[tid].s);
+    zt = t.targets[i] < V ? target_logit[r] : NAN;
+  }
+  loss[i] = lse - zt;
+  stats[i] = lse;
+  stats[stats_stride + i] = zt;
 }
 
 // dX [n, ldx] from the dense rows; tokens without a loss get zeros.  One work-group per row of the list.

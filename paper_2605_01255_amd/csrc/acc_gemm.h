@@ -19,6 +19,16 @@
 
 namespace acc {
 
+// What the products with the vocabulary's matrix read and write of a row (acc_ce.h), one piece of `v0` on.
+struct CeRows {
+  const int* targets;   // -1: none
+  const float* lse;
+  const float* g;       // incoming gradient
+  float* target_logit;
+  f32x2* part;          // [strips of the whole vocabulary][rows]: maximum and sum of exponentials
+  int64_t rows, v0;
+};
+
 struct FastGemmParams {
   const bf16* A;
   const bf16* B;
@@ -46,6 +56,9 @@ struct FastGemmParams {
   int tile_blocks;
   int64_t k_per_split;
   int64_t c_split_stride;
+  // The vocabulary's cross entropy (acc_ce.h).  live: device count of the rows of A that take part, the others are behind them.
+  const int* live;
+  CeRows ce;
   int64_t kb_rows;        // N-contiguous B only: rows of B that exist (0 = K); K may exceed it when A is
                           // zero-padded along K, the missing rows of B then read as zero
 };
@@ -171,6 +184,20 @@ __device__ __forceinline__ bool xcd_tile(const FastGemmParams& p, int b, int& tm
   tm = sm * p.super_m + in % p.super_m;
   tn = sn * p.super_n + in / p.super_m;
   return tm < p.tiles_m && tn < p.tiles_n;
+}
+
+// Tile number -> tile: XCD x (work-groups are dealt round-robin) owns a contiguous run of tile numbers, and consecutive
+// numbers walk down super_m tile rows before they move one column on, so that a run is a compact block of the output.
+template <typename P> __device__ __forceinline__ bool ring_tile(const P& p, int b, int& tm, int& tn) {
+  const int total = p.tiles_m * p.tiles_n, per = (total + 7) >> 3;
+  const int id = (b & 7) * per + (b >> 3);
+  if ((b >> 3) >= per || id >= total) return false;
+  const int group = id / (p.super_m * p.tiles_n), in = id - group * p.super_m * p.tiles_n;
+  const int first = group * p.super_m;
+  const int rows = p.tiles_m - first < p.super_m ? p.tiles_m - first : p.super_m;
+  tm = first + in % rows;
+  tn = in / rows;
+  return true;
 }
 
 // The work of one work-group: output tile number b (see xcd_tile), using the dynamic LDS at smem.  K % 64 == 0, bfloat16 C.

@@ -46,6 +46,7 @@
 #include <type_traits>
 
 #include "acc_gemm.h"
+#include "acc_gemm_ce.h"
 
 namespace acc {
 
@@ -75,7 +76,11 @@ __device__ __forceinline__ int swz_n16(int krow) { return ((krow & 3) << 2) | ((
 // RAGGED_K: K % 64 != 0 (K % 8 == 0).  The 16-byte chunks of the last K tile past K are sent out of the buffer's range and
 // read as zero; a lane's chunk is the same in all its wave-loads, so that is one select per K tile and one OR per
 // transfer, which an instantiation of its own keeps out of the slots of the K % 64 == 0 form.
-template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, int N1 = 12, int S1 = 4, int S0 = 4>
+// EPI: what becomes of an output tile.  kExpSums: nothing is stored; its sums of exponentials follow its last K tile, with the next
+// tile's transfers under way (at 64 K tiles 4 % of a tile).  kGradient: the elements change as they are staged, in the slots of the
+// matrix instructions of the block row after.  Either takes its rows from a device count and its tiles from ring_tile's order, which
+// leaves no work-group without a tile for as long as there are some, however many rows there are.
+template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore, int N1 = 12, int S1 = 4, int S0 = 4>
 __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, int n_slots) {
   // schedule of k-step 1: the barrier sits before its slot BAR_Q; N1 wave-loads go out after it, one every S1
   // slots, the other 16 - N1 in the next K tile's k-step 0, one every S0 slots from slot 2
@@ -90,6 +95,17 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   constexpr int BN_CHUNKS = BN / 8;   // of a row of either kind of transposed tile
   constexpr int REGION = 16 * 256;  // one staged block row: 16 rows x 128 bf16
   static_assert(NG == 16, "the slot program places sixteen wave-loads per K tile");
+
+  constexpr bool CE = EPI != Epilogue::kStore;
+  if constexpr (CE) {
+    take_live_rows<EPI>(p, BM);
+    n_slots = ((p.tiles_m * p.tiles_n + 7) >> 3) * 8;
+  }
+  if constexpr (!A_KMAJOR) take_live_tokens(p);
+  auto find_tile = [&](int b, int& tm, int& tn) -> bool {
+    if constexpr (CE) return ring_tile(p, b, tm, tn);
+    else return xcd_tile(p, b, tm, tn);
+  };
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -132,8 +148,8 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     int64_t m0, n0;
   };
   auto tile_ref = [&](int idx) -> TileRef {
-    int tm, tn;
-    xcd_tile(p, idx, tm, tn);
+    int tm = 0, tn = 0;
+    find_tile(idx, tm, tn);
     TileRef r;
     r.m0 = (int64_t)tm * BM;
     r.n0 = (int64_t)tn * BN;
@@ -213,7 +229,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   // slots of the XCD tile map that hold no tile are skipped
   auto next_slot = [&](int idx) -> int {
     int tm, tn;
-    for (idx += (int)gridDim.x; idx < n_slots && !xcd_tile(p, idx, tm, tn);) idx += (int)gridDim.x;
+    for (idx += (int)gridDim.x; idx < n_slots && !find_tile(idx, tm, tn);) idx += (int)gridDim.x;
     return idx;
   };
   const int first_idx = next_slot((int)blockIdx.x - (int)gridDim.x);
@@ -240,16 +256,21 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     const int64_t gm_base = t.m0 + wm * TB * 16, gn_base = t.n0 + wn * TB * 16;
     int64_t c_rows = p.M - gm_base;
     if (c_rows > TB * 16) c_rows = TB * 16;
-    const int64_t c_bytes = (c_rows > 0 && gn_base < p.N) ? ((c_rows - 1) * p.ldc + (p.N - gn_base)) * 2 : 0;
+    const int64_t c_bytes = (c_rows > 0 && gn_base < p.N) ? ((c_rows - 1) * p.ldc + (CE ? (p.N - gn_base + 7) & ~(int64_t)7 : p.N - gn_base)) * 2 : 0;
     c_rs = __builtin_amdgcn_make_buffer_rsrc((void*)(C + gm_base * p.ldc + gn_base), 0, (int)(uint32_t)c_bytes,
                                              0x00020000);
     c_voff = gn_base + l16 * 8 < p.N ? (uint32_t)((g4 * p.ldc + l16 * 8) * 2) : 0xFFFFFFF0u;  // columns past N: dropped
   };
   f32x4 acc[TB][TB];
+  // of this lane's row in each block row, requested before an output tile's last K tile
+  CeRow ce[EPI == Epilogue::kGradient ? TB : 1];
+  int target[TB];
   auto stage_write = [&](int i, int j) {
     bf16x4 v;
+    f32x4 x = acc[i][j];
+    if constexpr (EPI == Epilogue::kGradient) x = ce_gradient(ce[i], x);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = (bf16)acc[i][j][t];
+    for (int t = 0; t < 4; ++t) v[t] = (bf16)x[t];
     typedef bf16x4 __attribute__((address_space(3))) * lds_bf16x4_ptr;
     *(lds_bf16x4_ptr)(uintptr_t)((w_base ^ (uint32_t)(j << 5)) + (i & 1) * REGION) = v;
   };
@@ -304,7 +325,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
       if (q >= 2 && (q - 2) % S0 == 0 && (q - 2) / S0 < NG - N1) issue_at_m0(ref1, N1 + (q - 2) / S0, k1, oob1);
       if (j == 0 && i >= 1) a[i - 1] = read_a(cur, 1, i - 1);
       if (j == 4) b1[i] = read_b(cur, 1, i);
-      if (CARRY && q < 16) carry_slot(q);
+      if (CARRY && EPI != Epilogue::kExpSums && q < 16) carry_slot(q);
       if (q >= 1 && (q - 1) % S0 == 0 && (q - 1) / S0 < NG - N1) set_m0(N1 + (q - 1) / S0, nxt_lds + wave * 1024);
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -316,6 +337,12 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
         wait_vmcnt0();
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (FINAL && EPI == Epilogue::kGradient) {  // the rows' values have landed too: the compiler waits for them here
+          static_for<0, TB>([&](auto r) { landed(ce[decltype(r)::value]); });
+        }
+        if constexpr (FINAL && EPI == Epilogue::kExpSums) {
+          static_for<0, TB>([&](auto r) { landed(target[decltype(r)::value]); });
+        }
       }
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1[j], a[i], acc[i][j], 0, 0, 0);
       pin(acc[i][j]);
@@ -332,7 +359,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
         if (q >= BAR_Q + 1 && (q - BAR_Q - 1) % SP == 0 && (q - BAR_Q - 1) / SP < 8)
           b0[(q - BAR_Q - 1) / SP] = read_b(nxt, 0, (q - BAR_Q - 1) / SP);
       }
-      if constexpr (FINAL) {
+      if constexpr (FINAL && EPI != Epilogue::kExpSums) {
         if (i >= 2 && j == 0) wave_fence();
         if (i >= 1) stage_write(i - 1, j);
         if (i >= 2 && j < 4) back[j] = read_back(i - 2, j);
@@ -342,7 +369,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
         set_m0((q - BAR_Q - 1) / S1, cur_lds + wave * 1024);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (FINAL) {
+    if constexpr (FINAL && EPI != Epilogue::kExpSums) {
       static_for<0, TB>([&](auto col) { stage_write(TB - 1, decltype(col)::value); });
     }
   };
@@ -379,16 +406,23 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
       ktile((kt + par) & 1, cur_t, kt + 1, wraps ? next_t : cur_t, wraps ? 0 : kt + 2, F{}, F{}, F{});
     }
     const int kt = KT - 1;
-    set_output(cur_t);
+    if constexpr (EPI == Epilogue::kExpSums) ce_targets<TB>(p, target, cur_t.m0 + wm * TB * 16, l16);
+    else set_output(cur_t);
+    if constexpr (EPI == Epilogue::kGradient) {
+      static_for<0, TB>([&](auto r) { ce[decltype(r)::value] = ce_row(p, cur_t.m0 + (wm * TB + decltype(r)::value) * 16 + l16); });
+    }
     ktile((kt + par) & 1, next_t, 0, next_t, 1, F{}, F{}, T{});       // last: the read-out starts
+    if constexpr (EPI == Epilogue::kExpSums) ce_sums<TB, TB>(p, acc, target, cur_t.m0 + wm * TB * 16, cur_t.n0 + wn * TB * 16, l16, g4);
     if (!has_next) break;
     cur_t = next_t;
     par = (par + KT) & 1;
     idx = next_idx;
   }
   // no tile follows: block rows 6 and 7 are read out here
+  if constexpr (EPI != Epilogue::kExpSums) {
 #pragma unroll
-  for (int q = 0; q < 16; ++q) carry_slot(q);
+    for (int q = 0; q < 16; ++q) carry_slot(q);
+  }
   wait_vmcnt0();  // the surplus transfers of the last two K tiles must have landed before the LDS is released
 }
 

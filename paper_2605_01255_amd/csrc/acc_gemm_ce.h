@@ -1,0 +1,116 @@
+// What the products with the vocabulary's matrix do with their output tiles (acc_ce.h has the rest of the cross entropy): the
+// logits stay in the accumulators and become sums of exponentials (forward) or the logits' gradient (backward).
+// A wave's tile is TM x TN blocks of 16 x 16: lane l16 + 16 g4 holds row l16 of each block and its columns 4 g4 .. + 3.
+#pragma once
+#include "acc_gemm.h"
+
+namespace acc {
+
+enum class Epilogue { kStore, kExpSums, kGradient };
+
+constexpr float kLog2e = 1.44269504088896341f;
+// Rows of the logits' gradient that are written, whatever the count: what the product over the tokens takes at least, three K tiles of
+// it; rows behind the count are zero.  The dense matrices have 256 rows or more.
+constexpr int kCeLeastRows = 192;
+
+template <Epilogue EPI> __device__ __forceinline__ void take_live_rows(FastGemmParams& p, int bm) {
+  int rows = *p.live;
+  if (EPI == Epilogue::kGradient && rows < kCeLeastRows) rows = kCeLeastRows;
+  p.M = rows;
+  p.tiles_m = (rows + bm - 1) / bm;
+}
+__device__ __forceinline__ void take_live_tokens(FastGemmParams& p) {
+  if (!p.live) return;
+  const int rows = *p.live;
+  p.K = rows < kCeLeastRows ? kCeLeastRows : rows;
+}
+
+// Targets of this lane's row of each block row from m0 on.
+template <int TM> __device__ __forceinline__ void ce_targets(const FastGemmParams& p, int (&target)[TM], int64_t m0, int l16) {
+  static_for<0, TM>([&](auto row) {
+    int64_t gm = m0 + decltype(row)::value * 16 + l16;
+    if (gm >= p.ce.rows) gm = p.ce.rows - 1;
+    target[decltype(row)::value] = p.ce.targets[gm];
+  });
+}
+
+// The value is one that the compiler has in an accumulator register here, and copies it from here on: without it the copies of all 256
+// are made in front of ce_sums' branches, and others are pushed out into scratch memory.
+__device__ __forceinline__ void in_accumulators(f32x4& v) { asm volatile("" : "+a"(v)); }
+
+// The wave's sums: per row the maximum over the strip of TN * 16 columns and the sum of exponentials above it, and the logit of a
+// target in it.  Exponentials as powers of two: the product with log2 e and the difference are one operation.
+template <int TM, int TN>
+__device__ __forceinline__ void ce_sums(const FastGemmParams& p, f32x4 (&acc)[TM][TN], const int (&target)[TM], int64_t m0, int64_t n0, int l16, int g4) {
+  constexpr int STRIP = TN * 16;
+  if (n0 >= p.N) return;
+  const int64_t strip = (p.ce.v0 + n0) / STRIP;   // pieces are whole numbers of strips
+  const int left = (int)(p.N - n0 < STRIP ? p.N - n0 : STRIP) - 4 * g4;   // columns of this lane's that exist have j * 16 + e below this
+  auto block_row = [&](auto row, auto edge) {
+    constexpr int i = decltype(row)::value;
+    constexpr bool EDGE = decltype(edge)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t gm = m0 + i * 16 + l16;
+    const bool exists = gm < p.M;
+    f32x4 x[TN];
+    float m = -INFINITY;
+    static_for<0, TN>([&](auto col) {
+      constexpr int j = decltype(col)::value;
+      in_accumulators(acc[i][j]);
+      x[j] = acc[i][j];
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[j][e] = j * 16 + e < left ? x[j][e] : -INFINITY;
+      }
+      m = fmaxf(m, fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])));
+    });
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    if (isinf(m)) m = 0.f;   // exponentials of what is infinite are 0 or infinite, never NaN
+    const float m2 = m * kLog2e;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    // few waves hold a target's column
+    const int64_t rel = exists ? target[i] - (p.ce.v0 + n0) : -1;
+    if (__any(rel >= 0 && rel < STRIP)) {
+      const int at = rel >= 0 && rel < STRIP ? (int)rel - 4 * g4 : -1;
+      static_for<0, TN>([&](auto col) {
+        constexpr int j = decltype(col)::value;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at == j * 16 + e) p.ce.target_logit[gm] = x[j][e];
+      });
+    }
+    static_for<0, TN>([&](auto col) {
+      constexpr int j = decltype(col)::value;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], kLog2e, -m2));
+    });
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (exists && g4 == 0) p.ce.part[strip * p.ce.rows + gm] = f32x2{m, sum};
+  };
+  if (n0 + STRIP > p.N) static_for<0, TM>([&](auto row) { block_row(row, std::true_type{}); });
+  else static_for<0, TM>([&](auto row) { block_row(row, std::false_type{}); });
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// A row's log-sum-exp times log2 e and its incoming gradient.  A probability times it is the logit's gradient; the target's own element
+// is put right afterwards (ce_target_kernel), where 1 can be taken from its probability without cancellation.
+struct CeRow {
+  float lse2, g;
+};
+__device__ __forceinline__ CeRow ce_row(const FastGemmParams& p, int64_t row) {
+  if (row >= p.ce.rows) row = p.ce.rows - 1;
+  return CeRow{p.ce.lse[row] * kLog2e, p.ce.g[row]};
+}
+// The compiler has to have a requested value here.
+__device__ __forceinline__ void landed(CeRow& r) { asm volatile("" : "+v"(r.lse2), "+v"(r.g)); }
+__device__ __forceinline__ void landed(int& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ f32x4 ce_gradient(const CeRow& r, f32x4 x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = r.g * __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], kLog2e, -r.lse2));
+  return x;
+}
+
+}  // namespace acc

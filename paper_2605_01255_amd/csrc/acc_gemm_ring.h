@@ -32,20 +32,6 @@ template <int BN> __device__ __forceinline__ int swz_ring(int krow) {
   else return swz_n16(krow);
 }
 
-// Tile number -> tile: XCD x (work-groups are dealt round-robin) owns a contiguous run of tile numbers, and consecutive
-// numbers walk down super_m tile rows before they move one column on, so that a run is a compact block of the output.
-template <typename P> __device__ __forceinline__ bool ring_tile(const P& p, int b, int& tm, int& tn) {
-  const int total = p.tiles_m * p.tiles_n, per = (total + 7) >> 3;
-  const int id = (b & 7) * per + (b >> 3);
-  if ((b >> 3) >= per || id >= total) return false;
-  const int group = id / (p.super_m * p.tiles_n), in = id - group * p.super_m * p.tiles_n;
-  const int first = group * p.super_m;
-  const int rows = p.tiles_m - first < p.super_m ? p.tiles_m - first : p.super_m;
-  tm = first + in % rows;
-  tn = in / rows;
-  return true;
-}
-
 template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // SPLIT: the K range is split over groups of tile_blocks work-groups (skinny products of the RSVD path), each storing its
@@ -54,7 +40,8 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_
 // result is (error of a [16384, 3072] x [3072, 64] product: 6.3e-7 with one sum per split of 1536, 6.0e-7 so, 6.1e-7 with
 // the four splits of 768 that the two-stage kernel took; the time is the same).
 // SUM: C = beta C + alpha (A . B).  A form of its own: behind a branch its registers cost the plain one occupancy.
-template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, bool SPLIT = false, bool SUM = false, bool A_KMAJOR = true>
+template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, bool SPLIT = false, bool SUM = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore,
+          bool LIVE = false>
 __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int NW = 4, WN = 2;
@@ -66,6 +53,8 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   static_assert(A_KMAJOR || BM == 64 || BM == 128 || BM == 192 || BM == 256, "M-contiguous swizzle");
   static_assert((NS - 1) * NG <= 63, "vmcnt range");
 
+  if constexpr (LIVE) take_live_rows<EPI>(p, BM);
+  if constexpr (!A_KMAJOR) take_live_tokens(p);
   int tm, tn;
   const int split = SPLIT ? (int)blockIdx.x / p.tile_blocks : 0;
   const bool has_tile = ring_tile(p, (int)blockIdx.x - split * (SPLIT ? p.tile_blocks : 0), tm, tn);
@@ -258,6 +247,22 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
       for (int j = 0; j < TN; ++j) acc[i][j] += total[i][j];
   }
 
+  if constexpr (EPI == Epilogue::kExpSums) {
+    int target[TM];
+    ce_targets<TM>(p, target, m0 + wm * TM * 16, l16);
+    ce_sums<TM, TN>(p, acc, target, m0 + wm * TM * 16, n0 + wn * TN * 16, l16, g4);
+    return;
+  }
+  if constexpr (EPI == Epilogue::kGradient) {
+    static_for<0, TM>([&](auto row) {
+      constexpr int i = decltype(row)::value;
+      const CeRow r = ce_row(p, m0 + (wm * TM + i) * 16 + l16);
+      static_for<0, TN>([&](auto col) {
+        constexpr int j = decltype(col)::value;
+        acc[i][j] = ce_gradient(r, acc[i][j]);
+      });
+    });
+  }
   // ---- epilogue: lane holds output row l16 of each 16 x 16 block and columns 4 g4 .. + 3; a wave stages one block
   //      row (16 x TN * 16) in a private padded LDS region and moves 16 bytes per lane (whole rows); a product that is added
   //      to C is staged as float, so that only the sum is rounded ----

@@ -151,10 +151,4 @@ void exact_backward_gemm(const acc_linear_desc* desc, const Shape& s, const void
 // written up to a multiple of four, A's zeros behind K among them (any N and K then).
 void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtype, int64_t ldc, int64_t M, int64_t N, int64_t K,
                  bool accumulate, Launcher& L, bool padded = false);
-// The same for bfloat16 operands and a float C[M, N] (+)= A[M, K] . B, A zero-padded to a multiple of eight along K, rows of C
-// written up to a multiple of four; B is [N, K], or [K, N] where accumulate's form is asked for.
-void bf16_logits(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, Launcher& L);
-void bf16_input_gradient(const void* A, int64_t lda, const void* B, int64_t ldb, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                         bool accumulate, Launcher& L);
-
 }  // namespace acc

@@ -53,8 +53,10 @@ void ring_token_gemm(FastGemmParams& p, Launcher& L) {
 }
 
 template <typename TC, bool SUM>
-void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, Launcher& L) {
+void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, Launcher& L,
+                const int* live) {
   FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, nullptr, 1.f, 1.f);
+  p.live = live;
   const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
   const GemmChoice c = pick_gemm_tile(M, N, K, persist_ok);
   switch (c.tile) {
@@ -79,14 +81,15 @@ void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int
   }
 }
 
-// C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.
+// C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.  live (bfloat16):
+// device count of the rows of both that take part, at most K; kCeLeastRows of them are read at least.
 void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t M,
-                   int64_t N, int64_t K, bool accumulate, Launcher& L) {
+                   int64_t N, int64_t K, bool accumulate, Launcher& L, const int* live = nullptr) {
   if (io == ACC_BF16) {
     auto typed = [&](auto type) {
       using TC = decltype(type);
-      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L);
-      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L);
+      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L, live);
+      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L, live);
     };
     if (dtype == ACC_BF16) typed(bf16{});
     else typed(float{});
@@ -117,12 +120,22 @@ int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
 // ---- the vocabulary's cross entropy --------------------------------------------------------------------
 constexpr int64_t kCePieceBytes = (int64_t)512 << 20;
 
+// Tile of the products that form the logits: 64 x 128 for few tokens, where W is read once whatever the tile, 128 x 128 up to a full
+// 256 x 256 tile's rows, then 256 x 256.  Its waves' strips of columns are 64 or 128 wide.
+enum class CeTile { k64x128, k128, k256 };
+CeTile ce_tile(int64_t n, int64_t d) {
+  if (n <= 64) return CeTile::k64x128;
+  return n <= 128 || d <= 128 ? CeTile::k128 : CeTile::k256;   // the persistent kernel takes three K tiles at least
+}
+int64_t ce_strip(int64_t n, int64_t d) { return ce_tile(n, d) == CeTile::k256 ? 128 : 64; }
+
 struct CePlan {
   int64_t n, d, v, ldx, ldw;
   int64_t run;      // tokens of a run
   int64_t rows;     // of the dense matrices: a run, and 256 at least
   int64_t vp, ldz;  // columns of a piece, their row stride
-  size_t order, count, x, z, dz, per_row, dx;   // offsets into the workspace
+  int64_t strips;   // of the whole vocabulary
+  size_t order, count, per_row, x, part, z, dx;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
 
@@ -151,6 +164,7 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (vp > p->v) vp = p->v;
   p->vp = vp;
   p->ldz = round_up(vp, 8);
+  p->strips = ceil_div(p->v, ce_strip(p->run, p->d));
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t from = at;
@@ -159,13 +173,21 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   };
   p->order = take(p->run * 4);
   p->count = take(4);
-  p->per_row = take(3 * p->rows * 4);
+  p->per_row = take(4 * p->rows * 4);
   p->x = take(p->rows * p->d * es);
-  p->z = take(p->rows * p->ldz * 4);
+  // forward: bfloat16 logits never leave the accumulators, float ones do
+  const size_t shared = at;
+  p->part = take(p->strips * p->rows * 8);
+  p->z = shared;
+  if (d->io_dtype == ACC_F32) {
+    at = shared;
+    p->z = take(p->rows * p->ldz * 4);
+  }
   p->forward = at;
-  p->dz = d->io_dtype == ACC_F32 ? p->z : take(p->rows * p->ldz * 2);
+  at = shared;   // backward: dz, then dX in float
+  take(p->rows * p->ldz * es);
   p->dx = take(p->rows * p->d * 4);
-  p->backward = at;
+  p->backward = at > p->forward ? at : p->forward;
   return ACC_OK;
 }
 
@@ -194,24 +216,61 @@ template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, cons
 }
 
 void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
-  const dim3 grid((unsigned)r.p.rows);
-  float* per_row = stats ? (float*)(r.ws + r.p.per_row) : nullptr;
   auto typed = [&](auto value) {
     using T = decltype(value);
-    L(ce_gather_kernel<T>, grid, dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows, (T*)(r.ws + r.p.x),
-      stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, per_row);
+    L(ce_gather_kernel<T>, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows,
+      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, (float*)(r.ws + r.p.per_row));
   };
   if (r.desc->io_dtype == ACC_BF16) typed(bf16{});
   else typed(float{});
 }
 
-// Z [rows, piece] = X . W_piece^T, float.
-void ce_logits(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
-  const void* w = r.w_piece(W, v0);
-  float* z = (float*)(r.ws + r.p.z);
-  const int64_t vp = r.piece(v0);
-  if (r.desc->io_dtype == ACC_BF16) bf16_logits(r.ws + r.p.x, r.p.d, w, r.p.ldw, z, r.p.ldz, r.n, vp, r.p.d, L);
-  else f32_product(F32Operand{r.ws + r.p.x, r.p.d, true, false}, F32Operand{w, r.p.ldw, true, false}, z, ACC_F32, r.p.ldz, r.n, vp, r.p.d, false, L, true);
+// Z [rows, piece] = X . W_piece^T in float32.
+void ce_logits_f32(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
+  f32_product(F32Operand{r.ws + r.p.x, r.p.d, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, true, false}, r.ws + r.p.z, ACC_F32, r.p.ldz, r.n,
+              r.piece(v0), r.p.d, false, L, true);
+}
+
+// X . W^T over columns v0 .. v0 + vp - 1, bfloat16, into sums of exponentials or the logits' gradient [rows, ldz].
+template <Epilogue EPI> void ce_product(const CeRun& r, const void* W, int64_t v0, int64_t vp, Launcher& L) {
+  FastGemmParams p = fast_params(r.ws + r.p.x, r.w_piece(W, v0), r.ws + r.p.z, r.n, vp, r.p.d, r.p.d, r.p.ldw, r.p.ldz, nullptr, 1.f, 0.f);
+  float* per_row = (float*)(r.ws + r.p.per_row);
+  p.live = r.tokens.count;
+  p.ce = CeRows{(const int*)per_row, per_row + r.p.rows, per_row + 3 * r.p.rows, per_row + 2 * r.p.rows, (f32x2*)(r.ws + r.p.part), r.p.rows, v0};
+  if (EPI == Epilogue::kGradient && p.M < kCeLeastRows) p.M = kCeLeastRows;   // for the grid
+  auto ring = [&](auto tm, auto tn) {
+    constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = 3;
+    const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, true, bf16, false, false, true, EPI, true>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+  };
+  using std::integral_constant;
+  switch (ce_tile(r.p.run, r.p.d)) {
+    case CeTile::k64x128: return ring(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+    case CeTile::k128: return ring(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    case CeTile::k256: break;
+  }
+  gemm_ring_plan(p, 256, 256);
+  if (p.super_m > 8) p.super_m = 8;
+  if (p.K % 64) L.launch_lds(gemm16_persist_kernel<true, true, true, EPI>, dim3(256), dim3(256), (size_t)160 * 1024, p, 0);
+  else L.launch_lds(gemm16_persist_kernel<true, false, true, EPI>, dim3(256), dim3(256), (size_t)160 * 1024, p, 0);
+}
+
+// dX (float) (+)= dz . W_piece for the rows with a token.
+template <bool SUM> void ce_input_gradient(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
+  FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), r.ws + r.p.dx, r.n, r.p.d, round_up(r.piece(v0), 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 1.f);
+  p.kb_rows = r.piece(v0);
+  p.live = r.tokens.count;
+  auto ring = [&](auto tm, auto tn, auto ns) {
+    constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
+    const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, false, SUM, true, Epilogue::kStore, true>, dim3(grid), dim3(256),
+                 (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+  };
+  using std::integral_constant;
+  const GemmChoice c = pick_gemm_tile(r.n, r.p.d, p.K, false);
+  if (c.tile == GemmTile::k256 || c.tile == GemmTile::k256x192 || c.tile == GemmTile::k192x128) ring(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  else if (c.tile == GemmTile::k128) ring(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  else ring(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
 }
 
 }  // namespace
@@ -354,12 +413,21 @@ int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, con
   if ((rc = check_device()) != ACC_OK) return rc;
   return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
     ce_gather(r, X, nullptr, nullptr, L);
-    float* run = (float*)(r.ws + r.p.per_row);
+    float* per_row = (float*)(r.ws + r.p.per_row);
+    if (desc->io_dtype == ACC_BF16) {
+      ce_product<Epilogue::kExpSums>(r, W, 0, r.p.v, L);
+      int across = 32;   // rows of a work-group
+      while (across > 1 && across / 2 >= r.n) across /= 2;
+      const int strips = (int)r.p.strips;
+      L(ce_finish_kernel, dim3((unsigned)ceil_div(r.n, across)), dim3(256), r.tokens, (const f32x2*)(r.ws + r.p.part), strips, r.p.rows, across, r.p.v,
+        (const float*)(per_row + 2 * r.p.rows), loss + r.t0, stats + r.t0, r.p.n);
+      return;
+    }
     for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
       const int64_t vp = r.piece(v0);
-      ce_logits(r, W, v0, L);
+      ce_logits_f32(r, W, v0, L);
       L(ce_piece_stats_kernel, dim3((unsigned)r.n), dim3(256), r.tokens, (const float*)(r.ws + r.p.z), r.p.ldz, v0, (int)vp, v0 == 0, v0 + vp == r.p.v,
-        r.p.v, run, run + r.p.rows, run + 2 * r.p.rows, loss + r.t0, stats + r.t0, r.p.n);
+        r.p.v, per_row + r.p.rows, per_row + 2 * r.p.rows, per_row + 3 * r.p.rows, loss + r.t0, stats + r.t0, r.p.n);
     }
   });
 }
@@ -378,25 +446,29 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
   const bool b16 = desc->io_dtype == ACC_BF16;
   return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
     ce_gather(r, X, stats, dloss, L);
-    const float* per_row = (const float*)(r.ws + r.p.per_row);
-    float* z = (float*)(r.ws + r.p.z);
+    float* per_row = (float*)(r.ws + r.p.per_row);
     float* dxf = (float*)(r.ws + r.p.dx);
-    char* dz = r.ws + r.p.dz;
+    char* dz = r.ws + r.p.z;
     for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
       const int64_t vp = r.piece(v0);
-      ce_logits(r, W, v0, L);
-      const dim3 grid((unsigned)r.p.rows);
-      if (b16) L(ce_piece_grad_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)z, r.p.ldz, v0, (int)vp, r.p.v, r.p.rows, per_row, (bf16*)dz);
-      else L(ce_piece_grad_kernel<float>, grid, dim3(256), r.tokens, (const float*)z, r.p.ldz, v0, (int)vp, r.p.v, r.p.rows, per_row, (float*)dz);
+      if (b16) {
+        ce_product<Epilogue::kGradient>(r, W, v0, vp, L);
+        L(ce_target_kernel, dim3((unsigned)ceil_div(r.p.rows, 256)), dim3(256), (const int*)r.tokens.count, r.p.ldz, v0, (int)vp, r.p.rows,
+          (const float*)per_row, (bf16*)dz);
+      } else {
+        ce_logits_f32(r, W, v0, L);
+        L(ce_piece_grad_kernel, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (float*)dz, r.p.ldz, v0, (int)vp, r.p.rows, (const float*)per_row);
+      }
       if (dX) {
-        const void* w = r.w_piece(W, v0);
-        if (b16) bf16_input_gradient(dz, r.p.ldz, w, r.p.ldw, dxf, r.p.d, r.n, r.p.d, vp, v0 > 0, L);
-        else f32_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{w, r.p.ldw, false, false}, dxf, ACC_F32, r.p.d, r.n, r.p.d, vp, v0 > 0, L, true);
+        if (!b16) f32_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, ACC_F32, r.p.d, r.n, r.p.d, vp, v0 > 0, L, true);
+        else if (v0) ce_input_gradient<true>(r, W, v0, L);
+        else ce_input_gradient<false>(r, W, v0, L);
       }
       if (dW) {
         char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
         const bool add = r.t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
-        token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, r.n, add, L);
+        token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 ? r.p.rows : r.n, add, L,
+                      b16 ? r.tokens.count : nullptr);
       }
     }
     if (dX) {
