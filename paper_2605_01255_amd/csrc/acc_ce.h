@@ -6,95 +6,68 @@
 // the tokens with a loss cost, and infinities or NaN in a padded token's row reach no sum (0 times NaN is NaN).
 #pragma once
 #include "acc_common.h"
+#include "acc_gemm_ce.h"
 
 namespace acc {
 
-// What a call knows of its tokens after the selection.  `order` lists the tokens with a loss in their order, then the others.
+// What a call knows of its tokens.  `order` lists the tokens with a loss in their order, then the others; null: all tokens as they
+// come.
 struct CeTokens {
   const int64_t* targets;   // [n]
   int n;
   int* order;               // [n]
   int* count;               // tokens with a loss
+  __device__ __forceinline__ int token(int64_t r) const { return order ? order[r] : (int)r; }
+  __device__ __forceinline__ bool lives(int64_t r) const { return order ? r < *count : r < n && targets[r] >= 0; }
 };
 
-// One work-group of 1024 threads, eight tokens of a thread at a time.
+// One work-group of 1024 threads, eight tokens of a thread at a time; the others fill the list from its end.
 __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t) {
   constexpr int PER = 8;
-  __shared__ int wave_kept[16];
+  __shared__ int wave_kept[2][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int kept = 0;   // so far
-  for (int first = 0; first < t.n; first += 1024 * PER) {
+  int kept = 0, turn = 0;   // kept: so far
+  for (int first = 0; first < t.n; first += 1024 * PER, turn ^= 1) {
     const int i0 = first + tid * PER;
     bool keep[PER];
     int mine = 0;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      keep[k] = i0 + k < t.n && t.targets[i0 + k] >= 0;
-      mine += keep[k] ? 1 : 0;
-    }
+    for (int k = 0; k < PER; ++k) keep[k] = t.targets[i0 + k < t.n ? i0 + k : t.n - 1] >= 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) mine += keep[k] && i0 + k < t.n ? 1 : 0;
     int before = mine;   // inclusive scan over the wave
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int o = __shfl_up(before, d);
       before += lane >= d ? o : 0;
     }
-    if (lane == 63) wave_kept[wave] = before;
+    if (lane == 63) wave_kept[turn][wave] = before;
     __syncthreads();
     int total = 0, waves_before = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) {
-      waves_before += w < wave ? wave_kept[w] : 0;
-      total += wave_kept[w];
+      waves_before += w < wave ? wave_kept[turn][w] : 0;
+      total += wave_kept[turn][w];
     }
-    __syncthreads();
-    int at = kept + waves_before + before - mine;
+    int at = kept + waves_before + before - mine;   // tokens with a loss before this thread's
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
+    for (int k = 0; k < PER; ++k) {
+      if (i0 + k >= t.n) break;
       if (keep[k]) t.order[at++] = i0 + k;
+      else t.order[t.n - 1 - (i0 + k - at)] = i0 + k;
+    }
     kept += total;
   }
   if (tid == 0) *t.count = kept;
-  // the others from the end of the list: token i without a loss is the (i - kept ones before it)-th of them
-  int others = 0;
-  for (int first = 0; first < t.n; first += 1024 * PER) {
-    const int i0 = first + tid * PER;
-    bool keep[PER];
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      keep[k] = i0 + k < t.n && t.targets[i0 + k] < 0;
-      mine += keep[k] ? 1 : 0;
-    }
-    int before = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(before, d);
-      before += lane >= d ? o : 0;
-    }
-    if (lane == 63) wave_kept[wave] = before;
-    __syncthreads();
-    int total = 0, waves_before = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      waves_before += w < wave ? wave_kept[w] : 0;
-      total += wave_kept[w];
-    }
-    __syncthreads();
-    int at = kept + others + waves_before + before - mine;
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-      if (keep[k]) t.order[at++] = i0 + k;
-    others += total;
-  }
 }
 
 // What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero, up to
-// 256 of them for the products' least rows.  per_row: target (as int; -1: no gradient), and in a backward call lse, the target's
+// 256 of them for the products' least rows.  targets: -1 where there is no gradient.  per_row, in a backward call: lse, the target's
 // logit and the incoming gradient, `rows` of each.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc, int64_t V,
                                                         const float* __restrict__ stats, const float* __restrict__ dloss, int64_t stats_stride,
-                                                        float* __restrict__ per_row) {
+                                                        int64_t* __restrict__ targets, float* __restrict__ per_row) {
   constexpr int VEC = 16 / sizeof(T);
   typedef T vecT __attribute__((ext_vector_type(VEC)));
   const int64_t r = blockIdx.x;
@@ -103,11 +76,11 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
   const int i = lives ? t.order[r] : 0;
   if (threadIdx.x == 0) {
     const int64_t target = lives ? t.targets[i] : -1;
-    ((int*)per_row)[r] = target < V ? (int)target : -1;
+    targets[r] = target < V ? target : -1;
     if (stats) {
-      per_row[rows + r] = lives ? stats[i] : 0.f;
-      per_row[2 * rows + r] = lives ? stats[stats_stride + i] : 0.f;
-      per_row[3 * rows + r] = lives && target < V ? dloss[i] : 0.f;
+      per_row[r] = lives ? stats[i] : 0.f;
+      per_row[rows + r] = lives && target < V ? stats[stats_stride + i] : 0.f;
+      per_row[2 * rows + r] = lives && target < V ? dloss[i] : 0.f;
     }
   }
   if (sizeof(T) == 2 && !lives && r >= 256) return;   // the float32 products read every row
@@ -190,10 +163,9 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const f
 // dz of one piece from its logits, in place, one work-group per row; rows without a token and columns from vp to ldz are zero.  A
 // target beyond the vocabulary has no gradient.
 __global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, float* __restrict__ Z, int64_t ldz, int64_t v0, int vp, int64_t rows,
-                                                            const float* __restrict__ per_row) {
-  const int64_t r = blockIdx.x;
-  const int target = ((const int*)per_row)[r];   // -1 where there is no token or no gradient
-  const float lse = per_row[rows + r], zt = per_row[2 * rows + r], g = per_row[3 * rows + r];
+                                                            const int64_t* __restrict__ targets, const float* __restrict__ per_row) {
+  const int64_t r = blockIdx.x, target = targets[r];   // -1 where there is no token or no gradient
+  const float lse = per_row[r], zt = per_row[rows + r], g = per_row[2 * rows + r];
   for (int64_t c = threadIdx.x; c < ldz; c += 256) {
     float dz = 0.f;
     if (target >= 0 && c < vp) dz = v0 + c == target ? g * expm1f(zt - lse) : g * expf(Z[r * ldz + c] - lse);
@@ -201,32 +173,34 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, float* _
   }
 }
 
-// What the product that forms dz leaves to do: the targets' elements, g (exp(z - lse) - 1), and zeros from column vp to ldz (rows end
-// with whole 16 bytes).  One thread per row.
-__global__ __launch_bounds__(256) void ce_target_kernel(const int* __restrict__ live, int64_t ldz, int64_t v0, int vp, int64_t rows,
-                                                        const float* __restrict__ per_row, bf16* __restrict__ dZ) {
-  const int r = (int)(blockIdx.x * 256 + threadIdx.x);
-  const int count = *live;
-  if (r >= rows || r >= (count < 256 ? 256 : count)) return;
-  for (int64_t c = vp; c < ldz; ++c) dZ[r * ldz + c] = (bf16)0.f;
-  const int64_t at = ((const int*)per_row)[r] - v0;
-  if (at >= 0 && at < vp) dZ[r * ldz + at] = (bf16)(per_row[3 * rows + r] * expm1f(per_row[2 * rows + r] - per_row[rows + r]));
-}
-
-// Losses and statistics from the strips' sums.  A work-group takes `across` rows (a power of two up to 32); the threads of a row
-// share its strips.
+// Losses and statistics from the strips' sums.  A work-group takes `across` rows (a power of two); the threads of a row share its
+// strips, eight requested at a time.
 __global__ __launch_bounds__(256) void ce_finish_kernel(CeTokens t, const f32x2* __restrict__ part, int strips, int64_t rows, int across, int64_t V,
                                                         const float* __restrict__ target_logit, float* __restrict__ loss,
                                                         float* __restrict__ stats, int64_t stats_stride) {
   __shared__ ExpSum sums[256];
   const int tid = threadIdx.x, mine = tid & (across - 1), first = tid / across, step = 256 / across;
   const int r = (int)blockIdx.x * across + mine;
-  const bool lives = r < *t.count;
+  const bool exists = r < t.n, lives = exists && t.lives(r);
   ExpSum sum{0.f, 0.f};
   if (lives) {
-    for (int k = first; k < strips; k += step) {
-      const f32x2 v = part[k * rows + r];
-      sum = sum + ExpSum{v[0], v[1]};
+    constexpr int AT_ONCE = 8;
+    for (int k = first; k < strips; k += AT_ONCE * step) {
+      f32x2 v[AT_ONCE];
+      static_for<0, AT_ONCE>([&](auto u) {
+        constexpr int U = decltype(u)::value;
+        v[U] = f32x2{0.f, 0.f};
+        if (k + U * step < strips) v[U] = part[(int64_t)(k + U * step) * rows + r];
+      });
+      float m = sum.s == 0.f ? -INFINITY : sum.m;   // an empty sum's maximum does not count; NaN is not 0
+      static_for<0, AT_ONCE>([&](auto u) { m = v[decltype(u)::value][1] == 0.f ? m : fmaxf(m, v[decltype(u)::value][0]); });
+      if (isinf(m)) continue;                       // all of them are empty
+      float s = sum.s == 0.f ? 0.f : sum.s * __builtin_amdgcn_exp2f((sum.m - m) * kLog2e);
+      static_for<0, AT_ONCE>([&](auto u) {
+        const f32x2 x = v[decltype(u)::value];
+        s += x[1] == 0.f ? 0.f : x[1] * __builtin_amdgcn_exp2f((x[0] - m) * kLog2e);
+      });
+      sum = ExpSum{m, s};
     }
   }
   sums[tid] = sum;
@@ -235,8 +209,8 @@ __global__ __launch_bounds__(256) void ce_finish_kernel(CeTokens t, const f32x2*
     if (first < half) sums[tid] = sums[tid] + sums[tid + half * across];
     __syncthreads();
   }
-  if (first || r >= t.n) return;
-  const int i = t.order[r];
+  if (first || !exists) return;
+  const int i = t.token(r);
   float lse = 0.f, zt = 0.f;
   if (lives) {
     lse = sums[tid].m + logf(sums[tid].s);

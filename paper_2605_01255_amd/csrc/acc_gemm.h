@@ -21,10 +21,10 @@ namespace acc {
 
 // What the products with the vocabulary's matrix read and write of a row (acc_ce.h), one piece of `v0` on.
 struct CeRows {
-  const int* targets;   // -1: none
+  const int64_t* targets;
+  float* target_logit;  // written by the forward product, read by the backward one
   const float* lse;
   const float* g;       // incoming gradient
-  float* target_logit;
   f32x2* part;          // [strips of the whole vocabulary][rows]: maximum and sum of exponentials
   int64_t rows, v0;
 };

@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   auto stage_write = [&](int i, int j) {
     bf16x4 v;
     f32x4 x = acc[i][j];
-    if constexpr (EPI == Epilogue::kGradient) x = ce_gradient(ce[i], x);
+    if constexpr (EPI == Epilogue::kGradient) x = ce_gradient(ce[i], x, j);
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[t] = (bf16)x[t];
     typedef bf16x4 __attribute__((address_space(3))) * lds_bf16x4_ptr;
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     if constexpr (EPI == Epilogue::kExpSums) ce_targets<TB>(p, target, cur_t.m0 + wm * TB * 16, l16);
     else set_output(cur_t);
     if constexpr (EPI == Epilogue::kGradient) {
-      static_for<0, TB>([&](auto r) { ce[decltype(r)::value] = ce_row(p, cur_t.m0 + (wm * TB + decltype(r)::value) * 16 + l16); });
+      static_for<0, TB>([&](auto r) { ce[decltype(r)::value] = ce_row(p, cur_t.m0 + (wm * TB + decltype(r)::value) * 16 + l16, cur_t.n0 + wn * TB * 16, g4); });
     }
     ktile((kt + par) & 1, next_t, 0, next_t, 1, F{}, F{}, T{});       // last: the read-out starts
     if constexpr (EPI == Epilogue::kExpSums) ce_sums<TB, TB>(p, acc, target, cur_t.m0 + wm * TB * 16, cur_t.n0 + wn * TB * 16, l16, g4);

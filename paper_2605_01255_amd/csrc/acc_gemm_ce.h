@@ -14,6 +14,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCeLeastRows = 192;
 
 template <Epilogue EPI> __device__ __forceinline__ void take_live_rows(FastGemmParams& p, int bm) {
+  if (!p.live) return;   // all of them
   int rows = *p.live;
   if (EPI == Epilogue::kGradient && rows < kCeLeastRows) rows = kCeLeastRows;
   p.M = rows;
@@ -25,13 +26,14 @@ __device__ __forceinline__ void take_live_tokens(FastGemmParams& p) {
   p.K = rows < kCeLeastRows ? kCeLeastRows : rows;
 }
 
+__device__ __forceinline__ int64_t ce_clamped(const FastGemmParams& p, int64_t row) { return row < p.ce.rows ? row : p.ce.rows - 1; }
+__device__ __forceinline__ int ce_target(const FastGemmParams& p, int64_t row) {   // -1: none
+  const int64_t t = p.ce.targets[ce_clamped(p, row)];
+  return t < 0 || t > (1 << 30) ? -1 : (int)t;
+}
 // Targets of this lane's row of each block row from m0 on.
 template <int TM> __device__ __forceinline__ void ce_targets(const FastGemmParams& p, int (&target)[TM], int64_t m0, int l16) {
-  static_for<0, TM>([&](auto row) {
-    int64_t gm = m0 + decltype(row)::value * 16 + l16;
-    if (gm >= p.ce.rows) gm = p.ce.rows - 1;
-    target[decltype(row)::value] = p.ce.targets[gm];
-  });
+  static_for<0, TM>([&](auto row) { target[decltype(row)::value] = ce_target(p, m0 + decltype(row)::value * 16 + l16); });
 }
 
 // The value is one that the compiler has in an accumulator register here, and copies it from here on: without it the copies of all 256
@@ -95,21 +97,30 @@ __device__ __forceinline__ void ce_sums(const FastGemmParams& p, f32x4 (&acc)[TM
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A row's log-sum-exp times log2 e and its incoming gradient.  A probability times it is the logit's gradient; the target's own element
-// is put right afterwards (ce_target_kernel), where 1 can be taken from its probability without cancellation.
+// Of one row: log-sum-exp times log2 e, the incoming gradient g, the target's column counted from this lane's first one, and the
+// target's own gradient g (exp(z - lse) - 1), where 1 is taken from the probability without cancellation.
+// A row whose log-sum-exp is not finite gets NaN, as g.  That lets the exponent be cut off far above any probability's, which keeps
+// the columns behind the vocabulary's end, where the logits are 0, finite: the product with W takes rows of zeros for them.
 struct CeRow {
-  float lse2, g;
+  float lse2, g, own;
+  int at;
 };
-__device__ __forceinline__ CeRow ce_row(const FastGemmParams& p, int64_t row) {
-  if (row >= p.ce.rows) row = p.ce.rows - 1;
-  return CeRow{p.ce.lse[row] * kLog2e, p.ce.g[row]};
+__device__ __forceinline__ CeRow ce_row(const FastGemmParams& p, int64_t row, int64_t n0, int g4) {
+  row = ce_clamped(p, row);
+  const float lse = p.ce.lse[row], g = isfinite(lse) ? p.ce.g[row] : NAN;
+  const int target = ce_target(p, row);
+  return CeRow{lse * kLog2e, g, g * expm1f(p.ce.target_logit[row] - lse), target < 0 ? -1 : target - (int)(p.ce.v0 + n0) - 4 * g4};
 }
 // The compiler has to have a requested value here.
-__device__ __forceinline__ void landed(CeRow& r) { asm volatile("" : "+v"(r.lse2), "+v"(r.g)); }
+__device__ __forceinline__ void landed(CeRow& r) { asm volatile("" : "+v"(r.lse2), "+v"(r.g), "+v"(r.own), "+v"(r.at)); }
 __device__ __forceinline__ void landed(int& v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ f32x4 ce_gradient(const CeRow& r, f32x4 x) {
+// x: the logits of this lane's columns 16 j .. 16 j + 3.
+__device__ __forceinline__ f32x4 ce_gradient(const CeRow& r, f32x4 x, int j) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = r.g * __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], kLog2e, -r.lse2));
+  for (int e = 0; e < 4; ++e) {
+    const float p = __builtin_amdgcn_exp2f(fminf(__builtin_fmaf(x[e], kLog2e, -r.lse2), 60.f));
+    x[e] = r.at == j * 16 + e ? r.own : r.g * p;
+  }
   return x;
 }
 

@@ -256,10 +256,10 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   if constexpr (EPI == Epilogue::kGradient) {
     static_for<0, TM>([&](auto row) {
       constexpr int i = decltype(row)::value;
-      const CeRow r = ce_row(p, m0 + (wm * TM + i) * 16 + l16);
+      const CeRow r = ce_row(p, m0 + (wm * TM + i) * 16 + l16, n0 + wn * TN * 16, g4);
       static_for<0, TN>([&](auto col) {
         constexpr int j = decltype(col)::value;
-        acc[i][j] = ce_gradient(r, acc[i][j]);
+        acc[i][j] = ce_gradient(r, acc[i][j], j);
       });
     });
   }

@@ -135,7 +135,7 @@ struct CePlan {
   int64_t rows;     // of the dense matrices: a run, and 256 at least
   int64_t vp, ldz;  // columns of a piece, their row stride
   int64_t strips;   // of the whole vocabulary
-  size_t order, count, per_row, x, part, z, dx;   // offsets into the workspace
+  size_t order, count, targets, per_row, x, part, z, dx;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
 
@@ -173,7 +173,8 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   };
   p->order = take(p->run * 4);
   p->count = take(4);
-  p->per_row = take(4 * p->rows * 4);
+  p->targets = take(p->rows * 8);
+  p->per_row = take(3 * p->rows * 4);
   p->x = take(p->rows * p->d * es);
   // forward: bfloat16 logits never leave the accumulators, float ones do
   const size_t shared = at;
@@ -209,17 +210,19 @@ template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, cons
   for (int64_t t0 = 0; t0 < p.n; t0 += p.run) {
     const int64_t n = p.n - t0 < p.run ? p.n - t0 : p.run;
     const CeRun run{desc, p, ws, t0, n, CeTokens{targets + t0, (int)n, (int*)(ws + p.order), (int*)(ws + p.count)}};
-    L(ce_select_kernel, dim3(1), dim3(1024), run.tokens);
     f(run, L);
   }
   return L.status();
 }
 
+// The tokens with a loss, and what is read of them, into dense matrices.
 void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
+  L(ce_select_kernel, dim3(1), dim3(1024), r.tokens);
   auto typed = [&](auto value) {
     using T = decltype(value);
     L(ce_gather_kernel<T>, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows,
-      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, (float*)(r.ws + r.p.per_row));
+      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, (int64_t*)(r.ws + r.p.targets),
+      (float*)(r.ws + r.p.per_row));
   };
   if (r.desc->io_dtype == ACC_BF16) typed(bf16{});
   else typed(float{});
@@ -232,11 +235,13 @@ void ce_logits_f32(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
 }
 
 // X . W^T over columns v0 .. v0 + vp - 1, bfloat16, into sums of exponentials or the logits' gradient [rows, ldz].
-template <Epilogue EPI> void ce_product(const CeRun& r, const void* W, int64_t v0, int64_t vp, Launcher& L) {
-  FastGemmParams p = fast_params(r.ws + r.p.x, r.w_piece(W, v0), r.ws + r.p.z, r.n, vp, r.p.d, r.p.d, r.p.ldw, r.p.ldz, nullptr, 1.f, 0.f);
+// X: null for the gathered tokens, else the run's, all of them.
+template <Epilogue EPI> void ce_product(const CeRun& r, const void* X, const void* W, int64_t v0, int64_t vp, Launcher& L) {
+  FastGemmParams p = fast_params(X ? X : r.ws + r.p.x, r.w_piece(W, v0), r.ws + r.p.z, r.n, vp, r.p.d, X ? r.p.ldx : r.p.d, r.p.ldw, r.p.ldz, nullptr, 1.f, 0.f);
   float* per_row = (float*)(r.ws + r.p.per_row);
-  p.live = r.tokens.count;
-  p.ce = CeRows{(const int*)per_row, per_row + r.p.rows, per_row + 3 * r.p.rows, per_row + 2 * r.p.rows, (f32x2*)(r.ws + r.p.part), r.p.rows, v0};
+  p.live = X ? nullptr : r.tokens.count;
+  p.ce = CeRows{X ? r.tokens.targets : (const int64_t*)(r.ws + r.p.targets), per_row + r.p.rows, per_row, per_row + 2 * r.p.rows,
+                (f32x2*)(r.ws + r.p.part), X ? r.n : r.p.rows, v0};
   if (EPI == Epilogue::kGradient && p.M < kCeLeastRows) p.M = kCeLeastRows;   // for the grid
   auto ring = [&](auto tm, auto tn) {
     constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = 3;
@@ -412,22 +417,27 @@ int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, con
   if (!workspace || ws_bytes < p.forward) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
   return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
-    ce_gather(r, X, nullptr, nullptr, L);
     float* per_row = (float*)(r.ws + r.p.per_row);
     if (desc->io_dtype == ACC_BF16) {
-      ce_product<Epilogue::kExpSums>(r, W, 0, r.p.v, L);
-      int across = 32;   // rows of a work-group
+      // Where one tile of the product holds all tokens nothing is saved by leaving some out.  (A token's logits are its own, so what
+      // stands in the row of one without a loss reaches no other.)
+      CeTokens tokens = r.tokens;
+      const bool as_they_come = r.n <= 256;
+      if (as_they_come) tokens.order = tokens.count = nullptr;
+      else ce_gather(r, X, nullptr, nullptr, L);
+      ce_product<Epilogue::kExpSums>(r, as_they_come ? (const bf16*)X + (size_t)r.t0 * r.p.ldx : nullptr, W, 0, r.p.v, L);
+      int across = 16;   // rows of a work-group
       while (across > 1 && across / 2 >= r.n) across /= 2;
-      const int strips = (int)r.p.strips;
-      L(ce_finish_kernel, dim3((unsigned)ceil_div(r.n, across)), dim3(256), r.tokens, (const f32x2*)(r.ws + r.p.part), strips, r.p.rows, across, r.p.v,
-        (const float*)(per_row + 2 * r.p.rows), loss + r.t0, stats + r.t0, r.p.n);
+      L(ce_finish_kernel, dim3((unsigned)ceil_div(r.n, across)), dim3(256), tokens, (const f32x2*)(r.ws + r.p.part), (int)r.p.strips,
+        as_they_come ? r.n : r.p.rows, across, r.p.v, (const float*)(per_row + r.p.rows), loss + r.t0, stats + r.t0, r.p.n);
       return;
     }
+    ce_gather(r, X, nullptr, nullptr, L);
     for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
       const int64_t vp = r.piece(v0);
       ce_logits_f32(r, W, v0, L);
       L(ce_piece_stats_kernel, dim3((unsigned)r.n), dim3(256), r.tokens, (const float*)(r.ws + r.p.z), r.p.ldz, v0, (int)vp, v0 == 0, v0 + vp == r.p.v,
-        r.p.v, per_row + r.p.rows, per_row + 2 * r.p.rows, per_row + 3 * r.p.rows, loss + r.t0, stats + r.t0, r.p.n);
+        r.p.v, per_row, per_row + r.p.rows, per_row + 2 * r.p.rows, loss + r.t0, stats + r.t0, r.p.n);
     }
   });
 }
@@ -452,12 +462,10 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
     for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
       const int64_t vp = r.piece(v0);
       if (b16) {
-        ce_product<Epilogue::kGradient>(r, W, v0, vp, L);
-        L(ce_target_kernel, dim3((unsigned)ceil_div(r.p.rows, 256)), dim3(256), (const int*)r.tokens.count, r.p.ldz, v0, (int)vp, r.p.rows,
-          (const float*)per_row, (bf16*)dz);
+        ce_product<Epilogue::kGradient>(r, nullptr, W, v0, vp, L);
       } else {
         ce_logits_f32(r, W, v0, L);
-        L(ce_piece_grad_kernel, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (float*)dz, r.p.ldz, v0, (int)vp, r.p.rows, (const float*)per_row);
+        L(ce_piece_grad_kernel, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (float*)dz, r.p.ldz, v0, (int)vp, r.p.rows, (const int64_t*)(r.ws + r.p.targets), (const float*)per_row);
       }
       if (dX) {
         if (!b16) f32_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, ACC_F32, r.p.d, r.n, r.p.d, vp, v0 > 0, L, true);
