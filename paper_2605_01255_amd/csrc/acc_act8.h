@@ -25,20 +25,29 @@ constexpr uint32_t kActTop = 0x7F700000u;   // 1.875 2^127, as float bits
 constexpr uint32_t kInf = 0x7F800000u;
 static_assert(kActBlock == 4 * kActTokens, "a wave's rows are one block");
 
-// Eight consecutive elements as float; p is 16-byte aligned.
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const f32x4 lo = *(const f32x4*)p, hi = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    v[t] = lo[t];
-    v[4 + t] = hi[t];
+// Eight consecutive elements as they lie in memory (16-byte aligned).
+template <typename T> struct ActRow;
+template <> struct ActRow<bf16> {
+  u32x4 raw;
+  __device__ __forceinline__ void load(const bf16* p) { raw = *(const u32x4*)p; }
+  __device__ __forceinline__ void clear() { raw = u32x4{0, 0, 0, 0}; }
+  // The compiler takes the value for a new one: it does not keep what it has unpacked of it in registers of its own.
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(raw)); }
+  template <int T> __device__ __forceinline__ float get() const { return __uint_as_float(T % 2 ? raw[T / 2] & 0xFFFF0000u : raw[T / 2] << 16); }
+  // bits: a float whose lower half is zero
+  template <int T> __device__ __forceinline__ void set(uint32_t bits) { raw[T / 2] = T % 2 ? (raw[T / 2] & 0xFFFFu) | bits : (raw[T / 2] & 0xFFFF0000u) | bits >> 16; }
+};
+template <> struct ActRow<float> {
+  u32x4 raw[2];
+  __device__ __forceinline__ void load(const float* p) {
+    raw[0] = *(const u32x4*)p;
+    raw[1] = *(const u32x4*)(p + 4);
   }
-}
-__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const bf16x8 x = *(const bf16x8*)p;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) v[t] = (float)x[t];
-}
+  __device__ __forceinline__ void clear() { raw[0] = raw[1] = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(raw[0]), "+v"(raw[1])); }
+  template <int T> __device__ __forceinline__ float get() const { return __uint_as_float(raw[T / 4][T % 4]); }
+  template <int T> __device__ __forceinline__ void set(uint32_t bits) { raw[T / 4][T % 4] = bits; }
+};
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
   *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -48,6 +57,40 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
 #pragma unroll
   for (int t = 0; t < 8; ++t) x[t] = (bf16)v[t];
   *(bf16x8*)p = x;
+}
+
+// The largest magnitude of each of a block's eight channels, as float bits, over this lane's tokens and those of the three lanes that
+// hold the block's others.  bfloat16 magnitudes are compared as they lie, two at a time.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ void act_largest(const ActRow<bf16> (&x)[kActTokens], uint32_t (&largest)[8]) {
+  static_for<0, 4>([&](auto pair) {
+    constexpr int P = decltype(pair)::value;
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < kActTokens; ++k) m = max_halves(m, x[k].raw[P] & 0x7FFF7FFFu);
+    m = max_halves(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = max_halves(m, (uint32_t)__shfl_xor((int)m, 32));
+    largest[2 * P] = m << 16;
+    largest[2 * P + 1] = m & 0xFFFF0000u;
+  });
+}
+__device__ __forceinline__ void act_largest(const ActRow<float> (&x)[kActTokens], uint32_t (&largest)[8]) {
+  static_for<0, 8>([&](auto channel) {
+    constexpr int C = decltype(channel)::value;
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < kActTokens; ++k) {
+      const uint32_t a = x[k].raw[C / 4][C % 4] & 0x7FFFFFFFu;
+      m = a > m ? a : m;
+    }
+    uint32_t o = (uint32_t)__shfl_xor((int)m, 16);
+    m = o > m ? o : m;
+    o = (uint32_t)__shfl_xor((int)m, 32);
+    largest[C] = o > m ? o : m;
+  });
 }
 
 // e + 127 of a block whose largest finite magnitude has these float bits.
@@ -76,20 +119,30 @@ template <int FORMAT> __device__ __forceinline__ uint32_t act_bytes(float y0, fl
 }
 template <int FORMAT> constexpr uint32_t kActNotFinite = FORMAT == ACC_ACT8_E4M3 ? 0x7Fu : 0x80u;
 
-// Element t of four bytes as float, without its scale.
-template <int FORMAT, int T> __device__ __forceinline__ float act_element(uint32_t w) {
+// Whether a lane's bytes may hold a code for what is not finite: the sign bits of bytes that are the int8 code (the lowest of them
+// exactly, others beside it perhaps).  e4m3's conversion gives NaN by itself.
+template <int FORMAT> __device__ __forceinline__ uint32_t act_odd(u32x2 q) {
+  if constexpr (FORMAT == ACC_ACT8_E4M3) return 0;
+  const uint32_t a = q[0] ^ 0x80808080u, b = q[1] ^ 0x80808080u;
+  return (((a - 0x01010101u) & ~a) | ((b - 0x01010101u) & ~b)) & 0x80808080u;
+}
+// Element t of four bytes as float, without its scale; CHECK: the int8 code for what is not finite may be among them.
+template <int FORMAT, int T, bool CHECK> __device__ __forceinline__ float act_element(uint32_t w) {
   if constexpr (FORMAT == ACC_ACT8_E4M3) {
     return __builtin_amdgcn_cvt_f32_fp8((int)w, T);
   } else {
-    const int q = (int)(w << (24 - 8 * T)) >> 24;
-    return q == -128 ? __uint_as_float(0x7FC00000u) : (float)q;
+    const int q = (int)(int8_t)(w >> (8 * T));
+    return CHECK && q == -128 ? __uint_as_float(0x7FC00000u) : (float)q;
   }
 }
-// Eight bytes times their scales.
-template <int FORMAT> __device__ __forceinline__ void act_values(u32x2 q, u32x2 e, float (&v)[8]) {
+// Eight bytes' scales; eight bytes times them.
+__device__ __forceinline__ void act_scales(u32x2 e, float (&scale)[8]) {
+  static_for<0, 8>([&](auto t) { scale[decltype(t)::value] = act_scale((e[decltype(t)::value / 4] >> (8 * (decltype(t)::value % 4))) & 0xFFu); });
+}
+template <int FORMAT, bool CHECK> __device__ __forceinline__ void act_values(u32x2 q, const float (&scale)[8], float (&v)[8]) {
   static_for<0, 8>([&](auto t) {
     constexpr int T = decltype(t)::value;
-    v[T] = act_element<FORMAT, T % 4>(q[T / 4]) * act_scale((e[T / 4] >> (8 * (T % 4))) & 0xFFu);
+    v[T] = act_element<FORMAT, T % 4, CHECK>(q[T / 4]) * scale[T];
   });
 }
 
@@ -116,92 +169,69 @@ inline __host__ int64_t act_work_groups(int64_t n, int64_t c) {  // of 256 lanes
   return ceil_div(ceil_div(n, kActBlock) * ceil_div(c, kActChannels), 4);
 }
 
-// This lane's eight tokens of eight channels, x[token][channel] (0 where a token does not exist), into the checkpoint [n, c].
-template <int FORMAT>
-__device__ __forceinline__ void act_keep(const ActLane& l, int64_t c, float (&x)[kActTokens][8], uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
+// This lane's eight tokens of eight channels (0 where a token does not exist) into the checkpoint [n, c].
+template <int FORMAT, typename T>
+__device__ __forceinline__ void act_keep(const ActLane& l, int64_t c, ActRow<T> (&x)[kActTokens], uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
   uint32_t largest[8], any = 0;
+  act_largest(x, largest);
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < kActTokens; ++k) {
-      const uint32_t a = __float_as_uint(x[k][t]) & 0x7FFFFFFFu;
-      m = a > m ? a : m;
-    }
-    largest[t] = m;
-    any = m > any ? m : any;
-  }
+  for (int t = 0; t < 8; ++t) any = largest[t] > any ? largest[t] : any;
   uint64_t odd = 0;   // bit 8 k + t: element [k][t] is not finite
   if (__any(any > kActTop)) {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int k = 0; k < kActTokens; ++k) {
-        const uint32_t bits = __float_as_uint(x[k][t]), a = bits & 0x7FFFFFFFu;
-        if (a >= kInf) {
-          odd |= (uint64_t)1 << (8 * k + t);
-          x[k][t] = 0.f;
-        } else {
-          const uint32_t kept = a < kActTop ? a : kActTop;
-          m = kept > m ? kept : m;
-          x[k][t] = __uint_as_float((bits & 0x80000000u) | kept);
-        }
-      }
-      largest[t] = m;
-    }
+    static_for<0, kActTokens * 8>([&](auto at) {
+      constexpr int K = decltype(at)::value / 8, C = decltype(at)::value % 8;
+      const uint32_t bits = __float_as_uint(x[K].template get<C>()), a = bits & 0x7FFFFFFFu;
+      if (a >= kInf) odd |= (uint64_t)1 << (8 * K + C);
+      x[K].template set<C>(a >= kInf ? 0u : a > kActTop ? (bits & 0x80000000u) | kActTop : bits);
+    });
+    act_largest(x, largest);
   }
+#pragma unroll
+  for (int k = 0; k < kActTokens; ++k) x[k].renew();
+  if (l.rows == 0) return;
   uint32_t e[8];
+  float inv[8];
 #pragma unroll
   for (int t = 0; t < 8; ++t) {
-    uint32_t m = largest[t], o = (uint32_t)__shfl_xor((int)m, 16);
-    m = o > m ? o : m;
-    o = (uint32_t)__shfl_xor((int)m, 32);
-    e[t] = act_exponent<FORMAT>(o > m ? o : m);
+    e[t] = act_exponent<FORMAT>(largest[t]);
+    inv[t] = act_inverse_scale(e[t]);
   }
-  if (l.rows == 0) return;
   if (l.group == 0) {
     const u32x2 packed = {e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24};
     *(u32x2*)(E + l.block * c + l.c) = packed;
   }
-  float inv[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) inv[t] = act_inverse_scale(e[t]);
-#pragma unroll
-  for (int k = 0; k < kActTokens; ++k) {
-    if (k >= l.rows) break;
+  static_for<0, kActTokens>([&](auto token) {
+    constexpr int K = decltype(token)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    if (K >= l.rows) return;
     u32x2 q;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t w = act_bytes<FORMAT>(x[k][4 * h] * inv[4 * h], x[k][4 * h + 1] * inv[4 * h + 1], x[k][4 * h + 2] * inv[4 * h + 2],
-                                     x[k][4 * h + 3] * inv[4 * h + 3]);
+    static_for<0, 2>([&](auto half) {
+      constexpr int H = decltype(half)::value, C = 4 * H;
+      uint32_t w = act_bytes<FORMAT>(x[K].template get<C>() * inv[C], x[K].template get<C + 1>() * inv[C + 1], x[K].template get<C + 2>() * inv[C + 2],
+                                     x[K].template get<C + 3>() * inv[C + 3]);
       if (odd) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          if (odd >> (8 * k + 4 * h + t) & 1) w = (w & ~(0xFFu << (8 * t))) | kActNotFinite<FORMAT> << (8 * t);
+          if (odd >> (8 * K + C + t) & 1) w = (w & ~(0xFFu << (8 * t))) | kActNotFinite<FORMAT> << (8 * t);
       }
-      q[h] = w;
-    }
-    *(u32x2*)(Q + (l.row + k) * c + l.c) = q;
-  }
+      q[H] = w;
+    });
+    *(u32x2*)(Q + (l.row + K) * c + l.c) = q;
+  });
 }
 
-template <typename T> __device__ __forceinline__ void act_load(const ActLane& l, const T* __restrict__ X, int64_t ld, float (&x)[kActTokens][8]) {
+template <typename T> __device__ __forceinline__ void act_load(const ActLane& l, const T* __restrict__ X, int64_t ld, ActRow<T> (&x)[kActTokens]) {
 #pragma unroll
   for (int k = 0; k < kActTokens; ++k) {
-    if (k < l.rows) {
-      load8(X + (l.row + k) * ld + l.c, x[k]);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 8; ++t) x[k][t] = 0.f;
-    }
+    if (k < l.rows) x[k].load(X + (l.row + k) * ld + l.c);
+    else x[k].clear();
   }
 }
 
 template <typename T, int FORMAT>
 __global__ __launch_bounds__(256) void act8_pack_kernel(const T* __restrict__ X, int64_t n, int64_t c, int64_t ld, uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
   const ActLane l = act_lane(n, c);
-  float x[kActTokens][8];
+  ActRow<T> x[kActTokens];
   act_load(l, X, ld, x);
   act_keep<FORMAT>(l, c, x, Q, E);
 }
@@ -215,11 +245,13 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(const uint8_t* __restr
 #pragma unroll
   for (int k = 0; k < kActTokens; ++k)
     if (k < l.rows) q[k] = *(const u32x2*)(Q + (l.row + k) * c + l.c);
+  float scale[8];
+  act_scales(e, scale);
 #pragma unroll
   for (int k = 0; k < kActTokens; ++k) {
     if (k >= l.rows) break;
     float v[8];
-    act_values<FORMAT>(q[k], e, v);
+    act_values<FORMAT, true>(q[k], scale, v);
     store8(X + (l.row + k) * ld + l.c, v);
   }
 }
@@ -231,28 +263,41 @@ template <typename T> __device__ __forceinline__ float sigmoid(float x) {
   else return 1.f / (1.f + expf(-x));
 }
 
-// H = silu(G) o U, and G and U into their checkpoints.
+// H = silu(G) o U, and G and U into their checkpoints.  A row of H at a time: unrolled together the rows' intermediate values take the
+// registers of two waves more per SIMD.
 template <typename T, int FORMAT>
 __global__ __launch_bounds__(256) void gated_fwd_kernel(const T* __restrict__ G, const T* __restrict__ U, int64_t n, int64_t f, int64_t ldg, int64_t ldh,
                                                         T* __restrict__ H, uint8_t* __restrict__ Qg, uint8_t* __restrict__ Eg, uint8_t* __restrict__ Qu,
                                                         uint8_t* __restrict__ Eu) {
   const ActLane l = act_lane(n, f);
-  float g[kActTokens][8], u[kActTokens][8];
+  ActRow<T> g[kActTokens], u[kActTokens];
   act_load(l, G, ldg, g);
   act_load(l, U, ldg, u);
+  static_for<0, kActTokens>([&](auto token) {
+    constexpr int K = decltype(token)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    if (K >= l.rows) return;
+    float h[8];
+    static_for<0, 8>([&](auto t) {
+      constexpr int C = decltype(t)::value;
+      const float x = g[K].template get<C>();
+      h[C] = x * sigmoid<T>(x) * u[K].template get<C>();
+    });
+    store8(H + (l.row + K) * ldh + l.c, h);
+  });
 #pragma unroll
   for (int k = 0; k < kActTokens; ++k) {
-    if (k >= l.rows) break;
-    float h[8];
-#pragma unroll
-    for (int t = 0; t < 8; ++t) h[t] = g[k][t] * sigmoid<T>(g[k][t]) * u[k][t];
-    store8(H + (l.row + k) * ldh + l.c, h);
+    g[k].renew();
+    u[k].renew();
   }
+  __builtin_amdgcn_sched_barrier(0);
   act_keep<FORMAT>(l, f, g, Qg, Eg);
+  __builtin_amdgcn_sched_barrier(0);
   act_keep<FORMAT>(l, f, u, Qu, Eu);
 }
 
-// With s = sigmoid(G^):  dU = dH o G^ s,  dG = dH o U^ s (1 + G^ (1 - s)),  and on request H = G^ s o U^ again.
+// With s = sigmoid(G^):  dU = dH o G^ s,  dG = dH o U^ s (1 + G^ (1 - s)),  and on request H = G^ s o U^ again.  A row at a time, as in
+// the forward pass.
 template <typename T, int FORMAT>
 __global__ __launch_bounds__(256) void gated_bwd_kernel(const T* __restrict__ dH, const uint8_t* __restrict__ Qg, const uint8_t* __restrict__ Eg,
                                                         const uint8_t* __restrict__ Qu, const uint8_t* __restrict__ Eu, int64_t n, int64_t f, int64_t ldg,
@@ -261,33 +306,46 @@ __global__ __launch_bounds__(256) void gated_bwd_kernel(const T* __restrict__ dH
   if (l.rows == 0) return;
   const u32x2 eg = *(const u32x2*)(Eg + l.block * f + l.c), eu = *(const u32x2*)(Eu + l.block * f + l.c);
   u32x2 qg[kActTokens], qu[kActTokens];
-  float dh[kActTokens][8];
+  ActRow<T> dh[kActTokens];
+  uint32_t odd = 0;
 #pragma unroll
   for (int k = 0; k < kActTokens; ++k)
     if (k < l.rows) {
       const int64_t row = l.row + k;
       qg[k] = *(const u32x2*)(Qg + row * f + l.c);
       qu[k] = *(const u32x2*)(Qu + row * f + l.c);
-      load8(dH + row * ldh + l.c, dh[k]);
+      dh[k].load(dH + row * ldh + l.c);
     }
+  float sg[8], su[8];
+  act_scales(eg, sg);
+  act_scales(eu, su);
 #pragma unroll
-  for (int k = 0; k < kActTokens; ++k) {
-    if (k >= l.rows) break;
-    const int64_t row = l.row + k;
-    float g[8], u[8], dg[8], du[8], h[8];
-    act_values<FORMAT>(qg[k], eg, g);
-    act_values<FORMAT>(qu[k], eu, u);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const float s = sigmoid<T>(g[t]), a = g[t] * s;
-      du[t] = dh[k][t] * a;
-      dg[t] = dh[k][t] * u[t] * (s + a * (1.f - s));
-      h[t] = a * u[t];
-    }
-    store8(dG + row * ldg + l.c, dg);
-    store8(dU + row * ldg + l.c, du);
-    if (H) store8(H + row * ldh + l.c, h);
-  }
+  for (int k = 0; k < kActTokens; ++k)
+    if (k < l.rows) odd |= act_odd<FORMAT>(qg[k]) | act_odd<FORMAT>(qu[k]);
+  auto rows = [&](auto check) {
+    static_for<0, kActTokens>([&](auto token) {
+      constexpr int K = decltype(token)::value;
+      constexpr bool CHECK = decltype(check)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      if (K >= l.rows) return;
+      const int64_t row = l.row + K;
+      float g[8], u[8], dg[8], du[8];
+      act_values<FORMAT, CHECK>(qg[K], sg, g);
+      act_values<FORMAT, CHECK>(qu[K], su, u);
+      static_for<0, 8>([&](auto t) {
+        constexpr int C = decltype(t)::value;
+        const float s = sigmoid<T>(g[C]), a = g[C] * s, d = dh[K].template get<C>();
+        du[C] = d * a;
+        dg[C] = d * u[C] * (s + a * (1.f - s));
+        u[C] *= a;
+      });
+      store8(dG + row * ldg + l.c, dg);
+      store8(dU + row * ldg + l.c, du);
+      if (H) store8(H + row * ldh + l.c, u);
+    });
+  };
+  if (__any(odd)) rows(std::true_type{});
+  else rows(std::false_type{});
 }
 
 }  // namespace acc
