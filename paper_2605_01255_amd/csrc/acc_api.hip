@@ -853,6 +853,14 @@ void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtyp
   else launch_generic<float, float, float, float, false, true>(p, 1, L);
 }
 
+void f32_split_product(const F32Operand& a, const F32Operand& b, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, bool accumulate,
+                       int64_t k_per_split, int64_t split_stride, Launcher& L) {
+  const int64_t kp = a.kmajor ? round_up(K, 4) : K;
+  if (f32_gemm_ok(a, b, M, round_up(N, 4), kp, C, ldc))
+    f32_gemm<float>(a, b, C, ldc, M, N, kp, L, accumulate, 1.f, 1.f, k_per_split, split_stride, 8, K);
+  else L.err = hipErrorInvalidValue;   // operands that no caller has
+}
+
 namespace {
 
 // Product of the stored left factor (Xs, or V of the RSVD path) and the small factor, left . Gr (or Gr . left^T in

@@ -10,6 +10,17 @@
 
 namespace acc {
 
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
 // What a call knows of its tokens.  `order` lists the tokens with a loss in their order, then the others; null: all tokens as they
 // come.
 struct CeTokens {
@@ -22,9 +33,14 @@ struct CeTokens {
 };
 
 // One work-group of 1024 threads, eight tokens of a thread at a time; the others fill the list from its end.
-__global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t) {
+// largest (with dloss, backward): the largest magnitude among the incoming gradients of tokens with a loss, 1 if there is none.  dz is
+// formed in units of it: the tokens' gradients are one value as a rule, which as part of dz would be rounded to bfloat16 the same way
+// in every row (an error of up to 2^-8 in the gradients that does not average out), and in its own units is 1.
+__global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float* __restrict__ dloss, float* __restrict__ largest) {
   constexpr int PER = 8;
   __shared__ int wave_kept[2][16];
+  __shared__ float wave_largest[16];
+  float top = 0.f;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int kept = 0, turn = 0;   // kept: so far
   for (int first = 0; first < t.n; first += 1024 * PER, turn ^= 1) {
@@ -53,21 +69,33 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       if (i0 + k >= t.n) break;
+      if (dloss && keep[k]) {
+        const float g = fabsf(dloss[i0 + k]);
+        top = fmaxf(top, isfinite(g) ? g : 0.f);
+      }
       if (keep[k]) t.order[at++] = i0 + k;
       else t.order[t.n - 1 - (i0 + k - at)] = i0 + k;
     }
     kept += total;
   }
   if (tid == 0) *t.count = kept;
+  if (!dloss) return;
+  top = wave_max(top);
+  if (lane == 0) wave_largest[wave] = top;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, wave_largest[w]);
+    *largest = top > 0.f ? top : 1.f;
+  }
 }
 
 // What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero, up to
 // 256 of them for the products' least rows.  targets: -1 where there is no gradient.  per_row, in a backward call: lse, the target's
-// logit and the incoming gradient, `rows` of each.
+// logit and the incoming gradient (over *unit), `rows` of each.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc, int64_t V,
-                                                        const float* __restrict__ stats, const float* __restrict__ dloss, int64_t stats_stride,
-                                                        int64_t* __restrict__ targets, float* __restrict__ per_row) {
+                                                        const float* __restrict__ stats, const float* __restrict__ dloss, const float* __restrict__ unit,
+                                                        int64_t stats_stride, int64_t* __restrict__ targets, float* __restrict__ per_row) {
   constexpr int VEC = 16 / sizeof(T);
   typedef T vecT __attribute__((ext_vector_type(VEC)));
   const int64_t r = blockIdx.x;
@@ -80,7 +108,7 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
     if (stats) {
       per_row[r] = lives ? stats[i] : 0.f;
       per_row[rows + r] = lives && target < V ? stats[stats_stride + i] : 0.f;
-      per_row[2 * rows + r] = lives && target < V ? dloss[i] : 0.f;
+      per_row[2 * rows + r] = lives && target < V ? dloss[i] / (unit ? *unit : 1.f) : 0.f;
     }
   }
   if (sizeof(T) == 2 && !lives && r >= 256) return;   // the float32 products read every row
@@ -89,17 +117,6 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
     if (lives) v = *(const vecT*)(X + (int64_t)i * ldx + c);
     *(vecT*)(Xc + r * d + c) = v;
   }
-}
-
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
 }
 
 // A sum of exponentials as (m, s) = s exp(m), m finite; s = 0: nothing.
@@ -113,39 +130,53 @@ __device__ __forceinline__ ExpSum operator+(ExpSum a, ExpSum b) {
   return ExpSum{m, a.s * expf(a.m - m) + b.s * expf(b.m - m)};
 }
 
-// Losses and statistics, one work-group per token, from the logits of one piece [rows, vp]; running sums between the pieces.
+// (m, s) over eight values at a time, each requested before the first is used.
+constexpr int kCeAtOnce = 8;
+__device__ __forceinline__ ExpSum with_values(ExpSum sum, const float (&v)[kCeAtOnce]) {   // -infinity: no value
+  float m = sum.s == 0.f ? -INFINITY : sum.m;   // an empty sum's maximum does not count; NaN is not 0
+#pragma unroll
+  for (int u = 0; u < kCeAtOnce; ++u) m = fmaxf(m, v[u]);
+  if (isinf(m)) m = 0.f;                        // exponentials of what is infinite are 0 or infinite, never NaN
+  float s = sum.s == 0.f ? 0.f : sum.s * __builtin_amdgcn_exp2f((sum.m - m) * kLog2e);
+#pragma unroll
+  for (int u = 0; u < kCeAtOnce; ++u) s += __builtin_amdgcn_exp2f((v[u] - m) * kLog2e);
+  return ExpSum{m, s};
+}
+
+// Losses and statistics, one work-group per token, from the logits of one piece [rows, vp] (rows 16-byte aligned); running sums between
+// the pieces.
 __global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const float* __restrict__ Z, int64_t ldz, int64_t v0, int vp, bool first,
-                                                             bool last, int64_t V, float* __restrict__ run_m, float* __restrict__ run_s,
-                                                             float* __restrict__ run_z, float* __restrict__ loss, float* __restrict__ stats,
+                                                             bool last, int64_t V, float* __restrict__ run_m, float* __restrict__ run_z,
+                                                             float* __restrict__ run_s, float* __restrict__ loss, float* __restrict__ stats,
                                                              int64_t stats_stride) {
-  __shared__ float red[8];
+  __shared__ ExpSum sums[256];
   const int64_t r = blockIdx.x;
-  const int tid = threadIdx.x, wave = tid >> 6;
+  const int tid = threadIdx.x;
   const int i = t.order[r];
   if (r >= *t.count) {
     if (last && tid == 0) loss[i] = stats[i] = stats[stats_stride + i] = 0.f;
     return;
   }
   const float* z = Z + r * ldz;
-  float m = -INFINITY;
-  bool nan = false;
-  for (int c = tid; c < vp; c += 256) {
-    m = fmaxf(m, z[c]);
-    nan |= z[c] != z[c];
+  ExpSum sum{0.f, 0.f};
+  for (int c = 8 * tid; c < vp; c += 2048) {   // ldz is a multiple of eight
+    const f32x4 lo = *(const f32x4*)(z + c), hi = *(const f32x4*)(z + c + 4);
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      v[u] = c + u < vp ? lo[u] : -INFINITY;
+      v[4 + u] = c + 4 + u < vp ? hi[u] : -INFINITY;
+    }
+    sum = with_values(sum, v);
   }
-  m = wave_max(m);
-  if ((tid & 63) == 0) red[wave] = m;
+  sums[tid] = sum;
   __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (isinf(m)) m = 0.f;
-  float s = 0.f;
-  for (int c = tid; c < vp; c += 256) s += expf(z[c] - m);
-  if (nan) s = NAN;
-  s = wave_sum(s);
-  if ((tid & 63) == 0) red[4 + wave] = s;
-  __syncthreads();
+  for (int half = 128; half; half /= 2) {
+    if (tid < half) sums[tid] = sums[tid] + sums[tid + half];
+    __syncthreads();
+  }
   if (tid) return;
-  ExpSum sum{m, red[4] + red[5] + red[6] + red[7]};
+  sum = sums[0];
   if (!first) sum = sum + ExpSum{run_m[r], run_s[r]};
   const int64_t target = t.targets[i];
   if (target >= v0 && target < v0 + vp) run_z[r] = z[target - v0];
@@ -166,10 +197,15 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, float* _
                                                             const int64_t* __restrict__ targets, const float* __restrict__ per_row) {
   const int64_t r = blockIdx.x, target = targets[r];   // -1 where there is no token or no gradient
   const float lse = per_row[r], zt = per_row[rows + r], g = per_row[2 * rows + r];
-  for (int64_t c = threadIdx.x; c < ldz; c += 256) {
-    float dz = 0.f;
-    if (target >= 0 && c < vp) dz = v0 + c == target ? g * expm1f(zt - lse) : g * expf(Z[r * ldz + c] - lse);
-    Z[r * ldz + c] = dz;
+  const float own = g * expm1f(zt - lse);
+  for (int64_t c = 4 * threadIdx.x; c < ldz; c += 1024) {
+    f32x4 x = *(const f32x4*)(Z + r * ldz + c);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float dz = v0 + c + u == target ? own : g * expf(x[u] - lse);
+      x[u] = target >= 0 && c + u < vp ? dz : 0.f;
+    }
+    *(f32x4*)(Z + r * ldz + c) = x;
   }
 }
 
@@ -221,15 +257,21 @@ __global__ __launch_bounds__(256) void ce_finish_kernel(CeTokens t, const f32x2*
   stats[stats_stride + i] = zt;
 }
 
-// dX [n, ldx] from the dense rows; tokens without a loss get zeros.  One work-group per row of the list.
+// dX [n, ldx] from the dense rows, the sum of `splits` matrices times *unit; tokens without a loss get zeros.  One work-group per row of
+// the list.
 template <typename T>
-__global__ __launch_bounds__(256) void ce_scatter_kernel(CeTokens t, const float* __restrict__ dXf, int d, T* __restrict__ dX, int64_t ldx) {
+__global__ __launch_bounds__(256) void ce_scatter_kernel(CeTokens t, const float* __restrict__ dXf, int splits, int64_t split_stride,
+                                                         const float* __restrict__ unit, int d, T* __restrict__ dX, int64_t ldx) {
   const int64_t r = blockIdx.x;
   const bool lives = r < *t.count;
   const int i = t.order[r];
   for (int c = (int)threadIdx.x * 4; c < d; c += 1024) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (lives) v = *(const f32x4*)(dXf + r * d + c);
+    if (lives) {
+#pragma unroll 4
+      for (int k = 0; k < splits; ++k) v += *(const f32x4*)(dXf + k * split_stride + r * d + c);
+      if (unit) v *= *unit;
+    }
     T* dst = dX + (int64_t)i * ldx + c;
 #pragma unroll
     for (int k = 0; k < 4; ++k) dst[k] = from_f32<T>(v[k]);

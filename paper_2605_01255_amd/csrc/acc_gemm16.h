@@ -265,10 +265,12 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   // of this lane's row in each block row, requested before an output tile's last K tile
   CeRow ce[EPI == Epilogue::kGradient ? TB : 1];
   int target[TB];
+  const float scale = !A_KMAJOR && p.scale ? *p.scale : 1.f;
   auto stage_write = [&](int i, int j) {
     bf16x4 v;
     f32x4 x = acc[i][j];
     if constexpr (EPI == Epilogue::kGradient) x = ce_gradient(ce[i], x, j);
+    if constexpr (!A_KMAJOR) x *= scale;
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[t] = (bf16)x[t];
     typedef bf16x4 __attribute__((address_space(3))) * lds_bf16x4_ptr;

@@ -253,6 +253,15 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
     ce_sums<TM, TN>(p, acc, target, m0 + wm * TM * 16, n0 + wn * TN * 16, l16, g4);
     return;
   }
+  if constexpr (!A_KMAJOR) {
+    if (p.scale) {
+      const float scale = *p.scale;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] *= scale;
+    }
+  }
   if constexpr (EPI == Epilogue::kGradient) {
     static_for<0, TM>([&](auto row) {
       constexpr int i = decltype(row)::value;

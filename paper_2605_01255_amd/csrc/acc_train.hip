@@ -54,9 +54,10 @@ void ring_token_gemm(FastGemmParams& p, Launcher& L) {
 
 template <typename TC, bool SUM>
 void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, Launcher& L,
-                const int* live) {
+                const int* live, const float* scale) {
   FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, nullptr, 1.f, 1.f);
   p.live = live;
+  p.scale = scale;
   const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
   const GemmChoice c = pick_gemm_tile(M, N, K, persist_ok);
   switch (c.tile) {
@@ -82,14 +83,14 @@ void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int
 }
 
 // C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.  live (bfloat16):
-// device count of the rows of both that take part, at most K; kCeLeastRows of them are read at least.
+// device count of the rows of both that take part, at most K; kCeLeastRows of them are read at least.  scale (bfloat16): device factor.
 void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t M,
-                   int64_t N, int64_t K, bool accumulate, Launcher& L, const int* live = nullptr) {
+                   int64_t N, int64_t K, bool accumulate, Launcher& L, const int* live = nullptr, const float* scale = nullptr) {
   if (io == ACC_BF16) {
     auto typed = [&](auto type) {
       using TC = decltype(type);
-      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L, live);
-      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L, live);
+      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L, live, scale);
+      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L, live, scale);
     };
     if (dtype == ACC_BF16) typed(bf16{});
     else typed(float{});
@@ -135,9 +136,32 @@ struct CePlan {
   int64_t rows;     // of the dense matrices: a run, and 256 at least
   int64_t vp, ldz;  // columns of a piece, their row stride
   int64_t strips;   // of the whole vocabulary
-  size_t order, count, targets, per_row, x, part, z, dx;   // offsets into the workspace
+  int64_t dx_per_split, dx_splits;   // columns of a piece in a part of dX's sum, parts
+  size_t order, count, unit, targets, per_row, x, part, z, dx;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
+
+// dX [n, d] is a sum over the whole piece: where its tiles leave compute units idle the sum is taken in parts, which the last kernel adds
+// up.  Parts of 512 columns at least.
+enum class CeDxTile { k64, k128x64, k128, k192x128 };
+CeDxTile ce_dx_tile(int64_t n, int64_t d) {
+  if (n <= 64) return CeDxTile::k64;
+  if (n <= 128) return CeDxTile::k128x64;
+  return ceil_div(n, 192) * ceil_div(d, 128) >= 400 ? CeDxTile::k192x128 : CeDxTile::k128;
+}
+void plan_ce_dx(CePlan* p, bool b16) {
+  int64_t tiles, groups = 512;   // work-groups, two or three to a compute unit
+  const CeDxTile tile = ce_dx_tile(p->run, p->d);
+  if (!b16) tiles = ceil_div(p->run, 64) * ceil_div(p->d, 64);
+  else if (tile == CeDxTile::k64) tiles = ceil_div(p->d, 64), groups = 768;
+  else if (tile == CeDxTile::k128x64) tiles = ceil_div(p->d, 64);
+  else tiles = tile == CeDxTile::k128 ? ceil_div(p->run, 128) * ceil_div(p->d, 128) : groups;
+  int64_t splits = groups / tiles;
+  if (splits > p->vp / 512) splits = p->vp / 512;
+  if (splits < 1) splits = 1;
+  p->dx_per_split = round_up(ceil_div(p->vp, splits), 64);
+  p->dx_splits = ceil_div(p->vp, p->dx_per_split);
+}
 
 int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (!d || (d->flags & ~(uint32_t)ACC_FLAG_DW_ACCUMULATE) || d->reserved) return ACC_ERR_INVALID_ARG;
@@ -173,6 +197,7 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   };
   p->order = take(p->run * 4);
   p->count = take(4);
+  p->unit = take(4);
   p->targets = take(p->rows * 8);
   p->per_row = take(3 * p->rows * 4);
   p->x = take(p->rows * p->d * es);
@@ -187,7 +212,8 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   p->forward = at;
   at = shared;   // backward: dz, then dX in float
   take(p->rows * p->ldz * es);
-  p->dx = take(p->rows * p->d * 4);
+  plan_ce_dx(p, d->io_dtype == ACC_BF16);
+  p->dx = take(p->dx_splits * p->rows * p->d * 4);
   p->backward = at > p->forward ? at : p->forward;
   return ACC_OK;
 }
@@ -217,11 +243,13 @@ template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, cons
 
 // The tokens with a loss, and what is read of them, into dense matrices.
 void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
-  L(ce_select_kernel, dim3(1), dim3(1024), r.tokens);
+  float* unit = (float*)(r.ws + r.p.unit);
+  const bool units = dloss && r.desc->io_dtype == ACC_BF16;
+  L(ce_select_kernel, dim3(1), dim3(1024), r.tokens, units ? dloss + r.t0 : nullptr, unit);
   auto typed = [&](auto value) {
     using T = decltype(value);
     L(ce_gather_kernel<T>, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows,
-      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, r.p.n, (int64_t*)(r.ws + r.p.targets),
+      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, units ? (const float*)unit : nullptr, r.p.n, (int64_t*)(r.ws + r.p.targets),
       (float*)(r.ws + r.p.per_row));
   };
   if (r.desc->io_dtype == ACC_BF16) typed(bf16{});
@@ -260,22 +288,29 @@ template <Epilogue EPI> void ce_product(const CeRun& r, const void* X, const voi
   else L.launch_lds(gemm16_persist_kernel<true, false, true, EPI>, dim3(256), dim3(256), (size_t)160 * 1024, p, 0);
 }
 
-// dX (float) (+)= dz . W_piece for the rows with a token.
+// dX (float, in its parts) (+)= dz . W_piece for the rows with a token.
 template <bool SUM> void ce_input_gradient(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
   FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), r.ws + r.p.dx, r.n, r.p.d, round_up(r.piece(v0), 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 1.f);
   p.kb_rows = r.piece(v0);
   p.live = r.tokens.count;
-  auto ring = [&](auto tm, auto tn, auto ns) {
+  p.k_per_split = r.p.dx_per_split;
+  p.c_split_stride = r.p.rows * r.p.d;
+  auto ring = [&](auto tm, auto tn, auto ns, auto split) {
     constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
     const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
-    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, false, SUM, true, Epilogue::kStore, true>, dim3(grid), dim3(256),
+    const int64_t splits = decltype(split)::value ? ceil_div(p.K, p.k_per_split) : 1;
+    p.tile_blocks = (int)grid;
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, decltype(split)::value, SUM, true, Epilogue::kStore, true>, dim3(grid * (unsigned)splits), dim3(256),
                  (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
   };
   using std::integral_constant;
-  const GemmChoice c = pick_gemm_tile(r.n, r.p.d, p.K, false);
-  if (c.tile == GemmTile::k256 || c.tile == GemmTile::k256x192 || c.tile == GemmTile::k192x128) ring(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  else if (c.tile == GemmTile::k128) ring(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  else ring(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
+  const std::true_type split{};
+  switch (ce_dx_tile(r.p.run, r.p.d)) {
+    case CeDxTile::k64: return ring(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{}, split);
+    case CeDxTile::k128x64: return ring(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{}, split);
+    case CeDxTile::k128: return ring(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{}, split);
+    case CeDxTile::k192x128: return ring(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{}, std::false_type{});
+  }
 }
 
 }  // namespace
@@ -458,6 +493,7 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
     ce_gather(r, X, stats, dloss, L);
     float* per_row = (float*)(r.ws + r.p.per_row);
     float* dxf = (float*)(r.ws + r.p.dx);
+    const float* unit = b16 ? (const float*)(r.ws + r.p.unit) : nullptr;
     char* dz = r.ws + r.p.z;
     for (int64_t v0 = 0; v0 < r.p.v; v0 += r.p.vp) {
       const int64_t vp = r.piece(v0);
@@ -468,7 +504,8 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
         L(ce_piece_grad_kernel, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (float*)dz, r.p.ldz, v0, (int)vp, r.p.rows, (const int64_t*)(r.ws + r.p.targets), (const float*)per_row);
       }
       if (dX) {
-        if (!b16) f32_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, ACC_F32, r.p.d, r.n, r.p.d, vp, v0 > 0, L, true);
+        if (!b16) f32_split_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, r.p.d, r.n, r.p.d, vp,
+                                    v0 > 0, r.p.dx_per_split, r.p.rows * r.p.d, L);
         else if (v0) ce_input_gradient<true>(r, W, v0, L);
         else ce_input_gradient<false>(r, W, v0, L);
       }
@@ -476,13 +513,15 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
         char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
         const bool add = r.t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
         token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 ? r.p.rows : r.n, add, L,
-                      b16 ? r.tokens.count : nullptr);
+                      b16 ? r.tokens.count : nullptr, unit);
       }
     }
     if (dX) {
       const dim3 grid((unsigned)r.n);
-      if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)dxf, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
-      else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, (const float*)dxf, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
+      const int splits = (int)r.p.dx_splits;
+      const int64_t stride = r.p.rows * r.p.d;
+      if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
+      else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
     }
   });
 }
