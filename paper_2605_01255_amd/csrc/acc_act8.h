@@ -259,6 +259,20 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(const uint8_t* __restr
   }
 }
 
+// The parts of a product added up: C[row, ldc] (+)= sum of `splits` matrices of `count` elements, rows of `row`.  Four elements a thread,
+// eight parts requested at a time.
+template <typename TC, bool SUM>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict__ parts, int splits, int64_t count, int64_t row, int64_t ldc, TC* __restrict__ C) {
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= count) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int k = 0; k < splits; ++k) sum += *(const f32x4*)(parts + k * count + e);
+  TC* dst = C + e / row * ldc + e % row;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) dst[t] = from_f32<TC>(SUM ? sum[t] + to_f32(dst[t]) : sum[t]);
+}
+
 // 1 / (1 + exp(-x)); 0 and 1 at the ends, as exp overflows to infinity or vanishes.  bfloat16 results take the hardware's
 // exponential and reciprocal (a few 2^-23 of the value, under the rounding of 2^-9), float32 ones the library's.
 template <typename T> __device__ __forceinline__ float sigmoid(float x) {

@@ -273,7 +273,7 @@ template <int TM, int TN, int NS, bool KMAJ, typename TC, bool SUM>
 void ring_gemm(FastGemmParams& p, Launcher& L) {
   const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
   p.red_stride = (int64_t)grid * 256 * 4;
-  L.launch_lds(gemm_ring_kernel<TM, TN, NS, KMAJ, TC, false, SUM>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+  L.launch_lds(gemm_ring_kernel<TM, TN, NS, KMAJ, TC, kNone, SUM>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
 }
 
 // C = beta C + alpha (A . B), C bf16, for a short K on the three-stage kernel of acc_gemm_smallk.h.
@@ -393,7 +393,7 @@ int fast_gemm_splitk(const void* A, const void* B, float* part, int64_t M, int64
   splits = ceil_div(K, p.k_per_split);
   p.tile_blocks = (int)grid;
   p.c_split_stride = M * ldc;
-  L.launch_lds(gemm_ring_kernel<TM, TN, NS, KMAJ, float, true>, dim3(grid * (unsigned)splits), dim3(256),
+  L.launch_lds(gemm_ring_kernel<TM, TN, NS, KMAJ, float, kSums>, dim3(grid * (unsigned)splits), dim3(256),
                (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
   return (int)splits;
 }

@@ -58,6 +58,7 @@ struct FastGemmParams {
   int64_t c_split_stride;
   // The vocabulary's cross entropy (acc_ce.h).  live: device count of the rows of A that take part, the others are behind them.
   const int* live;
+  int least_rows;         // rows of dz that are written and read whatever the count
   CeRows ce;
   const float* scale;     // products over the tokens: device value that the product is multiplied by, null: 1
   int64_t kb_rows;        // N-contiguous B only: rows of B that exist (0 = K); K may exceed it when A is

@@ -9,21 +9,17 @@ namespace acc {
 enum class Epilogue { kStore, kExpSums, kGradient };
 
 constexpr float kLog2e = 1.44269504088896341f;
-// Rows of the logits' gradient that are written, whatever the count: what the product over the tokens takes at least, three K tiles of
-// it; rows behind the count are zero.  The dense matrices have 256 rows or more.
-constexpr int kCeLeastRows = 192;
-
 template <Epilogue EPI> __device__ __forceinline__ void take_live_rows(FastGemmParams& p, int bm) {
   if (!p.live) return;   // all of them
   int rows = *p.live;
-  if (EPI == Epilogue::kGradient && rows < kCeLeastRows) rows = kCeLeastRows;
+  if (EPI == Epilogue::kGradient && rows < p.least_rows) rows = p.least_rows;
   p.M = rows;
   p.tiles_m = (rows + bm - 1) / bm;
 }
 __device__ __forceinline__ void take_live_tokens(FastGemmParams& p) {
   if (!p.live) return;
   const int rows = *p.live;
-  p.K = rows < kCeLeastRows ? kCeLeastRows : rows;
+  p.K = rows < p.least_rows ? p.least_rows : rows;
 }
 
 __device__ __forceinline__ int64_t ce_clamped(const FastGemmParams& p, int64_t row) { return row < p.ce.rows ? row : p.ce.rows - 1; }

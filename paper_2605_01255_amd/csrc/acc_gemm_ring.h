@@ -35,12 +35,13 @@ template <int BN> __device__ __forceinline__ int swz_ring(int krow) {
 template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // SPLIT: the K range is split over groups of tile_blocks work-groups (skinny products of the RSVD path), each storing its
-// partial product at C + split * c_split_stride; kb_rows as in FastGemmParams.  A running sum is then four K tiles, 256
+// partial product at C + split * c_split_stride; kb_rows as in FastGemmParams.  kPlain: nothing else.  kSums: a running sum is then four K tiles, 256
 // elements, long and these are added up: the number of splits (512 to 1536 elements each) does not decide how exact the
 // result is (error of a [16384, 3072] x [3072, 64] product: 6.3e-7 with one sum per split of 1536, 6.0e-7 so, 6.1e-7 with
 // the four splits of 768 that the two-stage kernel took; the time is the same).
+enum SplitK { kNone = 0, kSums = 1, kPlain = 2 };
 // SUM: C = beta C + alpha (A . B).  A form of its own: behind a branch its registers cost the plain one occupancy.
-template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, bool SPLIT = false, bool SUM = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore,
+template <int TM, int TN, int NS, bool B_KMAJOR, typename TC, int SPLIT = kNone, bool SUM = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore,
           bool LIVE = false>
 __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -152,13 +153,13 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
     }
   };
 
-  f32x4 acc[TM][TN], total[SPLIT ? TM : 1][SPLIT ? TN : 1];
+  f32x4 acc[TM][TN], total[SPLIT == kSums ? TM : 1][SPLIT == kSums ? TN : 1];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (SPLIT) total[i][j] = acc[i][j];
+      if constexpr (SPLIT == kSums) total[i][j] = acc[i][j];
     }
 
   if (has_tile) {
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   auto step = [&]() { ++kt; sc = sc + 1 == NS ? 0 : sc + 1; };
   auto after = [&]() { return sc + 1 == NS ? 0 : sc + 1; };
   auto add_up = [&]() {
-    if constexpr (SPLIT) {
+    if constexpr (SPLIT == kSums) {
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
     if (kt % 4 == 3) add_up();
   }
   ktile(kt, sc, sc, F{}, T{});
-  if constexpr (SPLIT) {
+  if constexpr (SPLIT == kSums) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll

@@ -104,6 +104,40 @@ static inline FactorTile pick_factor_tile(int64_t M, int64_t N, int64_t K, bool 
   return best;
 }
 
+// Products with a float result whose K range may be taken in parts that a later kernel adds up: products over the tokens (a long K and,
+// at small layers, few tiles) and the input gradient of the cross entropy (the vocabulary is its K).  The least of the ring kernel's
+// estimates (pick_gemm_tile), with tiles x parts in the place of tiles, and for more than one part the launch that adds them up and
+// their bytes, written and read at 4 TB/s.  A part has four K tiles at least.
+struct SplitChoice {
+  GemmTile tile;
+  bool one_round;
+  int64_t splits, k_per_split;
+  int64_t ns;            // the estimate
+};
+static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits) {
+  struct Cost { GemmTile tile; int bm, bn, per_tile, per_k, alone_per_tile, alone_per_k; };
+  static const Cost costs[] = {{GemmTile::k192x128, 192, 128, 1700, 580, 3500, 500},
+                               {GemmTile::k128, 128, 128, 2000, 460, 3000, 370},
+                               {GemmTile::k128x64, 128, 64, 1500, 280, 1500, 260},
+                               {GemmTile::k64, 64, 64, 500, 200, 500, 230}};
+  SplitChoice best{GemmTile::k64, true, 1, round_up(K, 64), INT64_MAX};
+  const int64_t kt = ceil_div(K, 64);
+  for (const Cost& c : costs) {
+    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(N, c.bn);
+    for (int64_t want = 1; want <= most_splits && (want == 1 || 4 * want <= kt); want = want < 8 ? want + 1 : want + want / 4) {
+      const int64_t part = ceil_div(kt, want), splits = ceil_div(kt, part), rounds = ceil_div(tiles * splits, 256);
+      if (splits != want) continue;
+      int64_t per_k = rounds == 1 ? c.alone_per_k : rounds * c.per_k;
+      if (c.tile == GemmTile::k64 && rounds == 2) per_k = 300;   // as in pick_gemm_tile
+      int64_t ns = 3000 + rounds * (rounds == 1 ? c.alone_per_tile : c.per_tile) + part * per_k;
+      if (splits > 1) ns += 4000 + splits * M * N / 500;
+      if (ns < best.ns) best = SplitChoice{c.tile, rounds == 1, splits, part * 64, ns};
+      if (rounds > 16) break;
+    }
+  }
+  return best;
+}
+
 // Token splits of the sketch contraction: enough work-groups to fill 256 CUs, at most 32 partials.
 static inline int generic_sketch_splits(int64_t n, int64_t c, int64_t r) {
   const int64_t tiles = ceil_div(c, 64) * ceil_div(r, 64);

@@ -45,52 +45,101 @@ void act8_unpack(int32_t dtype, int32_t format, const void* Q, const void* E, in
 
 // ---- products over the tokens -------------------------------------------------------------------------
 // C[M, N] (op)= At^T . B with At [K, M] and B [K, N]: both operands of the ring kernel by transposing reads.
-template <int TM, int TN, int NS, typename TC, bool SUM>
+template <int TM, int TN, int NS, typename TC, int SPLIT, bool SUM>
 void ring_token_gemm(FastGemmParams& p, Launcher& L) {
   const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
-  p.red_stride = (int64_t)grid * 256 * 4;
-  L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, TC, false, SUM, false>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+  const int64_t splits = SPLIT ? ceil_div(p.K, p.k_per_split) : 1;
+  p.tile_blocks = (int)grid;
+  L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, TC, SPLIT, SUM, false>, dim3(grid * (unsigned)splits), dim3(256),
+               (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+}
+
+// f(the tile's 16 x 16 blocks in both directions and its stages as constants)
+template <typename F> void with_ring_tile(GemmTile tile, bool one_round, F&& f) {
+  using std::integral_constant;
+  switch (tile) {
+    case GemmTile::k256:
+    case GemmTile::k256x192:
+    case GemmTile::k192x128: return one_round ? f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 3>{})
+                                              : f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    case GemmTile::k128: return one_round ? f(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 3>{})
+                                          : f(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    case GemmTile::k128x64: return f(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
+    case GemmTile::k64: return f(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});
+  }
+}
+
+// Which form a bfloat16 product over K tokens takes: in parts of K with a float result each (splits > 1), or whole on the tile of
+// pick_gemm_tile, or up to 256 tokens, which is a product of two factors in all but the operands' order, on pick_factor_tile's.
+struct TokenPlan {
+  GemmChoice whole;
+  SplitChoice parts;      // splits == 1: whole
+};
+TokenPlan plan_token_gemm(int64_t M, int64_t N, int64_t K, bool bf16_c, bool sum) {
+  TokenPlan plan{pick_gemm_tile(M, N, K, bf16_c && !sum && K > 128), pick_split_gemm(M, N, K, 64)};   // the persistent kernel takes three K tiles
+  if (K <= kFactorMaxK) {
+    plan.parts.splits = 1;
+    switch (pick_factor_tile(M, N, K, bf16_c, sum)) {
+      case FactorTile::k64: plan.whole.tile = GemmTile::k64; break;
+      case FactorTile::k128x64: plan.whole.tile = GemmTile::k128x64; break;
+      case FactorTile::k128: plan.whole.tile = GemmTile::k128; break;
+      case FactorTile::kPersist: plan.whole.tile = GemmTile::k256; break;
+      default: plan.whole.tile = GemmTile::k192x128;
+    }
+    plan.whole.one_round = false;
+  }
+  if (plan.whole.tile == GemmTile::k256x192) plan.whole.tile = GemmTile::k192x128;
+  return plan;
+}
+// Bytes of the parts of a product over K tokens, whatever it is added to.
+size_t token_parts_bytes(int32_t io, int64_t M, int64_t N, int64_t K) {
+  if (io != ACC_BF16 || K <= kFactorMaxK) return 0;
+  const SplitChoice c = pick_split_gemm(M, N, K, 64);
+  return c.splits > 1 ? (size_t)c.splits * M * N * sizeof(float) : 0;
 }
 
 template <typename TC, bool SUM>
 void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, Launcher& L,
-                const int* live, const float* scale) {
+                float* parts, const int* live, const float* scale, int least_rows) {
   FastGemmParams p = fast_params(A, B, C, M, N, K, lda, ldb, ldc, nullptr, 1.f, 1.f);
   p.live = live;
   p.scale = scale;
-  const bool persist_ok = sizeof(TC) == 2 && !SUM && K > 128;  // three K tiles
-  const GemmChoice c = pick_gemm_tile(M, N, K, persist_ok);
-  switch (c.tile) {
-    case GemmTile::k256:
-      if constexpr (sizeof(TC) == 2 && !SUM) {
-        const unsigned slots = gemm_bf16_plan(p, 256, 256);
-        p.red_stride = (int64_t)256 * 256 * 4;
-        L.launch_lds(gemm16_persist_kernel<false, true, false>, dim3(256), dim3(256), (size_t)160 * 1024, p, (int)slots);
-      }
-      break;
-    case GemmTile::k256x192:
-    case GemmTile::k192x128:
-      if (c.one_round) ring_token_gemm<6, 4, 3, TC, SUM>(p, L);
-      else ring_token_gemm<6, 4, 2, TC, SUM>(p, L);
-      break;
-    case GemmTile::k128:
-      if (c.one_round) ring_token_gemm<4, 4, 3, TC, SUM>(p, L);
-      else ring_token_gemm<4, 4, 2, TC, SUM>(p, L);
-      break;
-    case GemmTile::k128x64: ring_token_gemm<4, 2, 3, TC, SUM>(p, L); break;
-    case GemmTile::k64: ring_token_gemm<2, 2, 3, TC, SUM>(p, L); break;
+  p.least_rows = least_rows;
+  const TokenPlan plan = plan_token_gemm(M, N, K, sizeof(TC) == 2, SUM);
+  if (parts && plan.parts.splits > 1) {
+    p.C = parts;
+    p.ldc = N;
+    p.k_per_split = plan.parts.k_per_split;
+    p.c_split_stride = M * N;
+    with_ring_tile(plan.parts.tile, false, [&](auto tm, auto tn, auto ns) {
+      ring_token_gemm<decltype(tm)::value, decltype(tn)::value, decltype(ns)::value, float, kPlain, false>(p, L);
+    });
+    L(add_parts_kernel<TC, SUM>, dim3((unsigned)ceil_div(M * N, 1024)), dim3(256), (const float*)parts, (int)plan.parts.splits, M * N, N, ldc, (TC*)C);
+    return;
   }
+  if constexpr (sizeof(TC) == 2 && !SUM) {
+    if (plan.whole.tile == GemmTile::k256) {
+      const unsigned slots = gemm_bf16_plan(p, 256, 256);
+      L.launch_lds(gemm16_persist_kernel<false, true, false>, dim3(256), dim3(256), (size_t)160 * 1024, p, (int)slots);
+      return;
+    }
+  }
+  with_ring_tile(plan.whole.tile, plan.whole.one_round, [&](auto tm, auto tn, auto ns) {
+    ring_token_gemm<decltype(tm)::value, decltype(tn)::value, decltype(ns)::value, TC, kNone, SUM>(p, L);
+  });
 }
 
-// C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.  live (bfloat16):
-// device count of the rows of both that take part, at most K; kCeLeastRows of them are read at least.  scale (bfloat16): device factor.
+// C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.  parts: room of
+// token_parts_bytes, or null: not in parts.  live (bfloat16): device count of the rows of both that take part, at most K; least_rows of
+// them are read at least.  scale (bfloat16): device factor.
 void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t M,
-                   int64_t N, int64_t K, bool accumulate, Launcher& L, const int* live = nullptr, const float* scale = nullptr) {
+                   int64_t N, int64_t K, bool accumulate, Launcher& L, float* parts, const int* live = nullptr, const float* scale = nullptr,
+                   int least_rows = 0) {
   if (io == ACC_BF16) {
     auto typed = [&](auto type) {
       using TC = decltype(type);
-      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L, live, scale);
-      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L, live, scale);
+      if (accumulate) token_gemm<TC, true>(A, B, C, M, N, K, lda, ldb, ldc, L, parts, live, scale, least_rows);
+      else token_gemm<TC, false>(A, B, C, M, N, K, lda, ldb, ldc, L, parts, live, scale, least_rows);
     };
     if (dtype == ACC_BF16) typed(bf16{});
     else typed(float{});
@@ -105,8 +154,19 @@ int64_t token_chunk(int64_t n, int64_t ld, int32_t io) {
   return n <= most ? n : most / 64 * 64;
 }
 
-size_t act8_workspace_bytes(const acc_linear_desc* d, const Shape& s) {
-  return (size_t)token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, d->io_dtype) * (size_t)s.d_in * dtype_size(d->io_dtype);
+// The checkpoint's values, then the parts of the product with them.
+struct Act8Plan {
+  int64_t tokens;   // of one product
+  size_t parts, total;
+};
+Act8Plan plan_act8(const acc_linear_desc* d, const Shape& s) {
+  Act8Plan p{};
+  p.tokens = token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, d->io_dtype);
+  p.parts = (size_t)round_up(p.tokens * s.d_in * (int64_t)dtype_size(d->io_dtype), 256);
+  p.total = p.parts + token_parts_bytes(d->io_dtype, s.d_in, s.d_out, p.tokens);
+  const size_t other = p.parts + token_parts_bytes(d->io_dtype, s.d_out, s.d_in, p.tokens);
+  if (d->flags & ACC_FLAG_W_OUT_IN) p.total = other;
+  return p;
 }
 
 int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
@@ -136,31 +196,23 @@ struct CePlan {
   int64_t rows;     // of the dense matrices: a run, and 256 at least
   int64_t vp, ldz;  // columns of a piece, their row stride
   int64_t strips;   // of the whole vocabulary
-  int64_t dx_per_split, dx_splits;   // columns of a piece in a part of dX's sum, parts
+  SplitChoice dx_choice;   // of dX's sum over a piece
+  int least_rows;
   size_t order, count, unit, targets, per_row, x, part, z, dx;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
 
 // dX [n, d] is a sum over the whole piece: where its tiles leave compute units idle the sum is taken in parts, which the last kernel adds
-// up.  Parts of 512 columns at least.
-enum class CeDxTile { k64, k128x64, k128, k192x128 };
-CeDxTile ce_dx_tile(int64_t n, int64_t d) {
-  if (n <= 64) return CeDxTile::k64;
-  if (n <= 128) return CeDxTile::k128x64;
-  return ceil_div(n, 192) * ceil_div(d, 128) >= 400 ? CeDxTile::k192x128 : CeDxTile::k128;
-}
+// up (pick_split_gemm; in float32 parts enough for two 64 x 64 tiles to a compute unit, of 512 columns at least).
 void plan_ce_dx(CePlan* p, bool b16) {
-  int64_t tiles, groups = 512;   // work-groups, two or three to a compute unit
-  const CeDxTile tile = ce_dx_tile(p->run, p->d);
-  if (!b16) tiles = ceil_div(p->run, 64) * ceil_div(p->d, 64);
-  else if (tile == CeDxTile::k64) tiles = ceil_div(p->d, 64), groups = 768;
-  else if (tile == CeDxTile::k128x64) tiles = ceil_div(p->d, 64);
-  else tiles = tile == CeDxTile::k128 ? ceil_div(p->run, 128) * ceil_div(p->d, 128) : groups;
-  int64_t splits = groups / tiles;
-  if (splits > p->vp / 512) splits = p->vp / 512;
-  if (splits < 1) splits = 1;
-  p->dx_per_split = round_up(ceil_div(p->vp, splits), 64);
-  p->dx_splits = ceil_div(p->vp, p->dx_per_split);
+  p->dx_choice = pick_split_gemm(p->run, p->d, p->vp, 64);
+  if (!b16) {
+    int64_t splits = 512 / (ceil_div(p->run, 64) * ceil_div(p->d, 64));
+    if (splits > p->vp / 512) splits = p->vp / 512;
+    if (splits < 1) splits = 1;
+    p->dx_choice.k_per_split = round_up(ceil_div(p->vp, splits), 64);
+    p->dx_choice.splits = ceil_div(p->vp, p->dx_choice.k_per_split);
+  }
 }
 
 int plan_ce(const acc_ce_desc* d, CePlan* p) {
@@ -178,6 +230,9 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (p->run > 1 << 18) p->run = 1 << 18;
   if (p->run > p->n) p->run = p->n;
   p->rows = p->run < 256 ? 256 : p->run;
+  // rows of dz that are there whatever the number of tokens with a loss, zeros behind them: what the product over the tokens takes at
+  // least, three K tiles where it may run on the persistent kernel
+  p->least_rows = p->run <= 128 ? 64 : 192;
   // a piece: at most kCePieceBytes of dz, and of W what a buffer resource reaches
   int64_t vp = d->piece ? d->piece : kCePieceBytes / (p->rows * es) / 256 * 256;
   const int64_t most = ((int64_t)2 << 30) / (p->ldw * es) / 256 * 256;
@@ -213,7 +268,7 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   at = shared;   // backward: dz, then dX in float
   take(p->rows * p->ldz * es);
   plan_ce_dx(p, d->io_dtype == ACC_BF16);
-  p->dx = take(p->dx_splits * p->rows * p->d * 4);
+  p->dx = take(p->dx_choice.splits * p->rows * p->d * 4);
   p->backward = at > p->forward ? at : p->forward;
   return ACC_OK;
 }
@@ -270,11 +325,12 @@ template <Epilogue EPI> void ce_product(const CeRun& r, const void* X, const voi
   p.live = X ? nullptr : r.tokens.count;
   p.ce = CeRows{X ? r.tokens.targets : (const int64_t*)(r.ws + r.p.targets), per_row + r.p.rows, per_row, per_row + 2 * r.p.rows,
                 (f32x2*)(r.ws + r.p.part), X ? r.n : r.p.rows, v0};
-  if (EPI == Epilogue::kGradient && p.M < kCeLeastRows) p.M = kCeLeastRows;   // for the grid
+  p.least_rows = r.p.least_rows;
+  if (EPI == Epilogue::kGradient && p.M < p.least_rows) p.M = p.least_rows;   // for the grid
   auto ring = [&](auto tm, auto tn) {
     constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = 3;
     const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
-    L.launch_lds(gemm_ring_kernel<TM, TN, NS, true, bf16, false, false, true, EPI, true>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, true, bf16, kNone, false, true, EPI, true>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
   };
   using std::integral_constant;
   switch (ce_tile(r.p.run, r.p.d)) {
@@ -293,24 +349,15 @@ template <bool SUM> void ce_input_gradient(const CeRun& r, const void* W, int64_
   FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), r.ws + r.p.dx, r.n, r.p.d, round_up(r.piece(v0), 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 1.f);
   p.kb_rows = r.piece(v0);
   p.live = r.tokens.count;
-  p.k_per_split = r.p.dx_per_split;
+  p.k_per_split = r.p.dx_choice.k_per_split;
   p.c_split_stride = r.p.rows * r.p.d;
-  auto ring = [&](auto tm, auto tn, auto ns, auto split) {
+  with_ring_tile(r.p.dx_choice.tile, false, [&](auto tm, auto tn, auto ns) {
     constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
     const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
-    const int64_t splits = decltype(split)::value ? ceil_div(p.K, p.k_per_split) : 1;
     p.tile_blocks = (int)grid;
-    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, decltype(split)::value, SUM, true, Epilogue::kStore, true>, dim3(grid * (unsigned)splits), dim3(256),
-                 (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
-  };
-  using std::integral_constant;
-  const std::true_type split{};
-  switch (ce_dx_tile(r.p.run, r.p.d)) {
-    case CeDxTile::k64: return ring(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{}, split);
-    case CeDxTile::k128x64: return ring(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{}, split);
-    case CeDxTile::k128: return ring(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{}, split);
-    case CeDxTile::k192x128: return ring(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{}, std::false_type{});
-  }
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, kPlain, SUM, true, Epilogue::kStore, true>, dim3(grid * (unsigned)ceil_div(p.K, p.k_per_split)),
+                 dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+  });
 }
 
 }  // namespace
@@ -368,7 +415,7 @@ int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, 
 size_t acc_linear_act8_workspace_bytes(const acc_linear_desc* desc) {
   Shape s;
   if (validate_desc(desc, &s) != ACC_OK) return 0;
-  return act8_workspace_bytes(desc, s);
+  return plan_act8(desc, s).total;
 }
 
 int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY, const void* W, const void* Q, const void* E,
@@ -381,20 +428,22 @@ int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY,
   if (!dY || (!dX && !dW) || (dX && !W) || (dW && (!Q || !E))) return ACC_ERR_INVALID_ARG;
   if (!aligned16(dY) || !aligned16(W) || !aligned16(Q) || !aligned16(E) || !aligned16(dX) || !aligned16(dW) || !aligned16(workspace))
     return ACC_ERR_ALIGN;
-  if (dW && (!workspace || ws_bytes < act8_workspace_bytes(desc, s))) return ACC_ERR_WORKSPACE;
+  const Act8Plan plan = plan_act8(desc, s);
+  if (dW && (!workspace || ws_bytes < plan.total)) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
   Launcher L{(hipStream_t)stream};
   if (dX) exact_backward_gemm(desc, s, dY, W, dX, L);
   if (dW) {
     const bool w_oi = (desc->flags & ACC_FLAG_W_OUT_IN) != 0;
-    const int64_t chunk = token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, desc->io_dtype);
+    const int64_t chunk = plan.tokens;
+    float* parts = (float*)((char*)workspace + plan.parts);
     for (int64_t t0 = 0; t0 < s.n; t0 += chunk) {
       const int64_t nt = s.n - t0 < chunk ? s.n - t0 : chunk;
       const char* dy = (const char*)dY + (size_t)t0 * s.ldy * dtype_size(desc->io_dtype);
       act8_unpack(desc->io_dtype, format, (const char*)Q + t0 * s.d_in, (const char*)E + t0 / kActBlock * s.d_in, nt, s.d_in, s.d_in, workspace, L);
       const bool add = t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
-      if (w_oi) token_product(desc->io_dtype, desc->dw_dtype, dy, s.ldy, workspace, s.d_in, dW, s.d_in, s.d_out, s.d_in, nt, add, L);
-      else token_product(desc->io_dtype, desc->dw_dtype, workspace, s.d_in, dy, s.ldy, dW, s.d_out, s.d_in, s.d_out, nt, add, L);
+      if (w_oi) token_product(desc->io_dtype, desc->dw_dtype, dy, s.ldy, workspace, s.d_in, dW, s.d_in, s.d_out, s.d_in, nt, add, L, nt == chunk ? parts : nullptr);
+      else token_product(desc->io_dtype, desc->dw_dtype, workspace, s.d_in, dy, s.ldy, dW, s.d_out, s.d_in, s.d_out, nt, add, L, nt == chunk ? parts : nullptr);
     }
   }
   return L.status();
@@ -505,20 +554,20 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
       }
       if (dX) {
         if (!b16) f32_split_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, r.p.d, r.n, r.p.d, vp,
-                                    v0 > 0, r.p.dx_per_split, r.p.rows * r.p.d, L);
+                                    v0 > 0, r.p.dx_choice.k_per_split, r.p.rows * r.p.d, L);
         else if (v0) ce_input_gradient<true>(r, W, v0, L);
         else ce_input_gradient<false>(r, W, v0, L);
       }
       if (dW) {
         char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
         const bool add = r.t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
-        token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 ? r.p.rows : r.n, add, L,
-                      b16 ? r.tokens.count : nullptr, unit);
+        token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 && r.n < r.p.least_rows ? r.p.least_rows : r.n, add,
+                      L, nullptr, b16 ? r.tokens.count : nullptr, unit, r.p.least_rows);
       }
     }
     if (dX) {
       const dim3 grid((unsigned)r.n);
-      const int splits = (int)r.p.dx_splits;
+      const int splits = (int)r.p.dx_choice.splits;
       const int64_t stride = r.p.rows * r.p.d;
       if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
       else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
