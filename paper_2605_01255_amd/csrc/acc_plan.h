@@ -104,36 +104,52 @@ static inline FactorTile pick_factor_tile(int64_t M, int64_t N, int64_t K, bool 
   return best;
 }
 
-// Products with a float result whose K range may be taken in parts that a later kernel adds up: products over the tokens (a long K and,
-// at small layers, few tiles) and the input gradient of the cross entropy (the vocabulary is its K).  The least of the ring kernel's
-// estimates (pick_gemm_tile), with tiles x parts in the place of tiles, and for more than one part the launch that adds them up and
-// their bytes, written and read at 4 TB/s.  A part has four K tiles at least.
+// Products whose K range may be taken in parts that a later kernel adds up: products over the tokens (a long K and, at small layers, few
+// tiles) and the input gradient of the cross entropy (the vocabulary is its K).  The least of estimates like pick_gemm_tile's, with tiles
+// x parts in the place of tiles, and for more than one part the launch that adds them up and their bytes, written and read at 4 TB/s.
+// A part has four K tiles at least.
+// over_tokens: both operands are read transposed, at half the rate from LDS, which the smaller wave tiles wait for (2048 x 2048 over
+// 32768 tokens on 128 x 128, one work-group per compute unit: 0.63 us a K tile, where a K-contiguous operand takes 0.37; two work-groups
+// cover each other's: 297 us in four parts, 323 in one).  Measured us there on 256 x 256 / 192 x 128 / 128 x 128 / 128 x 64 / 64 x 64
+// and the best with its parts:
+//   2048 x 2048 over 8192    176 / 119 /  87 /  88 /  - , 76 (128, 2)       512 x 512 over 8192    143 / 112 / 81 / - / - , 14.7 (64, 8)
+//   4096 x 4096 over 1024     33 /  57 /  39 /  48 / 47                     1544 x 1032 over 2049   47 /  34 / 25 / 16.8 / 20.8
+//   128000 x 4096 over 64      - / 318 / 243 / 328 / 380                    50264 x 2048 over 512  104 / 193 / 139 / 231 / 211
 struct SplitChoice {
   GemmTile tile;
   bool one_round;
   int64_t splits, k_per_split;
   int64_t ns;            // the estimate
 };
-static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits) {
+static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits, bool over_tokens = false, bool persist_ok = false) {
   struct Cost { GemmTile tile; int bm, bn, per_tile, per_k, alone_per_tile, alone_per_k; };
-  static const Cost costs[] = {{GemmTile::k192x128, 192, 128, 1700, 580, 3500, 500},
-                               {GemmTile::k128, 128, 128, 2000, 460, 3000, 370},
-                               {GemmTile::k128x64, 128, 64, 1500, 280, 1500, 260},
-                               {GemmTile::k64, 64, 64, 500, 200, 500, 230}};
+  static const Cost contiguous[] = {{GemmTile::k192x128, 192, 128, 1700, 580, 3500, 500},
+                                    {GemmTile::k128, 128, 128, 2000, 460, 3000, 370},
+                                    {GemmTile::k128x64, 128, 64, 1500, 280, 1500, 260},
+                                    {GemmTile::k64, 64, 64, 500, 200, 500, 230}};
+  static const Cost transposed[] = {{GemmTile::k192x128, 192, 128, 3000, 800, 4500, 880},
+                                    {GemmTile::k128, 128, 128, 1460, 480, 3000, 630},
+                                    {GemmTile::k128x64, 128, 64, 940, 320, 1500, 370},
+                                    {GemmTile::k64, 64, 64, 560, 185, 500, 220}};
   SplitChoice best{GemmTile::k64, true, 1, round_up(K, 64), INT64_MAX};
   const int64_t kt = ceil_div(K, 64);
-  for (const Cost& c : costs) {
-    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(N, c.bn);
+  for (int c = 0; c < 4; ++c) {
+    const Cost& cost = over_tokens ? transposed[c] : contiguous[c];
+    const int64_t tiles = ceil_div(M, cost.bm) * ceil_div(N, cost.bn);
     for (int64_t want = 1; want <= most_splits && (want == 1 || 4 * want <= kt); want = want < 8 ? want + 1 : want + want / 4) {
       const int64_t part = ceil_div(kt, want), splits = ceil_div(kt, part), rounds = ceil_div(tiles * splits, 256);
       if (splits != want) continue;
-      int64_t per_k = rounds == 1 ? c.alone_per_k : rounds * c.per_k;
-      if (c.tile == GemmTile::k64 && rounds == 2) per_k = 300;   // as in pick_gemm_tile
-      int64_t ns = 3000 + rounds * (rounds == 1 ? c.alone_per_tile : c.per_tile) + part * per_k;
+      int64_t per_k = rounds == 1 ? cost.alone_per_k : rounds * cost.per_k;
+      if (!over_tokens && cost.tile == GemmTile::k64 && rounds == 2) per_k = 300;   // as in pick_gemm_tile
+      int64_t ns = 3000 + rounds * (rounds == 1 ? cost.alone_per_tile : cost.per_tile) + part * per_k;
       if (splits > 1) ns += 4000 + splits * M * N / 500;
-      if (ns < best.ns) best = SplitChoice{c.tile, rounds == 1, splits, part * 64, ns};
+      if (ns < best.ns) best = SplitChoice{cost.tile, rounds == 1, splits, part * 64, ns};
       if (rounds > 16) break;
     }
+  }
+  if (persist_ok) {   // the persistent kernel, whole; a short K does not cover its tile's write
+    const int64_t rounds = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256), ns = 5000 + rounds * ((kt < 16 ? 5000 : 2000) + kt * 1340);
+    if (ns < best.ns) best = SplitChoice{GemmTile::k256, rounds == 1, 1, round_up(K, 64), ns};
   }
   return best;
 }

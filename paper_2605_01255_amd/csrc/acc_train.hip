@@ -54,7 +54,7 @@ void ring_token_gemm(FastGemmParams& p, Launcher& L) {
                (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
 }
 
-// f(the tile's 16 x 16 blocks in both directions and its stages as constants)
+// f(the tile's 16 x 16 blocks in both directions and its stages as constants): three stages where a compute unit has one work-group
 template <typename F> void with_ring_tile(GemmTile tile, bool one_round, F&& f) {
   using std::integral_constant;
   switch (tile) {
@@ -69,32 +69,15 @@ template <typename F> void with_ring_tile(GemmTile tile, bool one_round, F&& f) 
   }
 }
 
-// Which form a bfloat16 product over K tokens takes: in parts of K with a float result each (splits > 1), or whole on the tile of
-// pick_gemm_tile, or up to 256 tokens, which is a product of two factors in all but the operands' order, on pick_factor_tile's.
-struct TokenPlan {
-  GemmChoice whole;
-  SplitChoice parts;      // splits == 1: whole
-};
-TokenPlan plan_token_gemm(int64_t M, int64_t N, int64_t K, bool bf16_c, bool sum) {
-  TokenPlan plan{pick_gemm_tile(M, N, K, bf16_c && !sum && K > 128), pick_split_gemm(M, N, K, 64)};   // the persistent kernel takes three K tiles
-  if (K <= kFactorMaxK) {
-    plan.parts.splits = 1;
-    switch (pick_factor_tile(M, N, K, bf16_c, sum)) {
-      case FactorTile::k64: plan.whole.tile = GemmTile::k64; break;
-      case FactorTile::k128x64: plan.whole.tile = GemmTile::k128x64; break;
-      case FactorTile::k128: plan.whole.tile = GemmTile::k128; break;
-      case FactorTile::kPersist: plan.whole.tile = GemmTile::k256; break;
-      default: plan.whole.tile = GemmTile::k192x128;
-    }
-    plan.whole.one_round = false;
-  }
-  if (plan.whole.tile == GemmTile::k256x192) plan.whole.tile = GemmTile::k192x128;
-  return plan;
+// The form of a bfloat16 product over K tokens; the persistent kernel takes three K tiles and stores bfloat16.
+SplitChoice plan_token_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits, bool bf16_c, bool sum) {
+  return pick_split_gemm(M, N, K, most_splits, true, bf16_c && !sum && K > 128);
 }
-// Bytes of the parts of a product over K tokens, whatever it is added to.
-size_t token_parts_bytes(int32_t io, int64_t M, int64_t N, int64_t K) {
-  if (io != ACC_BF16 || K <= kFactorMaxK) return 0;
-  const SplitChoice c = pick_split_gemm(M, N, K, 64);
+constexpr int64_t kTokenParts = 64;
+// Bytes of the parts of a product over K tokens.
+size_t token_parts_bytes(int32_t io, int32_t dtype, bool sum, int64_t M, int64_t N, int64_t K) {
+  if (io != ACC_BF16) return 0;
+  const SplitChoice c = plan_token_gemm(M, N, K, kTokenParts, dtype == ACC_BF16, sum);
   return c.splits > 1 ? (size_t)c.splits * M * N * sizeof(float) : 0;
 }
 
@@ -105,26 +88,26 @@ void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int
   p.live = live;
   p.scale = scale;
   p.least_rows = least_rows;
-  const TokenPlan plan = plan_token_gemm(M, N, K, sizeof(TC) == 2, SUM);
-  if (parts && plan.parts.splits > 1) {
+  const SplitChoice plan = plan_token_gemm(M, N, K, parts ? kTokenParts : 1, sizeof(TC) == 2, SUM);
+  if (plan.splits > 1) {
     p.C = parts;
     p.ldc = N;
-    p.k_per_split = plan.parts.k_per_split;
+    p.k_per_split = plan.k_per_split;
     p.c_split_stride = M * N;
-    with_ring_tile(plan.parts.tile, false, [&](auto tm, auto tn, auto ns) {
+    with_ring_tile(plan.tile, plan.one_round, [&](auto tm, auto tn, auto ns) {
       ring_token_gemm<decltype(tm)::value, decltype(tn)::value, decltype(ns)::value, float, kPlain, false>(p, L);
     });
-    L(add_parts_kernel<TC, SUM>, dim3((unsigned)ceil_div(M * N, 1024)), dim3(256), (const float*)parts, (int)plan.parts.splits, M * N, N, ldc, (TC*)C);
+    L(add_parts_kernel<TC, SUM>, dim3((unsigned)ceil_div(M * N, 1024)), dim3(256), (const float*)parts, (int)plan.splits, M * N, N, ldc, (TC*)C);
     return;
   }
   if constexpr (sizeof(TC) == 2 && !SUM) {
-    if (plan.whole.tile == GemmTile::k256) {
+    if (plan.tile == GemmTile::k256) {
       const unsigned slots = gemm_bf16_plan(p, 256, 256);
       L.launch_lds(gemm16_persist_kernel<false, true, false>, dim3(256), dim3(256), (size_t)160 * 1024, p, (int)slots);
       return;
     }
   }
-  with_ring_tile(plan.whole.tile, plan.whole.one_round, [&](auto tm, auto tn, auto ns) {
+  with_ring_tile(plan.tile, plan.one_round, [&](auto tm, auto tn, auto ns) {
     ring_token_gemm<decltype(tm)::value, decltype(tn)::value, decltype(ns)::value, TC, kNone, SUM>(p, L);
   });
 }
@@ -163,9 +146,14 @@ Act8Plan plan_act8(const acc_linear_desc* d, const Shape& s) {
   Act8Plan p{};
   p.tokens = token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, d->io_dtype);
   p.parts = (size_t)round_up(p.tokens * s.d_in * (int64_t)dtype_size(d->io_dtype), 256);
-  p.total = p.parts + token_parts_bytes(d->io_dtype, s.d_in, s.d_out, p.tokens);
-  const size_t other = p.parts + token_parts_bytes(d->io_dtype, s.d_out, s.d_in, p.tokens);
-  if (d->flags & ACC_FLAG_W_OUT_IN) p.total = other;
+  const bool w_oi = (d->flags & ACC_FLAG_W_OUT_IN) != 0;
+  const int64_t M = w_oi ? s.d_out : s.d_in, N = w_oi ? s.d_in : s.d_out;
+  size_t parts = 0;   // of the first product, and of those that are added to it
+  for (bool sum : {(d->flags & ACC_FLAG_DW_ACCUMULATE) != 0, true}) {
+    const size_t bytes = token_parts_bytes(d->io_dtype, d->dw_dtype, sum, M, N, p.tokens);
+    if (bytes > parts && (!sum || (d->flags & ACC_FLAG_DW_ACCUMULATE) || p.tokens < s.n)) parts = bytes;
+  }
+  p.total = p.parts + parts;
   return p;
 }
 
@@ -242,7 +230,7 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (vp < 256) vp = 256;
   if (vp > p->v) vp = p->v;
   p->vp = vp;
-  p->ldz = round_up(vp, 8);
+  p->ldz = round_up(vp, 64);   // whole cache lines: rows that begin inside one cost the product with W twice the requests
   p->strips = ceil_div(p->v, ce_strip(p->run, p->d));
   size_t at = 0;
   auto take = [&](int64_t bytes) {
