@@ -18,6 +18,7 @@ import torch
 from . import binding as acc
 
 _CODES = {torch.bfloat16: acc.ACC_BF16, torch.float32: acc.ACC_F32}
+_FORMATS = {"e4m3": acc.ACC_ACT8_E4M3, "int8": acc.ACC_ACT8_INT8}   # 8-bit checkpoints
 
 
 def _workspace(nbytes: int, device):
@@ -28,7 +29,9 @@ class CompressedLinearFunction(torch.autograd.Function):
     """y = x @ weight.T (+ bias) with `weight` in torch.nn.Linear's [out_features, in_features] layout.
 
     compressor "rp": the seeded Gaussian token sketch (unbiased; keeps Xs [in_features, rank] + the seed);
-    compressor "rsvd": randomized range finder + projection (keeps U [tokens, rank] and V [in_features, rank]).
+    compressor "rsvd": randomized range finder + projection (keeps U [tokens, rank] and V [in_features, rank]);
+    compressor "e4m3" or "int8": an 8-bit checkpoint of the whole input (1 + 1 / 32 bytes per element, `rank` unused), from
+    which the weight gradient is formed in full.
     `seed` must differ from call to call for the random projection to be unbiased over a training run.
     Linears that share an input (q/k/v, gate/up; Sec. 5.1) are compressed once by stacking their weights
     into one call.
@@ -59,8 +62,16 @@ class CompressedLinearFunction(torch.autograd.Function):
             v = torch.empty(d_in, rank, dtype=x.dtype, device=dev)
             acc.acc_linear_fwd_rsvd(desc, x2, w, y, u, v, _workspace(acc.acc_rsvd_workspace_bytes(desc, False), dev))
             ctx.save_for_backward(w, u, v)
+        elif compressor in _FORMATS:
+            if factor_sink is not None:
+                raise ValueError("an 8-bit checkpoint gives a full weight gradient, not a factored one")
+            fmt = _FORMATS[compressor]
+            q, e = acc.alloc_act8(acc.make_act8_desc(n, d_in, io_dtype=code, format=fmt), dev)
+            with torch.cuda.device(dev):
+                acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, q, e)
+            ctx.save_for_backward(w, q, e)
         else:
-            raise ValueError("compressor must be 'rp' or 'rsvd'")
+            raise ValueError("compressor must be 'rp', 'rsvd', 'e4m3' or 'int8'")
         if bias is not None:
             y += bias
         ctx.meta = (compressor, n, d_in, d_out, rank, seed, code, bias is not None, x.shape)
@@ -74,6 +85,8 @@ class CompressedLinearFunction(torch.autograd.Function):
         if not dy2.is_contiguous():
             dy2 = dy2.contiguous()
         dev, dt = dy.device, dy.dtype
+        if compressor in _FORMATS:
+            return CompressedLinearFunction._backward_act8(ctx, dy2)
         dx = torch.empty(n, d_in, dtype=dt, device=dev)
         gr = torch.empty(d_out, rank, dtype=dt, device=dev)
         sink = ctx.factor_sink
@@ -98,12 +111,32 @@ class CompressedLinearFunction(torch.autograd.Function):
             acc.acc_linear_bias_grad(desc, dy2, db, ws)
         return dx.reshape(x_shape), dw, db, None, None, None, None, None
 
+    @staticmethod
+    def _backward_act8(ctx, dy2):
+        compressor, n, d_in, d_out, _, _, code, has_bias, x_shape = ctx.meta
+        w, q, e = ctx.saved_tensors
+        dev, dt = dy2.device, dy2.dtype
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        desc = acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=acc.ACC_FLAG_W_OUT_IN)
+        dx = torch.empty(n, d_in, dtype=dt, device=dev) if want_dx else None
+        dw = torch.empty(d_out, d_in, dtype=dt, device=dev) if want_dw else None
+        db = None
+        with torch.cuda.device(dev):
+            if want_dx or want_dw:
+                ws = _workspace(acc.acc_linear_act8_workspace_bytes(desc), dev) if want_dw else None
+                acc.acc_linear_bwd_act8(desc, _FORMATS[compressor], dy2, w, q, e, dx, dw, ws)
+            if has_bias and ctx.needs_input_grad[2]:
+                db = torch.empty(d_out, dtype=dt, device=dev)
+                acc.acc_linear_bias_grad(desc, dy2, db, _workspace(acc.acc_linear_workspace_bytes(desc, True), dev))
+        return None if dx is None else dx.reshape(x_shape), dw, db, None, None, None, None, None
+
 
 class CompressedLinear(torch.nn.Module):
     """Drop-in for torch.nn.Linear (same parameter names and layout) that keeps only the compressed input
-    for the backward pass.  Each forward call draws a fresh sketch seed from a per-module counter."""
+    for the backward pass.  Each forward call draws a fresh sketch seed from a per-module counter.  `rank` is that of the
+    "rp" and "rsvd" compressors; "e4m3" and "int8" have none."""
 
-    def __init__(self, in_features: int, out_features: int, rank: int, bias: bool = True, compressor: str = "rp",
+    def __init__(self, in_features: int, out_features: int, rank: int = 0, bias: bool = True, compressor: str = "rp",
                  seed: int = 0, power_iters: int = 0, device=None, dtype=torch.bfloat16, factored_grad: bool = False):
         super().__init__()
         self.factored_grad = factored_grad
@@ -126,6 +159,152 @@ class CompressedLinear(torch.nn.Module):
     def extra_repr(self):
         return (f"in_features={self.in_features}, out_features={self.out_features}, rank={self.rank}, "
                 f"compressor={self.compressor}, bias={self.bias is not None}")
+
+
+def _rows(t, width):
+    """t as rows of `width` elements the library can take as they lie (16-byte aligned, any stride), else a copy."""
+    t2 = t.reshape(-1, width)
+    if t2.stride(1) != 1 or (t2.shape[0] > 1 and (t2.stride(0) % 8 or t2.stride(0) < width)) or t2.data_ptr() % 16:
+        t2 = t2.contiguous()
+    return t2
+
+
+def _ld(t2):
+    return t2.stride(0) if t2.shape[0] > 1 else 0
+
+
+class CompressedSwiGLUFunction(torch.autograd.Function):
+    """silu(gate) * up of the two halves of x [..., 2 f] (gate first); gate and up are kept as 8-bit checkpoints, half of
+    x's bytes in bfloat16, and the gradients are formed from those (acc_gated_fwd_act8 / acc_gated_bwd_act8)."""
+
+    @staticmethod
+    def forward(ctx, x, fmt: str = "int8"):
+        if x.dtype not in _CODES:
+            raise TypeError("x must be bfloat16 or float32")
+        if fmt not in _FORMATS:
+            raise ValueError("format must be 'e4m3' or 'int8'")
+        f = x.shape[-1] // 2
+        if x.shape[-1] != 2 * f:
+            raise ValueError("the last dimension holds gate and up: it must be even")
+        x2 = _rows(x, 2 * f)
+        n, dev = x2.shape[0], x.device
+        h = torch.empty(n, f, dtype=x.dtype, device=dev)
+        ctx.meta = (n, f, fmt, x.shape)
+        if n == 0:
+            return h.reshape(*x.shape[:-1], f)
+        desc = acc.make_gated_desc(n, f, ldg=x2.stride(0) if n > 1 else 2 * f, io_dtype=_CODES[x.dtype], format=_FORMATS[fmt])
+        kept = acc.alloc_gated_act8(desc, dev)
+        with torch.cuda.device(dev):
+            acc.acc_gated_fwd_act8(desc, x2[:, :f], x2[:, f:], h, *kept)
+        ctx.save_for_backward(*kept)
+        return h.reshape(*x.shape[:-1], f)
+
+    @staticmethod
+    def backward(ctx, dh):
+        n, f, fmt, shape = ctx.meta
+        dx = torch.empty(n, 2 * f, dtype=dh.dtype, device=dh.device)
+        if n:
+            dh2 = _rows(dh, f)
+            desc = acc.make_gated_desc(n, f, ldg=2 * f, ldh=_ld(dh2), io_dtype=_CODES[dh.dtype], format=_FORMATS[fmt])
+            with torch.cuda.device(dh.device):
+                acc.acc_gated_bwd_act8(desc, dh2, *ctx.saved_tensors, dx[:, :f], dx[:, f:])
+        return dx.reshape(shape), None
+
+
+class CompressedSwiGLU(torch.nn.Module):
+    """The gated activation of an MLP whose gate and up projections are one linear: [..., 2 f] -> [..., f]."""
+
+    def __init__(self, format: str = "int8"):
+        super().__init__()
+        if format not in _FORMATS:
+            raise ValueError("format must be 'e4m3' or 'int8'")
+        self.format = format
+
+    def forward(self, x):
+        return CompressedSwiGLUFunction.apply(x, self.format)
+
+    def extra_repr(self):
+        return f"format={self.format}"
+
+
+class LinearCrossEntropyFunction(torch.autograd.Function):
+    """Per-token softmax cross entropy (float32) of x @ weight.T against `target`, weight [vocabulary, features], without the
+    logits (acc_linear_ce_fwd / acc_linear_ce_bwd).  Kept for the backward pass: x, weight, target and two floats a token.
+    Negative targets have no loss and no gradient."""
+
+    @staticmethod
+    def forward(ctx, x, weight, target):
+        if x.dtype not in _CODES or weight.dtype != x.dtype:
+            raise TypeError("x and weight must both be bfloat16 or both float32")
+        if target.dtype != torch.int64 or target.shape != x.shape[:-1]:
+            raise TypeError("target must be int64, one per token")
+        if not (x.device == weight.device == target.device):
+            raise ValueError("x, weight and target must be on one device")
+        v, d = weight.shape
+        x2, w, t = _rows(x, d), _rows(weight, d), target.reshape(-1).contiguous()
+        n, dev = x2.shape[0], x.device
+        loss = torch.empty(n, dtype=torch.float32, device=dev)
+        ctx.meta = (n, d, v, x.shape)
+        if n == 0:
+            ctx.save_for_backward(w)
+            return loss.reshape(target.shape)
+        stats = torch.empty(2, n, dtype=torch.float32, device=dev)
+        desc = LinearCrossEntropyFunction._desc(ctx, x2, w)
+        with torch.cuda.device(dev):
+            acc.acc_linear_ce_fwd(desc, x2, w, t, loss, stats, _workspace(acc.acc_linear_ce_workspace_bytes(desc, False), dev))
+        ctx.save_for_backward(w, x2, t, stats)
+        return loss.reshape(target.shape)
+
+    @staticmethod
+    def _desc(ctx, x2, w):
+        n, d, v, _ = ctx.meta
+        return acc.make_ce_desc(n, d, v, ldx=_ld(x2), ldw=_ld(w), io_dtype=_CODES[w.dtype])
+
+    @staticmethod
+    def backward(ctx, dloss):
+        n, d, v, shape = ctx.meta
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        w, dev = ctx.saved_tensors[0], dloss.device
+        if n == 0 or not (want_dx or want_dw):
+            return (torch.empty(shape, dtype=w.dtype, device=dev) if want_dx else None,
+                    torch.zeros(v, d, dtype=w.dtype, device=dev) if want_dw else None, None)
+        _, x2, t, stats = ctx.saved_tensors
+        desc = LinearCrossEntropyFunction._desc(ctx, x2, w)
+        g = dloss.reshape(-1).to(torch.float32).contiguous()
+        ldx = x2.stride(0) if n > 1 else d
+        dx = torch.empty(n, ldx, dtype=w.dtype, device=dev)[:, :d] if want_dx else None   # rows as far apart as x's
+        dw = torch.empty(v, d, dtype=w.dtype, device=dev) if want_dw else None
+        with torch.cuda.device(dev):
+            acc.acc_linear_ce_bwd(desc, x2, w, t, stats, g, dx, dw, _workspace(acc.acc_linear_ce_workspace_bytes(desc, True), dev))
+        return None if dx is None else dx.reshape(shape), dw, None
+
+
+class LinearCrossEntropy(torch.nn.Module):
+    """The last product of a language model with its loss: torch.nn.Linear(features, vocabulary, bias=False) followed by
+    torch.nn.functional.cross_entropy, without the logits.  `weight` may be tied to an embedding table's.
+
+    reduction "mean" (over the tokens whose target is not ignore_index), "sum" or "none"."""
+
+    def __init__(self, in_features: int, vocabulary: int, ignore_index: int = -100, reduction: str = "mean", device=None,
+                 dtype=torch.bfloat16):
+        super().__init__()
+        if reduction not in ("mean", "sum", "none"):
+            raise ValueError("reduction must be 'mean', 'sum' or 'none'")
+        self.ignore_index, self.reduction = ignore_index, reduction
+        self.weight = torch.nn.Parameter(torch.empty(vocabulary, in_features, device=device, dtype=dtype))
+        torch.nn.init.normal_(self.weight, std=0.02)
+
+    def forward(self, x, target):
+        if self.ignore_index >= 0:
+            target = torch.where(target == self.ignore_index, -1, target)
+        loss = LinearCrossEntropyFunction.apply(x, self.weight, target)
+        if self.reduction == "none":
+            return loss
+        total = loss.sum()
+        return total if self.reduction == "sum" else total / (target >= 0).sum()
+
+    def extra_repr(self):
+        return f"in_features={self.weight.shape[1]}, vocabulary={self.weight.shape[0]}, reduction={self.reduction}"
 
 
 class LowRankAdamW:
