@@ -154,6 +154,34 @@ static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64
   return best;
 }
 
+// Tile of the products that form the cross entropy's logits, by an estimate like pick_gemm_tile's; a tile's cost holds its exponentials,
+// which the persistent kernel does between two tiles and two work-groups of a compute unit behind each other's products.
+enum class CeTile { k64x128, k128, k192x128, k256 };
+struct CeChoice {
+  CeTile tile;
+  bool one_round;
+};
+static inline CeChoice pick_ce_tile(int64_t M, int64_t N, int64_t K) {
+  struct Cost { CeTile tile; int bm, bn, launch, per_tile, per_k, alone_per_tile, alone_per_k; };
+  static const Cost costs[] = {{CeTile::k64x128, 64, 128, 3000, 2000, 280, 2500, 260},
+                               {CeTile::k128, 128, 128, 3000, 3000, 460, 4500, 370},
+                               {CeTile::k192x128, 192, 128, 3000, 3200, 580, 5500, 500},
+                               {CeTile::k256, 256, 256, 5000, 6000, 1330, 6000, 1330}};
+  const int64_t kt = ceil_div(K, 64);
+  CeChoice best{CeTile::k64x128, true};
+  int64_t best_ns = INT64_MAX;
+  for (const Cost& c : costs) {
+    if (c.tile == CeTile::k256 && K <= 128) continue;   // the persistent kernel takes three K tiles
+    const int64_t rounds = ceil_div(ceil_div(M, c.bm) * ceil_div(N, c.bn), 256);
+    const int64_t ns = c.launch + rounds * (rounds == 1 ? c.alone_per_tile : c.per_tile) + kt * (rounds == 1 ? c.alone_per_k : rounds * c.per_k);
+    if (ns < best_ns) {
+      best_ns = ns;
+      best = CeChoice{c.tile, rounds == 1};
+    }
+  }
+  return best;
+}
+
 // Token splits of the sketch contraction: enough work-groups to fill 256 CUs, at most 32 partials.
 static inline int generic_sketch_splits(int64_t n, int64_t c, int64_t r) {
   const int64_t tiles = ceil_div(c, 64) * ceil_div(r, 64);

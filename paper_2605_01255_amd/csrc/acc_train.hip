@@ -169,21 +169,13 @@ int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
 // ---- the vocabulary's cross entropy --------------------------------------------------------------------
 constexpr int64_t kCePieceBytes = (int64_t)512 << 20;
 
-// Tile of the products that form the logits: 64 x 128 for few tokens, where W is read once whatever the tile, 128 x 128 up to a full
-// 256 x 256 tile's rows, then 256 x 256.  Its waves' strips of columns are 64 or 128 wide.
-enum class CeTile { k64x128, k128, k256 };
-CeTile ce_tile(int64_t n, int64_t d) {
-  if (n <= 64) return CeTile::k64x128;
-  return n <= 128 || d <= 128 ? CeTile::k128 : CeTile::k256;   // the persistent kernel takes three K tiles at least
-}
-int64_t ce_strip(int64_t n, int64_t d) { return ce_tile(n, d) == CeTile::k256 ? 128 : 64; }
-
 struct CePlan {
   int64_t n, d, v, ldx, ldw;
   int64_t run;      // tokens of a run
   int64_t rows;     // of the dense matrices: a run, and 256 at least
   int64_t vp, ldz;  // columns of a piece, their row stride
-  int64_t strips;   // of the whole vocabulary
+  CeChoice sums;    // tile of the forward product
+  int64_t strips;   // its waves' strips of columns, 128 wide on the persistent kernel, else 64
   SplitChoice dx_choice;   // of dX's sum over a piece
   int least_rows;
   size_t order, count, unit, targets, per_row, x, part, z, dx;   // offsets into the workspace
@@ -231,7 +223,8 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (vp > p->v) vp = p->v;
   p->vp = vp;
   p->ldz = round_up(vp, 64);   // whole cache lines: rows that begin inside one cost the product with W twice the requests
-  p->strips = ceil_div(p->v, ce_strip(p->run, p->d));
+  p->sums = pick_ce_tile(p->run, p->v, p->d);
+  p->strips = ceil_div(p->v, p->sums.tile == CeTile::k256 ? 128 : 64);
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t from = at;
@@ -315,15 +308,20 @@ template <Epilogue EPI> void ce_product(const CeRun& r, const void* X, const voi
                 (f32x2*)(r.ws + r.p.part), X ? r.n : r.p.rows, v0};
   p.least_rows = r.p.least_rows;
   if (EPI == Epilogue::kGradient && p.M < p.least_rows) p.M = p.least_rows;   // for the grid
-  auto ring = [&](auto tm, auto tn) {
-    constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = 3;
+  auto ring = [&](auto tm, auto tn, auto ns) {
+    constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
     const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
     L.launch_lds(gemm_ring_kernel<TM, TN, NS, true, bf16, kNone, false, true, EPI, true>, dim3(grid), dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
   };
   using std::integral_constant;
-  switch (ce_tile(r.p.run, r.p.d)) {
-    case CeTile::k64x128: return ring(integral_constant<int, 2>{}, integral_constant<int, 4>{});
-    case CeTile::k128: return ring(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  const integral_constant<int, 2> two{};
+  const integral_constant<int, 3> three{};
+  const integral_constant<int, 4> four{};
+  const CeChoice c = EPI == Epilogue::kExpSums ? r.p.sums : pick_ce_tile(r.p.run, r.p.vp, r.p.d);
+  switch (c.tile) {
+    case CeTile::k64x128: return ring(two, four, three);
+    case CeTile::k128: return c.one_round ? ring(four, four, three) : ring(four, four, two);
+    case CeTile::k192x128: return ring(integral_constant<int, 6>{}, four, two);
     case CeTile::k256: break;
   }
   gemm_ring_plan(p, 256, 256);
