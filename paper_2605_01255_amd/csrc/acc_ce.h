@@ -257,24 +257,47 @@ __global__ __launch_bounds__(256) void ce_finish_kernel(CeTokens t, const f32x2*
   stats[stats_stride + i] = zt;
 }
 
-// dX [n, ldx] from the dense rows, the sum of `splits` matrices times *unit; tokens without a loss get zeros.  One work-group per row of
-// the list.
-template <typename T>
-__global__ __launch_bounds__(256) void ce_scatter_kernel(CeTokens t, const float* __restrict__ dXf, int splits, int64_t split_stride,
-                                                         const float* __restrict__ unit, int d, T* __restrict__ dX, int64_t ldx) {
+// A dense matrix [rows, d] as the sum of the parts of a product, `stride` apart, and of what there was before (null: nothing).
+struct CeParts {
+  const float* parts;
+  int splits;
+  int64_t stride;
+  const float* before;
+  __device__ __forceinline__ f32x4 at(int64_t e) const {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (before) v = *(const f32x4*)(before + e);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) v += *(const f32x4*)(parts + k * stride + e);
+    return v;
+  }
+};
+
+// The sum between two pieces, for the rows with a token.  One work-group per row.
+__global__ __launch_bounds__(256) void ce_add_kernel(CeTokens t, CeParts sum, int d, float* dXf) {
   const int64_t r = blockIdx.x;
-  const bool lives = r < *t.count;
-  const int i = t.order[r];
+  if (!t.lives(r)) return;
+  for (int c = (int)threadIdx.x * 4; c < d; c += 1024) *(f32x4*)(dXf + r * d + c) = sum.at(r * d + c);
+}
+
+// dX [n, ldx] from the dense rows times *unit; tokens without a loss get zeros.  One work-group per row of the list.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_scatter_kernel(CeTokens t, CeParts sum, const float* __restrict__ unit, int d, T* __restrict__ dX, int64_t ldx) {
+  const int64_t r = blockIdx.x;
+  const bool lives = t.lives(r);
+  const int i = t.token(r);
+  const float scale = unit ? *unit : 1.f;
   for (int c = (int)threadIdx.x * 4; c < d; c += 1024) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (lives) {
-#pragma unroll 4
-      for (int k = 0; k < splits; ++k) v += *(const f32x4*)(dXf + k * split_stride + r * d + c);
-      if (unit) v *= *unit;
-    }
+    if (lives) v = sum.at(r * d + c) * scale;
     T* dst = dX + (int64_t)i * ldx + c;
+    if constexpr (sizeof(T) == 2) {
+      bf16x4 o;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) dst[k] = from_f32<T>(v[k]);
+      for (int k = 0; k < 4; ++k) o[k] = (bf16)v[k];
+      *(bf16x4*)dst = o;
+    } else {
+      *(f32x4*)dst = v;
+    }
   }
 }
 

@@ -80,6 +80,10 @@ __device__ __forceinline__ int swz_n16(int krow) { return ((krow & 3) << 2) | ((
 // tile's transfers under way (at 64 K tiles 4 % of a tile).  kGradient: the elements change as they are staged, in the slots of the
 // matrix instructions of the block row after.  Either takes its rows from a device count and its tiles from ring_tile's order, which
 // leaves no work-group without a tile for as long as there are some, however many rows there are.
+// kParts: C is float, and what a work-group walks over are pairs of a tile and a part of the K range (k_per_split columns, three K tiles
+// at least, the last part what is left): part s is stored at C + s c_split_stride, from the accumulators as they are (64 bytes of a row
+// at a time; staged as float they would need LDS that the stages have).  Chunks past the part's end are sent out of range in whichever
+// K tile they lie.  Against the ring kernel's 128 x 128 tiles, us: 1024 x 4096 by 128000 columns 906 / 1780, 2048 x 2048 by 50257 409 / 661.
 template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore, int N1 = 12, int S1 = 4, int S0 = 4>
 __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, int n_slots) {
   // schedule of k-step 1: the barrier sits before its slot BAR_Q; N1 wave-loads go out after it, one every S1
@@ -96,14 +100,18 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   constexpr int REGION = 16 * 256;  // one staged block row: 16 rows x 128 bf16
   static_assert(NG == 16, "the slot program places sixteen wave-loads per K tile");
 
-  constexpr bool CE = EPI != Epilogue::kStore;
+  constexpr bool CE = EPI != Epilogue::kStore, PARTS = EPI == Epilogue::kParts;
+  static_assert(!PARTS || (RAGGED_K && A_KMAJOR && !B_KMAJOR), "the order of operands that parts are written for");
+  int part_slots = 0;
   if constexpr (CE) {
     take_live_rows<EPI>(p, BM);
-    n_slots = ((p.tiles_m * p.tiles_n + 7) >> 3) * 8;
+    n_slots = part_slots = ((p.tiles_m * p.tiles_n + 7) >> 3) * 8;
+    if constexpr (PARTS) n_slots *= (int)((p.K + p.k_per_split - 1) / p.k_per_split);
   }
   if constexpr (!A_KMAJOR) take_live_tokens(p);
   auto find_tile = [&](int b, int& tm, int& tn) -> bool {
-    if constexpr (CE) return ring_tile(p, b, tm, tn);
+    if constexpr (PARTS) return part_slots && ring_tile(p, b % part_slots, tm, tn);
+    else if constexpr (CE) return ring_tile(p, b, tm, tn);
     else return xcd_tile(p, b, tm, tn);
   };
 
@@ -111,7 +119,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int KT = RAGGED_K ? (int)((p.K + BK - 1) / BK) : (int)(p.K / BK);
+  const int KT = PARTS ? (int)(p.k_per_split / BK) : RAGGED_K ? (int)((p.K + BK - 1) / BK) : (int)(p.K / BK);
 
   // ---- global -> LDS sources (relative to a tile's buffer resources) ----
   uint32_t a_src[A_LOADS], b_src[B_LOADS];
@@ -138,7 +146,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   }
   // this lane's chunk of the last K tile lies past K (rows a multiple of 32 apart share their swizzle)
   const uint32_t tail = RAGGED_K && (((lane & 7) ^ swz(wave * 8 + (lane >> 3))) * 8 >= p.K - (int64_t)(KT - 1) * BK) ? 0xFFFFFFF0u : 0u;
-  auto past_k = [&](int kt) -> uint32_t { return RAGGED_K && kt == KT - 1 ? tail : 0u; };
+  const int chunk_k = ((lane & 7) ^ swz(wave * 8 + (lane >> 3))) * 8;   // this lane's first k in a K tile
   const uint32_t a_kstep = A_KMAJOR ? BK * 2 : (uint32_t)(BK * p.lda * 2);
   const uint32_t b_kstep = B_KMAJOR ? BK * 2 : (uint32_t)(BK * p.ldb * 2);
   const uint32_t smem_lds = (uint32_t)(uintptr_t)smem;
@@ -146,6 +154,11 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   struct TileRef {
     u32x4 a_rsrc, b_rsrc;
     int64_t m0, n0;
+    int part, kn;   // of the K range, and its columns (kParts)
+  };
+  auto past_k = [&](const TileRef& r, int kt) -> uint32_t {
+    if constexpr (PARTS) return kt * BK + chunk_k >= r.kn ? 0xFFFFFFF0u : 0u;
+    else return RAGGED_K && kt == KT - 1 ? tail : 0u;
   };
   auto tile_ref = [&](int idx) -> TileRef {
     int tm = 0, tn = 0;
@@ -153,6 +166,14 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     TileRef r;
     r.m0 = (int64_t)tm * BM;
     r.n0 = (int64_t)tn * BN;
+    if constexpr (PARTS) {
+      r.part = part_slots ? idx / part_slots : 0;
+      const int64_t k0 = r.part * p.k_per_split, rows = (p.kb_rows < k0 + p.k_per_split ? p.kb_rows : k0 + p.k_per_split) - k0;
+      r.kn = (int)(p.K - k0 < p.k_per_split ? p.K - k0 : p.k_per_split);
+      r.a_rsrc = make_rsrc(p.A + r.m0 * p.lda + k0, ((p.M - r.m0 - 1) * p.lda + r.kn) * 2);
+      r.b_rsrc = make_rsrc(p.B + k0 * p.ldb + r.n0, rows > 0 ? ((rows - 1) * p.ldb + (p.N - r.n0)) * 2 : 0);
+      return r;
+    }
     r.a_rsrc = A_KMAJOR ? make_rsrc(p.A + r.m0 * p.lda, ((p.M - r.m0 - 1) * p.lda + p.K) * 2)
                         : make_rsrc(p.A + r.m0, ((p.K - 1) * p.lda + ((p.M - r.m0 + 7) & ~(int64_t)7)) * 2);
     r.b_rsrc = B_KMAJOR ? make_rsrc(p.B + r.n0 * p.ldb, ((p.N - r.n0 - 1) * p.ldb + p.K) * 2)
@@ -160,7 +181,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     return r;
   };
   auto issue_one = [&](const TileRef& r, int g, int kt, uint32_t stage) {
-    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, a_src[g], (uint32_t)kt * a_kstep, stage + (g * NW + wave) * 1024);
+    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, PARTS ? a_src[g] | past_k(r, kt) : a_src[g], (uint32_t)kt * a_kstep, stage + (g * NW + wave) * 1024);
     else buffer_to_lds_b128(r.b_rsrc, b_src[g - A_LOADS], (uint32_t)kt * b_kstep,
                             stage + A_BYTES + ((g - A_LOADS) * NW + wave) * 1024);
   };
@@ -252,16 +273,29 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   };
   __amdgpu_buffer_rsrc_t c_rs = __builtin_amdgcn_make_buffer_rsrc((void*)C, 0, 0, 0x00020000);  // empty: nothing to store yet
   uint32_t c_voff = 0xFFFFFFF0u;
+  int left = 0;   // kParts: columns from this lane's first one to N
   auto set_output = [&](const TileRef& t) {
     const int64_t gm_base = t.m0 + wm * TB * 16, gn_base = t.n0 + wn * TB * 16;
     int64_t c_rows = p.M - gm_base;
     if (c_rows > TB * 16) c_rows = TB * 16;
+    if constexpr (PARTS) {
+      float* const base = (float*)p.C + t.part * p.c_split_stride + gm_base * p.ldc + gn_base;
+      const int64_t bytes = (c_rows > 0 && gn_base < p.N) ? ((c_rows - 1) * p.ldc + (p.N - gn_base)) * 4 : 0;
+      c_rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(uint32_t)bytes, 0x00020000);
+      c_voff = (uint32_t)((l16 * p.ldc + 4 * g4) * 4);
+      left = (int)(p.N - gn_base < BN ? p.N - gn_base : BN) - 4 * g4;
+      return;
+    }
     const int64_t c_bytes = (c_rows > 0 && gn_base < p.N) ? ((c_rows - 1) * p.ldc + (CE ? (p.N - gn_base + 7) & ~(int64_t)7 : p.N - gn_base)) * 2 : 0;
     c_rs = __builtin_amdgcn_make_buffer_rsrc((void*)(C + gm_base * p.ldc + gn_base), 0, (int)(uint32_t)c_bytes,
                                              0x00020000);
     c_voff = gn_base + l16 * 8 < p.N ? (uint32_t)((g4 * p.ldc + l16 * 8) * 2) : 0xFFFFFFF0u;  // columns past N: dropped
   };
   f32x4 acc[TB][TB];
+  auto store_block = [&](int i, int j) {   // kParts: straight from the accumulators
+    const uint32_t soff = (uint32_t)((i * 16 * p.ldc + j * 16) * 4);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), c_rs, j * 16 < left ? c_voff : 0xFFFFFFF0u, soff, 0);
+  };
   // of this lane's row in each block row, requested before an output tile's last K tile
   CeRow ce[EPI == Epilogue::kGradient ? TB : 1];
   int target[TB];
@@ -311,7 +345,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     const char* cur = smem + sc * STAGE;
     const char* nxt = smem + (sc ^ 1) * STAGE;
     const uint32_t cur_lds = smem_lds + sc * STAGE, nxt_lds = smem_lds + (sc ^ 1) * STAGE;
-    const uint32_t oob1 = past_k(k1), oob2 = past_k(k2);
+    const uint32_t oob1 = past_k(ref1, k1), oob2 = past_k(ref2, k2);
     __builtin_amdgcn_sched_barrier(0);
     static_for<0, 64>([&](auto slot) {  // k-step 0
       constexpr int q = decltype(slot)::value;
@@ -327,7 +361,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
       if (q >= 2 && (q - 2) % S0 == 0 && (q - 2) / S0 < NG - N1) issue_at_m0(ref1, N1 + (q - 2) / S0, k1, oob1);
       if (j == 0 && i >= 1) a[i - 1] = read_a(cur, 1, i - 1);
       if (j == 4) b1[i] = read_b(cur, 1, i);
-      if (CARRY && EPI != Epilogue::kExpSums && q < 16) carry_slot(q);
+      if (CARRY && EPI != Epilogue::kExpSums && !PARTS && q < 16) carry_slot(q);
       if (q >= 1 && (q - 1) % S0 == 0 && (q - 1) / S0 < NG - N1) set_m0(N1 + (q - 1) / S0, nxt_lds + wave * 1024);
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -361,7 +395,10 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
         if (q >= BAR_Q + 1 && (q - BAR_Q - 1) % SP == 0 && (q - BAR_Q - 1) / SP < 8)
           b0[(q - BAR_Q - 1) / SP] = read_b(nxt, 0, (q - BAR_Q - 1) / SP);
       }
-      if constexpr (FINAL && EPI != Epilogue::kExpSums) {
+      if constexpr (FINAL && PARTS) {
+        if (i >= 1) store_block(i - 1, j);
+      }
+      if constexpr (FINAL && EPI != Epilogue::kExpSums && !PARTS) {
         if (i >= 2 && j == 0) wave_fence();
         if (i >= 1) stage_write(i - 1, j);
         if (i >= 2 && j < 4) back[j] = read_back(i - 2, j);
@@ -371,7 +408,10 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
         set_m0((q - BAR_Q - 1) / S1, cur_lds + wave * 1024);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (FINAL && EPI != Epilogue::kExpSums) {
+    if constexpr (FINAL && PARTS) {
+      static_for<0, TB>([&](auto col) { store_block(TB - 1, decltype(col)::value); });
+    }
+    if constexpr (FINAL && EPI != Epilogue::kExpSums && !PARTS) {
       static_for<0, TB>([&](auto col) { stage_write(TB - 1, decltype(col)::value); });
     }
   };
@@ -421,7 +461,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     idx = next_idx;
   }
   // no tile follows: block rows 6 and 7 are read out here
-  if constexpr (EPI != Epilogue::kExpSums) {
+  if constexpr (EPI != Epilogue::kExpSums && !PARTS) {
 #pragma unroll
     for (int q = 0; q < 16; ++q) carry_slot(q);
   }

@@ -6,7 +6,7 @@
 
 namespace acc {
 
-enum class Epilogue { kStore, kExpSums, kGradient };
+enum class Epilogue { kStore, kExpSums, kGradient, kParts };
 
 constexpr float kLog2e = 1.44269504088896341f;
 template <Epilogue EPI> __device__ __forceinline__ void take_live_rows(FastGemmParams& p, int bm) {

@@ -107,7 +107,8 @@ static inline FactorTile pick_factor_tile(int64_t M, int64_t N, int64_t K, bool 
 // Products whose K range may be taken in parts that a later kernel adds up: products over the tokens (a long K and, at small layers, few
 // tiles) and the input gradient of the cross entropy (the vocabulary is its K).  The least of estimates like pick_gemm_tile's, with tiles
 // x parts in the place of tiles, and for more than one part the launch that adds them up and their bytes, written and read at 4 TB/s.
-// A part has four K tiles at least.
+// A part has four K tiles at least.  Two operands that stay in no cache come through the L2s at 9.5 TB/s, which is what the smaller tiles
+// of the input gradient wait for (1024 x 4096 by 128000 columns on 128 x 128, 16.8 GB: 1780 us; on the persistent kernel 906).
 // over_tokens: both operands are read transposed, at half the rate from LDS, which the smaller wave tiles wait for (2048 x 2048 over
 // 32768 tokens on 128 x 128, one work-group per compute unit: 0.63 us a K tile, where a K-contiguous operand takes 0.37; two work-groups
 // cover each other's: 297 us in four parts, 323 in one).  Measured us there on 256 x 256 / 192 x 128 / 128 x 128 / 128 x 64 / 64 x 64
@@ -121,7 +122,7 @@ struct SplitChoice {
   int64_t splits, k_per_split;
   int64_t ns;            // the estimate
 };
-static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits, bool over_tokens = false, bool persist_ok = false) {
+static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits, bool over_tokens, bool persist_ok) {
   struct Cost { GemmTile tile; int bm, bn, per_tile, per_k, alone_per_tile, alone_per_k; };
   static const Cost contiguous[] = {{GemmTile::k192x128, 192, 128, 1700, 580, 3500, 500},
                                     {GemmTile::k128, 128, 128, 2000, 460, 3000, 370},
@@ -133,6 +134,7 @@ static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64
                                     {GemmTile::k64, 64, 64, 560, 185, 500, 220}};
   SplitChoice best{GemmTile::k64, true, 1, round_up(K, 64), INT64_MAX};
   const int64_t kt = ceil_div(K, 64);
+  const bool streams = !over_tokens && M * K * 2 > (int64_t)96 << 20 && N * K * 2 > (int64_t)32 << 20;
   for (int c = 0; c < 4; ++c) {
     const Cost& cost = over_tokens ? transposed[c] : contiguous[c];
     const int64_t tiles = ceil_div(M, cost.bm) * ceil_div(N, cost.bn);
@@ -142,12 +144,25 @@ static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64
       int64_t per_k = rounds == 1 ? cost.alone_per_k : rounds * cost.per_k;
       if (!over_tokens && cost.tile == GemmTile::k64 && rounds == 2) per_k = 300;   // as in pick_gemm_tile
       int64_t ns = 3000 + rounds * (rounds == 1 ? cost.alone_per_tile : cost.per_tile) + part * per_k;
+      const int64_t moved = tiles * kt * (cost.bm + cost.bn) * 128 / 9500;   // bytes through L2, in ns
+      if (streams && ns < moved) ns = moved;
       if (splits > 1) ns += 4000 + splits * M * N / 500;
       if (ns < best.ns) best = SplitChoice{cost.tile, rounds == 1, splits, part * 64, ns};
       if (rounds > 16) break;
     }
   }
-  if (persist_ok) {   // the persistent kernel, whole; a short K does not cover its tile's write
+  if (persist_ok && !over_tokens && kt >= 3) {   // the persistent kernel's parts; M is the most rows there may be, so half a round is lost
+    const int64_t tiles = ceil_div(M, 256) * ceil_div(N, 256);
+    for (int64_t want = 1; want <= most_splits && 3 * want <= kt; want = want < 8 ? want + 1 : want + want / 4) {
+      const int64_t part = ceil_div(kt, want), splits = ceil_div(kt, part), unit = 4000 + part * 1340;
+      if (splits != want || part < 3) continue;
+      int64_t ns = 5000 + tiles * splits * unit / 256 + unit / 2;
+      if (ns < 5000 + unit) ns = 5000 + unit;
+      if (splits > 1) ns += 4000 + splits * M * N / 500;
+      if (ns < best.ns) best = SplitChoice{GemmTile::k256, tiles * splits <= 256, splits, part * 64, ns};
+    }
+  }
+  if (persist_ok && over_tokens) {   // the persistent kernel, whole; a short K does not cover its tile's write
     const int64_t rounds = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256), ns = 5000 + rounds * ((kt < 16 ? 5000 : 2000) + kt * 1340);
     if (ns < best.ns) best = SplitChoice{GemmTile::k256, rounds == 1, 1, round_up(K, 64), ns};
   }

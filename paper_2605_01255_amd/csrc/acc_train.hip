@@ -167,7 +167,7 @@ int validate_gated(const acc_gated_desc* d, int64_t* ldg, int64_t* ldh) {
 }
 
 // ---- the vocabulary's cross entropy --------------------------------------------------------------------
-constexpr int64_t kCePieceBytes = (int64_t)512 << 20;
+constexpr int64_t kCePieceBytes = (int64_t)1 << 30;
 
 struct CePlan {
   int64_t n, d, v, ldx, ldw;
@@ -178,14 +178,14 @@ struct CePlan {
   int64_t strips;   // its waves' strips of columns, 128 wide on the persistent kernel, else 64
   SplitChoice dx_choice;   // of dX's sum over a piece
   int least_rows;
-  size_t order, count, unit, targets, per_row, x, part, z, dx;   // offsets into the workspace
+  size_t order, count, unit, targets, per_row, x, part, z, parts, dx;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
 
 // dX [n, d] is a sum over the whole piece: where its tiles leave compute units idle the sum is taken in parts, which the last kernel adds
 // up (pick_split_gemm; in float32 parts enough for two 64 x 64 tiles to a compute unit, of 512 columns at least).
 void plan_ce_dx(CePlan* p, bool b16) {
-  p->dx_choice = pick_split_gemm(p->run, p->d, p->vp, 64);
+  p->dx_choice = pick_split_gemm(p->run, p->d, p->vp, 32, false, true);
   if (!b16) {
     int64_t splits = 512 / (ceil_div(p->run, 64) * ceil_div(p->d, 64));
     if (splits > p->vp / 512) splits = p->vp / 512;
@@ -249,7 +249,8 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   at = shared;   // backward: dz, then dX in float
   take(p->rows * p->ldz * es);
   plan_ce_dx(p, d->io_dtype == ACC_BF16);
-  p->dx = take(p->dx_choice.splits * p->rows * p->d * 4);
+  p->parts = take(p->dx_choice.splits * p->rows * p->d * 4);
+  p->dx = take(p->vp < p->v ? p->rows * p->d * 4 : 0);
   p->backward = at > p->forward ? at : p->forward;
   return ACC_OK;
 }
@@ -330,20 +331,36 @@ template <Epilogue EPI> void ce_product(const CeRun& r, const void* X, const voi
   else L.launch_lds(gemm16_persist_kernel<true, false, true, EPI>, dim3(256), dim3(256), (size_t)160 * 1024, p, 0);
 }
 
-// dX (float, in its parts) (+)= dz . W_piece for the rows with a token.
-template <bool SUM> void ce_input_gradient(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
-  FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), r.ws + r.p.dx, r.n, r.p.d, round_up(r.piece(v0), 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 1.f);
-  p.kb_rows = r.piece(v0);
+// The parts (float) of dz . W_piece for the rows with a token; their number.
+int ce_input_gradient(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
+  const int64_t vp = r.piece(v0), stride = r.p.rows * r.p.d;
+  const SplitChoice& c = r.p.dx_choice;
+  const int splits = (int)ceil_div(vp, c.k_per_split);
+  float* parts = (float*)(r.ws + r.p.parts);
+  if (r.desc->io_dtype != ACC_BF16) {
+    f32_split_product(F32Operand{r.ws + r.p.z, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, parts, r.p.d, r.n, r.p.d, vp,
+                      false, c.k_per_split, stride, L);
+    return splits;
+  }
+  FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), parts, r.n, r.p.d, round_up(vp, 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 0.f);
+  p.kb_rows = vp;
   p.live = r.tokens.count;
-  p.k_per_split = r.p.dx_choice.k_per_split;
-  p.c_split_stride = r.p.rows * r.p.d;
-  with_ring_tile(r.p.dx_choice.tile, false, [&](auto tm, auto tn, auto ns) {
+  p.k_per_split = c.k_per_split;
+  p.c_split_stride = stride;
+  if (c.tile == GemmTile::k256) {
+    gemm_ring_plan(p, 256, 256);
+    if (p.super_m > 8) p.super_m = 8;
+    L.launch_lds(gemm16_persist_kernel<false, true, true, Epilogue::kParts>, dim3(256), dim3(256), (size_t)160 * 1024, p, 0);
+    return splits;
+  }
+  with_ring_tile(c.tile, false, [&](auto tm, auto tn, auto ns) {
     constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
     const unsigned grid = gemm_ring_plan(p, 32 * TM, 32 * TN);
     p.tile_blocks = (int)grid;
-    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, kPlain, SUM, true, Epilogue::kStore, true>, dim3(grid * (unsigned)ceil_div(p.K, p.k_per_split)),
-                 dim3(256), (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
+    L.launch_lds(gemm_ring_kernel<TM, TN, NS, false, float, kPlain, false, true, Epilogue::kStore, true>, dim3(grid * (unsigned)splits), dim3(256),
+                 (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
   });
+  return splits;
 }
 
 }  // namespace
@@ -539,10 +556,12 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
         L(ce_piece_grad_kernel, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (float*)dz, r.p.ldz, v0, (int)vp, r.p.rows, (const int64_t*)(r.ws + r.p.targets), (const float*)per_row);
       }
       if (dX) {
-        if (!b16) f32_split_product(F32Operand{dz, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, dxf, r.p.d, r.n, r.p.d, vp,
-                                    v0 > 0, r.p.dx_choice.k_per_split, r.p.rows * r.p.d, L);
-        else if (v0) ce_input_gradient<true>(r, W, v0, L);
-        else ce_input_gradient<false>(r, W, v0, L);
+        const int splits = ce_input_gradient(r, W, v0, L);
+        const CeParts sum{(const float*)(r.ws + r.p.parts), splits, r.p.rows * r.p.d, v0 > 0 ? dxf : nullptr};
+        const dim3 grid((unsigned)r.n);
+        if (v0 + vp < r.p.v) L(ce_add_kernel, grid, dim3(256), r.tokens, sum, (int)r.p.d, dxf);
+        else if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, sum, unit, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
+        else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, sum, unit, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
       }
       if (dW) {
         char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
@@ -550,13 +569,6 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
         token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 && r.n < r.p.least_rows ? r.p.least_rows : r.n, add,
                       L, nullptr, b16 ? r.tokens.count : nullptr, unit, r.p.least_rows);
       }
-    }
-    if (dX) {
-      const dim3 grid((unsigned)r.n);
-      const int splits = (int)r.p.dx_choice.splits;
-      const int64_t stride = r.p.rows * r.p.d;
-      if (b16) L(ce_scatter_kernel<bf16>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (bf16*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
-      else L(ce_scatter_kernel<float>, grid, dim3(256), r.tokens, (const float*)dxf, splits, stride, unit, (int)r.p.d, (float*)dX + (size_t)r.t0 * r.p.ldx, r.p.ldx);
     }
   });
 }
