@@ -91,9 +91,10 @@ F32GemmParams f32_params(const F32Operand& a, const F32Operand& b, void* C, int6
 template <typename TC>
 void f32_gemm(const F32Operand& a, const F32Operand& b, void* C, int64_t ldc, int64_t M, int64_t N, int64_t K, Launcher& L,
               bool accumulate = false, float alpha = 1.f, float beta = 1.f, int64_t k_per_split = 0,
-              int64_t c_split_stride = 0, int sum_tiles = 8, int64_t kb_rows = 0) {
+              int64_t c_split_stride = 0, int sum_tiles = 8, int64_t kb_rows = 0, const int* live = nullptr) {
   F32GemmParams p = f32_params(a, b, C, ldc, M, N, K);
   p.kb_rows = kb_rows;
+  p.live = live;
   p.accumulate = accumulate ? 1 : 0; p.alpha = alpha; p.beta = beta;
   if (k_per_split) p.k_per_split = k_per_split;
   p.c_split_stride = c_split_stride;
@@ -832,11 +833,11 @@ void exact_backward_gemm(const acc_linear_desc* desc, const Shape& s, const void
 }
 
 void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtype, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                 bool accumulate, Launcher& L, bool padded) {
-  if (padded && dtype == ACC_F32) {
-    const int64_t kp = a.kmajor ? round_up(K, 4) : K;
-    if (f32_gemm_ok(a, b, M, round_up(N, 4), kp, C, ldc)) {
-      f32_gemm<float>(a, b, C, ldc, M, N, kp, L, accumulate, 1.f, 1.f, 0, 0, 8, K);
+                 bool accumulate, Launcher& L, bool padded, const int* live) {
+  if ((padded || live) && dtype == ACC_F32) {
+    const int64_t kp = padded && a.kmajor ? round_up(K, 4) : K;
+    if (f32_gemm_ok(a, b, M, padded ? round_up(N, 4) : N, kp, C, ldc)) {
+      f32_gemm<float>(a, b, C, ldc, M, N, kp, L, accumulate, 1.f, 1.f, 0, 0, 8, K, live);
       return;
     }
   }
@@ -853,11 +854,11 @@ void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtyp
   else launch_generic<float, float, float, float, false, true>(p, 1, L);
 }
 
-void f32_split_product(const F32Operand& a, const F32Operand& b, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, bool accumulate,
-                       int64_t k_per_split, int64_t split_stride, Launcher& L) {
+void f32_split_product(const F32Operand& a, const F32Operand& b, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, int64_t k_per_split,
+                       int64_t split_stride, const int* live, Launcher& L) {
   const int64_t kp = a.kmajor ? round_up(K, 4) : K;
   if (f32_gemm_ok(a, b, M, round_up(N, 4), kp, C, ldc))
-    f32_gemm<float>(a, b, C, ldc, M, N, kp, L, accumulate, 1.f, 1.f, k_per_split, split_stride, 8, K);
+    f32_gemm<float>(a, b, C, ldc, M, N, kp, L, false, 1.f, 1.f, k_per_split, split_stride, 8, K, live);
   else L.err = hipErrorInvalidValue;   // operands that no caller has
 }
 

@@ -44,13 +44,22 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int kept = 0, turn = 0;   // kept: so far
   for (int first = 0; first < t.n; first += 1024 * PER, turn ^= 1) {
-    const int i0 = first + tid * PER;
+    const int i0 = first + tid * PER, last = t.n - 1;
+    int64_t target[PER];
+    float g[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) target[k] = t.targets[i0 + k < last ? i0 + k : last];
+    if (dloss) {
+#pragma unroll
+      for (int k = 0; k < PER; ++k) g[k] = dloss[i0 + k < last ? i0 + k : last];
+    }
     bool keep[PER];
     int mine = 0;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) keep[k] = t.targets[i0 + k < t.n ? i0 + k : t.n - 1] >= 0;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) mine += keep[k] && i0 + k < t.n ? 1 : 0;
+    for (int k = 0; k < PER; ++k) {
+      keep[k] = target[k] >= 0;
+      mine += keep[k] && i0 + k < t.n ? 1 : 0;
+    }
     int before = mine;   // inclusive scan over the wave
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -69,10 +78,7 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       if (i0 + k >= t.n) break;
-      if (dloss && keep[k]) {
-        const float g = fabsf(dloss[i0 + k]);
-        top = fmaxf(top, isfinite(g) ? g : 0.f);
-      }
+      if (dloss && keep[k] && isfinite(g[k])) top = fmaxf(top, fabsf(g[k]));
       if (keep[k]) t.order[at++] = i0 + k;
       else t.order[t.n - 1 - (i0 + k - at)] = i0 + k;
     }

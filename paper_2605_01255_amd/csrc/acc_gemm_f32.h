@@ -36,6 +36,7 @@ struct F32GemmParams {
   int64_t k_per_split;     // multiple of 32; split s writes its partial product at C + s * c_split_stride
   int64_t c_split_stride;
   int sum_tiles;           // K tiles of one running sum, a power of two
+  const int* live;         // device count of A's rows that take part (its K range, where A is given transposed); null: all
   int64_t kb_rows;         // N-contiguous B only: rows of B that exist (0 = K); K may exceed it when A is zero-padded along K
 };
 
@@ -276,6 +277,15 @@ __device__ __forceinline__ void gemm_f32_block(const F32GemmParams& p, const Out
 template <int TM, int TN, int NS, bool A_KMAJOR, bool B_KMAJOR, typename TA, typename TB, typename Output>
 __global__ __launch_bounds__(256) void gemm_f32_kernel(F32GemmParams p, Output output) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
+  if (p.live) {
+    const int rows = *p.live > 0 ? *p.live : 1;
+    if constexpr (A_KMAJOR) {
+      p.M = rows;
+      p.tiles_m = (rows + 32 * TM - 1) / (32 * TM);
+    } else {
+      p.K = rows;
+    }
+  }
   gemm_f32_block<TM, TN, NS, A_KMAJOR, B_KMAJOR, TA, TB>(p, output, (int)blockIdx.x, smem);
 }
 

@@ -68,11 +68,12 @@ __global__ __launch_bounds__(256) void gemm_ring_kernel(FastGemmParams p) {
   const int64_t k0 = SPLIT ? (int64_t)split * p.k_per_split : 0;
   const int64_t kn = SPLIT && k0 + p.k_per_split < p.K ? p.k_per_split : p.K - k0;   // this work-group's K range
   const int64_t kb = p.kb_rows && p.kb_rows < k0 + kn ? p.kb_rows - k0 : kn;  // rows of an N-contiguous B in it
-  const int KT = (int)((kn + BK - 1) / BK);
+  // A part behind the last token that takes part is a K tile of zeros.
+  const int KT = !A_KMAJOR && SPLIT && kn < 1 ? 1 : (int)((kn + BK - 1) / BK);
 
   // ---- global -> LDS: wave-load t of wave w fills LDS bytes [(t * NW + w) * 1024, +1024) of the operand tile ----
   const u32x4 a_rsrc = A_KMAJOR ? make_rsrc(p.A + m0 * p.lda + k0, ((p.M - m0 - 1) * p.lda + kn) * 2)
-                                : make_rsrc(p.A + k0 * p.lda + m0, ((kn - 1) * p.lda + ((p.M - m0 + 7) & ~(int64_t)7)) * 2);
+                                : make_rsrc(p.A + k0 * p.lda + m0, kn > 0 ? ((kn - 1) * p.lda + ((p.M - m0 + 7) & ~(int64_t)7)) * 2 : 0);
   const u32x4 b_rsrc = B_KMAJOR ? make_rsrc(p.B + n0 * p.ldb + k0, ((p.N - n0 - 1) * p.ldb + kn) * 2)
                                 : make_rsrc(p.B + k0 * p.ldb + n0, kb > 0 ? ((kb - 1) * p.ldb + (p.N - n0)) * 2 : 0);
   uint32_t a_src[A_LOADS], b_src[B_LOADS];

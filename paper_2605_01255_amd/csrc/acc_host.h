@@ -149,9 +149,10 @@ void exact_backward_gemm(const acc_linear_desc* desc, const Shape& s, const void
                          const ReduceJob* job = nullptr);
 // C[M, N] (+)= A . B for float32 operands of any order, C of `dtype`.  `padded`: rows of a K-contiguous A and of C may be read and
 // written up to a multiple of four, A's zeros behind K among them (any N and K then).  f32_split_product: the same with the K range in
-// runs of k_per_split (a multiple of 32), each into (or onto) a C of its own, split_stride apart.
+// runs of k_per_split (a multiple of 32), each into a C of its own, split_stride apart.  live: device count of A's rows that need to
+// take part (the K range, where A is transposed); those behind it hold what changes nothing, and may take part.
 void f32_product(const F32Operand& a, const F32Operand& b, void* C, int32_t dtype, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                 bool accumulate, Launcher& L, bool padded = false);
-void f32_split_product(const F32Operand& a, const F32Operand& b, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, bool accumulate,
-                       int64_t k_per_split, int64_t split_stride, Launcher& L);
+                 bool accumulate, Launcher& L, bool padded = false, const int* live = nullptr);
+void f32_split_product(const F32Operand& a, const F32Operand& b, float* C, int64_t ldc, int64_t M, int64_t N, int64_t K, int64_t k_per_split,
+                       int64_t split_stride, const int* live, Launcher& L);
 }  // namespace acc

@@ -113,8 +113,8 @@ void token_gemm(const void* A, const void* B, void* C, int64_t M, int64_t N, int
 }
 
 // C[M, N] (op)= At^T . B, operands of `io`, C of `dtype`; rows of At and B 16-byte aligned and below 4 GiB in all.  parts: room of
-// token_parts_bytes, or null: not in parts.  live (bfloat16): device count of the rows of both that take part, at most K; least_rows of
-// them are read at least.  scale (bfloat16): device factor.
+// token_parts_bytes, or null: not in parts.  live: device count of the rows of both that take part, at most K; in bfloat16 least_rows of
+// them are read at least, and in float32 what is behind them holds zeros.  scale (bfloat16): device factor.
 void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int64_t M,
                    int64_t N, int64_t K, bool accumulate, Launcher& L, float* parts, const int* live = nullptr, const float* scale = nullptr,
                    int least_rows = 0) {
@@ -128,7 +128,7 @@ void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const 
     else typed(float{});
     return;
   }
-  f32_product(F32Operand{A, lda, false, false}, F32Operand{B, ldb, false, false}, C, dtype, ldc, M, N, K, accumulate, L);
+  f32_product(F32Operand{A, lda, false, false}, F32Operand{B, ldb, false, false}, C, dtype, ldc, M, N, K, accumulate, L, false, live);
 }
 
 // Tokens of one such product: a buffer resource has to reach over the wider operand.  A multiple of 64, so of a block too.
@@ -178,7 +178,7 @@ struct CePlan {
   int64_t strips;   // its waves' strips of columns, 128 wide on the persistent kernel, else 64
   SplitChoice dx_choice;   // of dX's sum over a piece
   int least_rows;
-  size_t order, count, unit, targets, per_row, x, part, z, parts, dx;   // offsets into the workspace
+  size_t order, count, unit, targets, per_row, x, part, z, parts, dx, dw_parts;   // offsets into the workspace
   size_t forward, backward;                      // its bytes
 };
 
@@ -251,6 +251,13 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   plan_ce_dx(p, d->io_dtype == ACC_BF16);
   p->parts = take(p->dx_choice.splits * p->rows * p->d * 4);
   p->dx = take(p->vp < p->v ? p->rows * p->d * 4 : 0);
+  int64_t dw = 0;
+  for (bool sum : {(d->flags & ACC_FLAG_DW_ACCUMULATE) != 0, true}) {   // runs after the first are added
+    if (sum && !(d->flags & ACC_FLAG_DW_ACCUMULATE) && p->run == p->n) continue;
+    const int64_t bytes = (int64_t)token_parts_bytes(d->io_dtype, d->dw_dtype, sum, p->vp, p->d, p->run < p->least_rows ? p->least_rows : p->run);
+    if (bytes > dw) dw = bytes;
+  }
+  p->dw_parts = take(dw);
   p->backward = at > p->forward ? at : p->forward;
   return ACC_OK;
 }
@@ -296,7 +303,7 @@ void ce_gather(const CeRun& r, const void* X, const float* stats, const float* d
 // Z [rows, piece] = X . W_piece^T in float32.
 void ce_logits_f32(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
   f32_product(F32Operand{r.ws + r.p.x, r.p.d, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, true, false}, r.ws + r.p.z, ACC_F32, r.p.ldz, r.n,
-              r.piece(v0), r.p.d, false, L, true);
+              r.piece(v0), r.p.d, false, L, true, r.tokens.count);
 }
 
 // X . W^T over columns v0 .. v0 + vp - 1, bfloat16, into sums of exponentials or the logits' gradient [rows, ldz].
@@ -339,7 +346,7 @@ int ce_input_gradient(const CeRun& r, const void* W, int64_t v0, Launcher& L) {
   float* parts = (float*)(r.ws + r.p.parts);
   if (r.desc->io_dtype != ACC_BF16) {
     f32_split_product(F32Operand{r.ws + r.p.z, r.p.ldz, true, false}, F32Operand{r.w_piece(W, v0), r.p.ldw, false, false}, parts, r.p.d, r.n, r.p.d, vp,
-                      false, c.k_per_split, stride, L);
+                      c.k_per_split, stride, r.tokens.count, L);
     return splits;
   }
   FastGemmParams p = fast_params(r.ws + r.p.z, r.w_piece(W, v0), parts, r.n, r.p.d, round_up(vp, 8), r.p.ldz, r.p.ldw, r.p.d, nullptr, 1.f, 0.f);
@@ -567,7 +574,7 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
         char* dw = (char*)dW + (size_t)v0 * r.p.d * dtype_size(desc->dw_dtype);
         const bool add = r.t0 > 0 || (desc->flags & ACC_FLAG_DW_ACCUMULATE);
         token_product(desc->io_dtype, desc->dw_dtype, dz, r.p.ldz, r.ws + r.p.x, r.p.d, dw, r.p.d, vp, r.p.d, b16 && r.n < r.p.least_rows ? r.p.least_rows : r.n, add,
-                      L, nullptr, b16 ? r.tokens.count : nullptr, unit, r.p.least_rows);
+                      L, vp == r.p.vp && r.n == r.p.run ? (float*)(r.ws + r.p.dw_parts) : nullptr, r.tokens.count, unit, r.p.least_rows);
       }
     }
   });
