@@ -98,23 +98,83 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
 // What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero, up to
 // 256 of them for the products' least rows.  targets: -1 where there is no gradient.  per_row, in a backward call: lse, the target's
 // logit and the incoming gradient (over *unit), `rows` of each.
-template <typename T>
+// SELECT: the selection as well, for up to kCeSelectHere tokens: every work-group finds its row's token by itself, from all targets, which
+// saves a launch that takes 4.5 us with the pause behind it.
+constexpr int kCeSelectHere = 1024;
+template <typename T, bool SELECT>
 __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __restrict__ X, int64_t ldx, int d, int64_t rows, T* __restrict__ Xc, int64_t V,
-                                                        const float* __restrict__ stats, const float* __restrict__ dloss, const float* __restrict__ unit,
+                                                        const float* __restrict__ stats, const float* __restrict__ dloss, float* __restrict__ unit,
                                                         int64_t stats_stride, int64_t* __restrict__ targets, float* __restrict__ per_row) {
   constexpr int VEC = 16 / sizeof(T);
   typedef T vecT __attribute__((ext_vector_type(VEC)));
   const int64_t r = blockIdx.x;
-  const int count = *t.count;
+  int count, i = 0;
+  float g_unit = 1.f;
+  if constexpr (SELECT) {
+    constexpr int PER = kCeSelectHere / 256;
+    __shared__ int wave_kept[4], token;
+    __shared__ float wave_largest[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i0 = tid * PER;
+    bool keep[PER];
+    int mine = 0;
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int at = i0 + k < t.n ? i0 + k : t.n - 1;
+      keep[k] = t.targets[at] >= 0 && i0 + k < t.n;
+      mine += keep[k] ? 1 : 0;
+      if (unit) {
+        const float g = dloss[at];
+        if (keep[k] && isfinite(g)) top = fmaxf(top, fabsf(g));
+      }
+    }
+    int before = mine;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int o = __shfl_up(before, s);
+      before += lane >= s ? o : 0;
+    }
+    top = wave_max(top);
+    if (lane == 63) {
+      wave_kept[wave] = before;
+      wave_largest[wave] = top;
+    }
+    __syncthreads();
+    count = wave_kept[0] + wave_kept[1] + wave_kept[2] + wave_kept[3];
+    if (unit) {
+      top = fmaxf(fmaxf(wave_largest[0], wave_largest[1]), fmaxf(wave_largest[2], wave_largest[3]));
+      g_unit = top > 0.f ? top : 1.f;
+    }
+    int at = before - mine;   // tokens with a loss before this thread's
+#pragma unroll
+    for (int w = 0; w < 3; ++w) at += w < wave ? wave_kept[w] : 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {   // the others behind those with a loss
+      if (i0 + k < t.n && (keep[k] ? at : count + i0 + k - at) == r) token = i0 + k;
+      at += keep[k] ? 1 : 0;
+    }
+    __syncthreads();
+    if (r < t.n) {
+      i = token;
+      if (tid == 0) t.order[r] = i;
+    }
+    if (r == 0 && tid == 0) {
+      *t.count = count;
+      if (unit) *unit = g_unit;
+    }
+  } else {
+    count = *t.count;
+    if (r < count) i = t.order[r];
+    if (unit) g_unit = *unit;
+  }
   const bool lives = r < count;
-  const int i = lives ? t.order[r] : 0;
   if (threadIdx.x == 0) {
     const int64_t target = lives ? t.targets[i] : -1;
     targets[r] = target < V ? target : -1;
     if (stats) {
       per_row[r] = lives ? stats[i] : 0.f;
       per_row[rows + r] = lives && target < V ? stats[stats_stride + i] : 0.f;
-      per_row[2 * rows + r] = lives && target < V ? dloss[i] / (unit ? *unit : 1.f) : 0.f;
+      per_row[2 * rows + r] = lives && target < V ? dloss[i] / g_unit : 0.f;
     }
   }
   if (sizeof(T) == 2 && !lives && r >= 256) return;   // the float32 products read every row

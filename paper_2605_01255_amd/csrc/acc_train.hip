@@ -289,15 +289,17 @@ template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, cons
 void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
   float* unit = (float*)(r.ws + r.p.unit);
   const bool units = dloss && r.desc->io_dtype == ACC_BF16;
-  L(ce_select_kernel, dim3(1), dim3(1024), r.tokens, units ? dloss + r.t0 : nullptr, unit);
-  auto typed = [&](auto value) {
+  const bool here = r.n <= kCeSelectHere;
+  if (!here) L(ce_select_kernel, dim3(1), dim3(1024), r.tokens, units ? dloss + r.t0 : nullptr, unit);
+  auto typed = [&](auto value, auto select) {
     using T = decltype(value);
-    L(ce_gather_kernel<T>, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d, r.p.rows,
-      (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, units ? (const float*)unit : nullptr, r.p.n, (int64_t*)(r.ws + r.p.targets),
-      (float*)(r.ws + r.p.per_row));
+    L(ce_gather_kernel<T, decltype(select)::value>, dim3((unsigned)r.p.rows), dim3(256), r.tokens, (const T*)X + (size_t)r.t0 * r.p.ldx, r.p.ldx, (int)r.p.d,
+      r.p.rows, (T*)(r.ws + r.p.x), r.p.v, stats ? stats + r.t0 : nullptr, dloss ? dloss + r.t0 : nullptr, units ? unit : nullptr, r.p.n,
+      (int64_t*)(r.ws + r.p.targets), (float*)(r.ws + r.p.per_row));
   };
-  if (r.desc->io_dtype == ACC_BF16) typed(bf16{});
-  else typed(float{});
+  auto of = [&](auto value) { here ? typed(value, std::true_type{}) : typed(value, std::false_type{}); };
+  if (r.desc->io_dtype == ACC_BF16) of(bf16{});
+  else of(float{});
 }
 
 // Z [rows, piece] = X . W_piece^T in float32.
