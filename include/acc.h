@@ -276,7 +276,7 @@ int acc_linear_bwd_rsvd(const acc_linear_desc* desc, const void* dY, const void*
 typedef enum { ACC_ACT8_E4M3 = 0, ACC_ACT8_INT8 = 1 } acc_act8_format;
 
 typedef struct acc_act8_desc {
-  int64_t n;         /* tokens, 1 .. 2^30                                                    */
+  int64_t n;         /* tokens, 1 .. 2^30, and n times c (in whole 64 channels) below 2^37   */
   int64_t c;         /* channels, a multiple of 8, at most 2^21                              */
   int64_t ldx;       /* row stride of X in elements, a multiple of 8; 0 = c                  */
   int32_t io_dtype;  /* acc_dtype of X                                                       */
@@ -297,7 +297,7 @@ int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, 
 
 /* Its backward pass: dX = dY.W^T exact, and dW [d_in, d_out] = X^^T.dY of dw_dtype ([d_out, d_in] = dY^T.X^ with
  * ACC_FLAG_W_OUT_IN; += with ACC_FLAG_DW_ACCUMULATE), a full gradient, not a factored one.  The products are accumulated in
- * float and rounded once (where X^ or dY takes more than 4 GiB once per 4 GiB of tokens).  dX (W is then not read and may be
+ * float and rounded once (where X^ or dY takes more than 4 GiB once per 4 GiB of tokens; 64 rows of dY have to fit there).  dX (W is then not read and may be
  * NULL) or dW (Q, E and the workspace likewise) may be NULL, not both.  ACC_FLAG_SKIP_SKETCH is refused.
  * workspace: ws_bytes >= acc_linear_act8_workspace_bytes(desc) for dW. */
 size_t acc_linear_act8_workspace_bytes(const acc_linear_desc* desc);
@@ -335,15 +335,15 @@ int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Q
  *                of X holds, infinities and NaN included, is not read into any sum).  v and above: loss NaN, no gradient.
  *   loss [n]     float;  stats [2, n] float: lse, then the target's logit, which the backward call reads.
  *   dloss [n]    float, the gradient of every token's loss (1 / tokens with a loss for their mean).
- * n above 2^18, or X of more than 2 GiB, is worked off in runs of tokens, and a bfloat16 dW is then rounded once per run.
- * A row of logits of which none is finite gives what the formulas give (infinities, NaN). */
+ * n above 2^18, X of more than 2 GiB, or n times v above 2^35 is worked off in runs of tokens, and a bfloat16 dW is then rounded
+ * once per run.  A token whose log-sum-exp is not finite gets a loss that is not, and NaN gradients. */
 typedef struct acc_ce_desc {
   int64_t n;         /* tokens, 1 .. 2^30                                                    */
   int64_t d;         /* features, a multiple of 8, at most 2^16                              */
   int64_t v;         /* vocabulary, 1 .. 2^21, any size                                      */
   int64_t ldx;       /* row stride of X and dX in elements, a multiple of 8, at most 2^18; 0 = d */
   int64_t ldw;       /* row stride of W (and not of dW, which is dense), likewise; 0 = d     */
-  int64_t piece;     /* columns of a piece, a multiple of 256; 0 = as many as keep a piece within 512 MiB */
+  int64_t piece;     /* columns of a piece, a multiple of 256; 0 = as many as keep a piece within 1 GiB */
   int32_t io_dtype;  /* acc_dtype of X, W and dX                                             */
   int32_t dw_dtype;  /* acc_dtype of dW                                                      */
   uint32_t flags;    /* ACC_FLAG_DW_ACCUMULATE: dW += (acc_linear_ce_bwd)                    */

@@ -164,7 +164,7 @@ class CompressedLinear(torch.nn.Module):
 def _rows(t, width):
     """t as rows of `width` elements the library can take as they lie (16-byte aligned, any stride), else a copy."""
     t2 = t.reshape(-1, width)
-    if t2.stride(1) != 1 or (t2.shape[0] > 1 and (t2.stride(0) % 8 or t2.stride(0) < width)) or t2.data_ptr() % 16:
+    if t2.stride(1) != 1 or (t2.shape[0] > 1 and (t2.stride(0) % 8 or not width <= t2.stride(0) <= 1 << 18)) or t2.data_ptr() % 16:
         t2 = t2.contiguous()
     return t2
 
@@ -200,6 +200,7 @@ class CompressedSwiGLUFunction(torch.autograd.Function):
         return h.reshape(*x.shape[:-1], f)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dh):
         n, f, fmt, shape = ctx.meta
         dx = torch.empty(n, 2 * f, dtype=dh.dtype, device=dh.device)
@@ -261,6 +262,7 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
         return acc.make_ce_desc(n, d, v, ldx=_ld(x2), ldw=_ld(w), io_dtype=_CODES[w.dtype])
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dloss):
         n, d, v, shape = ctx.meta
         want_dx, want_dw = ctx.needs_input_grad[:2]

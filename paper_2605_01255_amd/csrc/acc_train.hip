@@ -12,9 +12,9 @@ namespace {
 // ---- 8-bit checkpoints ------------------------------------------------------------------------------
 bool valid_format(int32_t f) { return f == ACC_ACT8_E4M3 || f == ACC_ACT8_INT8; }
 
-// Sizes and strides that the calls without an acc_linear_desc share: rows of `c` elements, `ld` apart (0: dense).
+// Sizes and strides that the 8-bit calls share: rows of `c` elements, `ld` apart (0: dense), in a grid of less than 2^32 lanes.
 int validate_rows(int64_t n, int64_t c, int64_t* ld) {
-  if (n <= 0 || n > (int64_t)1 << 30 || c <= 0 || c > (1 << 21) || c % 8) return ACC_ERR_SHAPE;
+  if (n <= 0 || n > (int64_t)1 << 30 || c <= 0 || c > (1 << 21) || c % 8 || act_work_groups(n, c) >= 1 << 24) return ACC_ERR_SHAPE;
   if (!*ld) *ld = c;
   return *ld < c || *ld % 8 || *ld > ((int64_t)1 << 24) ? ACC_ERR_SHAPE : ACC_OK;
 }
@@ -131,13 +131,14 @@ void token_product(int32_t io, int32_t dtype, const void* A, int64_t lda, const 
   f32_product(F32Operand{A, lda, false, false}, F32Operand{B, ldb, false, false}, C, dtype, ldc, M, N, K, accumulate, L, false, live);
 }
 
-// Tokens of one such product: a buffer resource has to reach over the wider operand.  A multiple of 64, so of a block too.
+// Tokens of one such product: a buffer resource has to reach over the wider operand, whole K tiles of 64 tokens (so whole blocks too)
+// included.  0: not even over one.
 int64_t token_chunk(int64_t n, int64_t ld, int32_t io) {
-  const int64_t most = kMaxOperandBytes / (ld * (int64_t)dtype_size(io)) - 64;
-  return n <= most ? n : most / 64 * 64;
+  const int64_t most = kMaxOperandBytes / (ld * (int64_t)dtype_size(io)) / 64 * 64;
+  return n <= most ? n : most;
 }
 
-// The checkpoint's values, then the parts of the product with them.
+// The checkpoint's values, then the parts of the product with them.  total == 0: rows too far apart, or too many.
 struct Act8Plan {
   int64_t tokens;   // of one product
   size_t parts, total;
@@ -145,6 +146,7 @@ struct Act8Plan {
 Act8Plan plan_act8(const acc_linear_desc* d, const Shape& s) {
   Act8Plan p{};
   p.tokens = token_chunk(s.n, s.ldy > s.d_in ? s.ldy : s.d_in, d->io_dtype);
+  if (p.tokens == 0 || act_work_groups(s.n, s.d_in) >= 1 << 24) return p;
   p.parts = (size_t)round_up(p.tokens * s.d_in * (int64_t)dtype_size(d->io_dtype), 256);
   const bool w_oi = (d->flags & ACC_FLAG_W_OUT_IN) != 0;
   const int64_t M = w_oi ? s.d_out : s.d_in, N = w_oi ? s.d_in : s.d_out;
@@ -208,6 +210,8 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   const int64_t es = (int64_t)dtype_size(d->io_dtype);
   p->run = ((int64_t)2 << 30) / (p->d * es) / 256 * 256;
   if (p->run > 1 << 18) p->run = 1 << 18;
+  const int64_t by_strips = ((int64_t)4 << 30) / (8 * ceil_div(p->v, 64)) / 256 * 256;   // 4 GiB of strips' sums
+  if (p->run > by_strips) p->run = by_strips;
   if (p->run > p->n) p->run = p->n;
   p->rows = p->run < 256 ? 256 : p->run;
   // rows of dz that are there whatever the number of tokens with a loss, zeros behind them: what the product over the tokens takes at
@@ -414,6 +418,7 @@ int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, 
   if (rc != ACC_OK) return rc;
   if (!valid_format(format)) return ACC_ERR_DTYPE;
   const bool keep = !(desc->flags & ACC_FLAG_SKIP_SKETCH);
+  if (keep && act_work_groups(s.n, s.d_in) >= 1 << 24) return ACC_ERR_SHAPE;
   if (!X || !W || !Y || (keep && (!Q || !E))) return ACC_ERR_INVALID_ARG;
   if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Q) || !aligned16(E)) return ACC_ERR_ALIGN;
   if ((rc = check_device()) != ACC_OK) return rc;
@@ -441,6 +446,7 @@ int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY,
   if (!aligned16(dY) || !aligned16(W) || !aligned16(Q) || !aligned16(E) || !aligned16(dX) || !aligned16(dW) || !aligned16(workspace))
     return ACC_ERR_ALIGN;
   const Act8Plan plan = plan_act8(desc, s);
+  if (dW && !plan.total) return ACC_ERR_SHAPE;
   if (dW && (!workspace || ws_bytes < plan.total)) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
   Launcher L{(hipStream_t)stream};

@@ -97,6 +97,23 @@ def test_the_linear_layers_calls_are_refused():
     assert lib.acc_linear_bwd_act8(None, 0, *range(0x1000, 0x8000, 0x1000), need, None) == -1
 
 
+def test_grids_and_rows_beyond_the_kernels_reach_are_refused():
+    # 2^24 work-groups of 256 lanes are more than a launch takes; 64 rows of dY have to fit into 4 GiB
+    lib = acc._lib
+    wide = acc.make_act8_desc(1 << 30, 128)
+    assert lib.acc_act8_pack(ctypes.byref(wide), 0x1000, 0x2000, 0x3000, None) == -2
+    assert lib.acc_act8_pack(ctypes.byref(acc.make_act8_desc((1 << 30) - 64, 64)), 0x1000, 0x2000, 0x3000, None) in FINE
+    for n in (1, 1 << 20):
+        far = acc.make_desc(n, 64, 64, 8, ldy=1 << 26)
+        assert acc.acc_linear_act8_workspace_bytes(far) == 0
+        args = (0x1000, 0x2000, 0x3000, 0x4000)
+        assert lib.acc_linear_bwd_act8(ctypes.byref(far), 0, *args, 0x5000, 0x6000, 0x7000, 1 << 40, None) == -2
+        assert lib.acc_linear_bwd_act8(ctypes.byref(far), 0, *args, 0x5000, None, None, 0, None) in FINE
+    long = acc.make_desc(1 << 30, 128, 8, 8)
+    assert lib.acc_linear_fwd_act8(ctypes.byref(long), 0, *range(0x1000, 0x6000, 0x1000), None) == -2
+    assert acc.acc_linear_act8_workspace_bytes(long) == 0
+
+
 def test_the_workspace_of_long_inputs_is_that_of_a_part():
     # an operand of a product reaches over 4 GiB at most: more tokens take several products through one workspace
     part = acc.acc_linear_act8_workspace_bytes(acc.make_desc(1 << 20, 4096, 4096, 8))

@@ -58,3 +58,4 @@ def test_the_workspace_does_not_grow_to_the_logits():
     assert at(65536) < 6 << 30
     assert at(1 << 20) == at(1 << 19)
     assert at(8192, piece=1024) < at(8192)
+    assert acc.acc_linear_ce_workspace_bytes(acc.make_ce_desc(1 << 18, 64, 1 << 21), False) < 8 << 30   # of 2^39 logits
