@@ -527,7 +527,10 @@ int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, con
       const bool as_they_come = r.n <= 256;
       if (as_they_come) tokens.order = tokens.count = nullptr;
       else ce_gather(r, X, nullptr, nullptr, L);
-      ce_product<Epilogue::kExpSums>(r, as_they_come ? (const bf16*)X + (size_t)r.t0 * r.p.ldx : nullptr, W, 0, r.p.v, L);
+      // of W what a buffer resource reaches: chunks past K go to its end, and have to lie outside
+      const int64_t columns = ((int64_t)2 << 30) / (r.p.ldw * 2) / 256 * 256;
+      for (int64_t v0 = 0; v0 < r.p.v; v0 += columns)
+        ce_product<Epilogue::kExpSums>(r, as_they_come ? (const bf16*)X + (size_t)r.t0 * r.p.ldx : nullptr, W, v0, r.p.v - v0 < columns ? r.p.v - v0 : columns, L);
       int across = 16;   // rows of a work-group
       while (across > 1 && across / 2 >= r.n) across /= 2;
       L(ce_finish_kernel, dim3((unsigned)ceil_div(r.n, across)), dim3(256), tokens, (const f32x2*)(r.ws + r.p.part), (int)r.p.strips,

@@ -142,6 +142,41 @@ def test_large_bfloat16(acc, shape):
     Case(acc, dtype="bf16", **shape).check()
 
 
+def test_losses_of_a_matrix_beyond_four_gib(acc):
+    """More of W than one buffer resource reaches, with a ragged last K tile; targets at both ends.  By the terms above a logit is
+    off by e_z, and a log-sum-exp by that and (2^21 / 64 + 64) u < 2^-8 / 2, and 8 u of its own size, under 2^-8 / 2 as well."""
+    import torch
+    n, d, v = 5, 1032, (1 << 21) - 3
+    torch.manual_seed(9)
+    x = (torch.randn(n, d, device="cuda") * 0.05).to(torch.bfloat16)
+    w = torch.empty(v, d, device="cuda", dtype=torch.bfloat16).normal_()
+    t = torch.tensor([0, v - 1, v // 2, -1, (1 << 20) + 77], device="cuda")
+    desc = acc.make_ce_desc(n, d, v)
+    loss, stats = torch.full((n,), 7.0, device="cuda"), torch.full((2, n), 7.0, device="cuda")
+    ws = torch.empty(acc.acc_linear_ce_workspace_bytes(desc, False), dtype=torch.uint8, device="cuda")
+    acc.acc_linear_ce_fwd(desc, x, w, t, loss, stats, ws)
+    torch.cuda.synchronize()
+    x64, z, off = x.double(), [], 0.0
+    for v0 in range(0, v, 1 << 18):
+        part = w[v0:v0 + (1 << 18)].double().t().contiguous()
+        z.append(x64 @ part)
+        off = max(off, float((x64.abs() @ part.abs()).max()))
+    z = torch.cat(z, 1)
+    bound = 2 * (d + 8) * U * off + 2.0 ** -8
+    keep = t >= 0
+    lse = torch.where(keep, torch.logsumexp(z, 1), 0.0)
+    zt = torch.where(keep, z.gather(1, t.clamp(min=0)[:, None])[:, 0], 0.0)
+    assert float((stats[0].double() - lse).abs().max()) <= bound
+    assert float((stats[1].double() - zt).abs().max()) <= bound
+    assert float((loss.double() - (lse - zt)).abs().max()) <= bound and float(loss[3]) == 0.0
+
+
+@pytest.mark.parametrize("rest", [100, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_tokens_than_a_run(acc, dtype, rest):
+    Case(acc, (1 << 18) + rest, 8, 77, dtype, dw="f32", ignored=0.3).check()
+
+
 @pytest.mark.parametrize("dtype,dw", [("bf16", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("add", [False, True])
 def test_gradient_of_the_other_type(acc, dtype, dw, add):
