@@ -115,6 +115,7 @@ class CompressedLinearFunction(torch.autograd.Function):
     def _backward_act8(ctx, dy2):
         compressor, n, d_in, d_out, _, _, code, has_bias, x_shape = ctx.meta
         w, q, e = ctx.saved_tensors
+        dy2 = _aligned(dy2)
         dev, dt = dy2.device, dy2.dtype
         want_dx, want_dw = ctx.needs_input_grad[:2]
         desc = acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=acc.ACC_FLAG_W_OUT_IN)
@@ -161,11 +162,17 @@ class CompressedLinear(torch.nn.Module):
                 f"compressor={self.compressor}, bias={self.bias is not None}")
 
 
+def _aligned(t):
+    """t, contiguous and 16-byte aligned: a slice of a vector (labels[1:]) is the one and not the other."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 def _rows(t, width):
     """t as rows of `width` elements the library can take as they lie (16-byte aligned, any stride), else a copy."""
     t2 = t.reshape(-1, width)
     if t2.stride(1) != 1 or (t2.shape[0] > 1 and (t2.stride(0) % 8 or not width <= t2.stride(0) <= 1 << 18)) or t2.data_ptr() % 16:
-        t2 = t2.contiguous()
+        t2 = _aligned(t2)
     return t2
 
 
@@ -242,7 +249,7 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
         if not (x.device == weight.device == target.device):
             raise ValueError("x, weight and target must be on one device")
         v, d = weight.shape
-        x2, w, t = _rows(x, d), _rows(weight, d), target.reshape(-1).contiguous()
+        x2, w, t = _rows(x, d), _rows(weight, d), _aligned(target.reshape(-1))
         n, dev = x2.shape[0], x.device
         loss = torch.empty(n, dtype=torch.float32, device=dev)
         ctx.meta = (n, d, v, x.shape)
@@ -272,7 +279,7 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
                     torch.zeros(v, d, dtype=w.dtype, device=dev) if want_dw else None, None)
         _, x2, t, stats = ctx.saved_tensors
         desc = LinearCrossEntropyFunction._desc(ctx, x2, w)
-        g = dloss.reshape(-1).to(torch.float32).contiguous()
+        g = _aligned(dloss.reshape(-1).to(torch.float32))
         ldx = x2.stride(0) if n > 1 else d
         dx = torch.empty(n, ldx, dtype=w.dtype, device=dev)[:, :d] if want_dx else None   # rows as far apart as x's
         dw = torch.empty(v, d, dtype=w.dtype, device=dev) if want_dw else None

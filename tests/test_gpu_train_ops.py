@@ -232,6 +232,28 @@ def test_a_training_step(mods, kinds):
     assert np.all(np.abs(flat(x.grad) - total) <= 2.0 ** -8 * 1.01 * (np.abs(into) + np.abs(total)) + (2 * f + 8) * U * (np.abs(dGU) @ np.abs(_f64(l1.weight))) + 1e-12)
 
 
+def test_slices_that_are_not_aligned(mods):
+    """Shifted labels and gradients that arrive as slices of a longer vector, against copies of them."""
+    torch, ag = mods
+    torch.manual_seed(5)
+    x = torch.randn(2, 77, 72, device="cuda", dtype=torch.bfloat16)
+    w0 = torch.randn(301, 72, device="cuda", dtype=torch.bfloat16)
+    ids, g = torch.randint(0, 301, (155,), device="cuda"), torch.randn(155, device="cuda")
+    assert ids[1:].data_ptr() % 16 and g[1:].data_ptr() % 16
+    got = []
+    for labels, weight in ((ids[1:], g[1:]), (ids[1:].clone(), g[1:].clone())):
+        a, w = x.detach().requires_grad_(), w0.detach().requires_grad_()
+        first = torch.zeros(1, device="cuda", requires_grad=True)
+        loss = ag.LinearCrossEntropyFunction.apply(a, w, labels.reshape(2, 77))
+        (torch.cat([first, loss.reshape(-1)]) * torch.cat([g[:1], weight])).sum().backward()   # its gradient starts at the second element
+        got.append((loss.detach(), a.grad, w.grad))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    flat = torch.randn(9 * 144 + 3, device="cuda")
+    h = [ag.CompressedSwiGLUFunction.apply(f.reshape(9, 144), "int8") for f in (flat[3:], flat[3:].clone())]
+    assert torch.equal(*h)
+
+
 def test_two_streams_at_once(mods):
     """Calls that share nothing on two streams, against the same calls one after the other."""
     torch, ag = mods
