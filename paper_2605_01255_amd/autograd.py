@@ -112,6 +112,7 @@ class CompressedLinearFunction(torch.autograd.Function):
         return dx.reshape(x_shape), dw, db, None, None, None, None, None
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def _backward_act8(ctx, dy2):
         compressor, n, d_in, d_out, _, _, code, has_bias, x_shape = ctx.meta
         w, q, e = ctx.saved_tensors

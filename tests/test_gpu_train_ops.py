@@ -254,6 +254,18 @@ def test_slices_that_are_not_aligned(mods):
     assert torch.equal(*h)
 
 
+def test_second_derivatives_are_refused(mods):
+    torch, ag = mods
+    x = torch.randn(8, 64, device="cuda", requires_grad=True)
+    w = torch.randn(32, 64, device="cuda", requires_grad=True)
+    t = torch.zeros(8, dtype=torch.int64, device="cuda")
+    for y in (ag.CompressedLinearFunction.apply(x, w, None, 0, 0, "int8"), ag.CompressedSwiGLUFunction.apply(x, "e4m3"),
+              ag.LinearCrossEntropyFunction.apply(x, w, t)):
+        (dx,) = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            dx.sum().backward()
+
+
 def test_two_streams_at_once(mods):
     """Calls that share nothing on two streams, against the same calls one after the other."""
     torch, ag = mods
