@@ -297,8 +297,8 @@ int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, 
 
 /* Its backward pass: dX = dY.W^T exact, and dW [d_in, d_out] = X^^T.dY of dw_dtype ([d_out, d_in] = dY^T.X^ with
  * ACC_FLAG_W_OUT_IN; += with ACC_FLAG_DW_ACCUMULATE), a full gradient, not a factored one.  The products are accumulated in
- * float and rounded once (where X^ or dY takes more than 4 GiB once per 4 GiB of tokens; 64 rows of dY have to fit there).  dX (W is then not read and may be
- * NULL) or dW (Q, E and the workspace likewise) may be NULL, not both.  ACC_FLAG_SKIP_SKETCH is refused.
+ * float and rounded once (where X^ or dY takes more than 4 GiB once per 4 GiB of tokens; 64 rows of dY have to fit there).
+ * dX (W is then not read and may be NULL) or dW (Q, E and the workspace likewise) may be NULL, not both.  ACC_FLAG_SKIP_SKETCH is refused.
  * workspace: ws_bytes >= acc_linear_act8_workspace_bytes(desc) for dW. */
 size_t acc_linear_act8_workspace_bytes(const acc_linear_desc* desc);
 int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY, const void* W, const void* Q, const void* E,

@@ -12,8 +12,9 @@
 //
 // All kernels here are bound by HBM.  One wave takes 32 tokens x 64 channels: lane = 8 channels (16 bytes of bfloat16) of 4 tokens,
 // all its loads requested at once, so a block's maximum needs three exchanges between lanes and no LDS, and rows are read in whole
-// cache lines.  Eight tokens a lane take twice the registers: the gated forward pass of 16384 x 8192 226 us against 203, where its
-// 1.08 GB at the rate of a copy take 190; pack and unpack of 16384 x 4096 the same with both (39 and 31 us).
+// cache lines.  Eight tokens a lane take twice the registers: the gated forward pass of 16384 x 8192 226 us against 203 on one box
+// (189 to 203 since, its backward pass 186 to 192: 5.3 to 5.8 TB/s, where a copy runs at 5.0); pack and unpack of 16384 x 4096 the same
+// with both (35 to 40 and 31 us).
 #pragma once
 #include "acc_common.h"
 
@@ -149,7 +150,7 @@ template <int FORMAT, bool CHECK> __device__ __forceinline__ void act_values(u32
   });
 }
 
-// A wave's tile: 8 channels from `c`, tokens row .. row + 7 of block `block`.
+// A wave's tile: 8 channels from `c`, tokens row .. row + 3 of block `block`.
 struct ActLane {
   int64_t block, row, c;
   int rows;       // tokens of this lane that exist (0: none, or its channels do not)
@@ -172,7 +173,7 @@ inline __host__ int64_t act_work_groups(int64_t n, int64_t c) {  // of 256 lanes
   return ceil_div(ceil_div(n, kActBlock) * ceil_div(c, kActChannels), 4);
 }
 
-// This lane's eight tokens of eight channels (0 where a token does not exist) into the checkpoint [n, c].
+// This lane's four tokens of eight channels (0 where a token does not exist) into the checkpoint [n, c].
 template <int FORMAT, typename T>
 __device__ __forceinline__ void act_keep(const ActLane& l, int64_t c, ActRow<T> (&x)[kActTokens], uint8_t* __restrict__ Q, uint8_t* __restrict__ E) {
   uint32_t largest[8], any = 0;
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict_
 }
 
 // 1 / (1 + exp(-x)); 0 and 1 at the ends, as exp overflows to infinity or vanishes.  bfloat16 results take the hardware's
-// exponential and reciprocal (a few 2^-23 of the value, under the rounding of 2^-9), float32 ones the library's.
+// exponential and reciprocal (a few 2^-23 of the value, under the rounding of 2^-8), float32 ones the library's.
 template <typename T> __device__ __forceinline__ float sigmoid(float x) {
   if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-x));
   else return 1.f / (1.f + expf(-x));

@@ -54,14 +54,13 @@ void ring_token_gemm(FastGemmParams& p, Launcher& L) {
                (size_t)gemm_ring_lds_bytes<TM, TN, NS>(), p);
 }
 
-// f(the tile's 16 x 16 blocks in both directions and its stages as constants): three stages where a compute unit has one work-group
+// f(the tile's 16 x 16 blocks in both directions and its stages as constants): three stages where a compute unit has one work-group.
+// 192 x 128 is the largest that pick_split_gemm has for this kernel.
 template <typename F> void with_ring_tile(GemmTile tile, bool one_round, F&& f) {
   using std::integral_constant;
   switch (tile) {
-    case GemmTile::k256:
-    case GemmTile::k256x192:
-    case GemmTile::k192x128: return one_round ? f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 3>{})
-                                              : f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    default: return one_round ? f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 3>{})
+                              : f(integral_constant<int, 6>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
     case GemmTile::k128: return one_round ? f(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 3>{})
                                           : f(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
     case GemmTile::k128x64: return f(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 3>{});

@@ -258,6 +258,31 @@ def test_linear_layer(acc, n, d_in, d_out, dtype, dw, w_out_in, pad, add, fmt):
     assert torch.equal(Y, Y2)
 
 
+def test_linear_layer_over_more_tokens_than_a_product(acc):
+    """Rows of dY so far apart that 4 GiB hold fewer tokens than there are: the weight gradient is a sum of two products.
+    Its operands are exact in bfloat16, so it is off by (n + 8) 2^-24 of the sum of magnitudes and its own rounding."""
+    import torch
+    n, d_in, d_out, ldy = 2121, 136, 72, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(3)
+    wide = torch.empty(n, ldy, dtype=torch.bfloat16, device="cuda")
+    dY = wide[:, :d_out]
+    dY.copy_(torch.randn(n, d_out, generator=g, device="cuda"))
+    X = torch.randn(n, d_in, generator=g, device="cuda").to(torch.bfloat16)
+    q, e = acc.alloc_act8(acc.make_act8_desc(n, d_in, format=acc.ACC_ACT8_INT8))
+    acc.acc_act8_pack(acc.make_act8_desc(n, d_in, format=acc.ACC_ACT8_INT8), X, q, e)
+    xq = torch.from_numpy(orc.act8_unpack(q.cpu().numpy(), e.cpu().numpy(), "int8")).cuda()
+    for w_out_in in (False, True):
+        desc = acc.make_desc(n, d_in, d_out, 8, ldy=ldy, dw_dtype=acc.ACC_F32, flags=acc.ACC_FLAG_W_OUT_IN if w_out_in else 0)
+        dW = torch.full((d_out, d_in) if w_out_in else (d_in, d_out), 7.0, device="cuda")
+        wsb, ws = _guarded(torch, (acc.acc_linear_act8_workspace_bytes(desc),), torch.uint8, 0xA5)
+        acc.acc_linear_bwd_act8(desc, acc.ACC_ACT8_INT8, wide, None, q, e, None, dW, ws)
+        torch.cuda.synchronize()
+        assert _guards_hold(wsb, 0xA5)
+        want, terms = xq.t() @ dY.double(), xq.abs().t() @ dY.double().abs()
+        got = dW.double().t() if w_out_in else dW.double()
+        assert bool(((got - want).abs() <= (n + 8) * 2.0 ** -24 * terms + 2.0 ** -24 * want.abs()).all())
+
+
 def test_captured_and_replayed(acc):
     """One graph of a whole step on a side stream, replayed on new inputs with eager work between, against eager calls."""
     import torch
