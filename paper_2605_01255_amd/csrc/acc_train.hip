@@ -184,11 +184,13 @@ struct CePlan {
 };
 
 // dX [n, d] is a sum over the whole piece: where its tiles leave compute units idle the sum is taken in parts, which the last kernel adds
-// up (pick_split_gemm; in float32 parts enough for two 64 x 64 tiles to a compute unit, of 512 columns at least).
+// up (pick_split_gemm; in float32 parts of 512 columns at least, enough for four 64 x 64 tiles to a compute unit, two where
+// there is one row of tiles: us a step with two / four, 1 x 2048 x 32000 313 / 321, 200 x 1024 x 16000 291 / 285, 1024 x 512 x 32000
+// 1127 / 1109, 2048 x 1024 x 16000 1884 / 1826, 515 x 520 x 10007 244 / 244).
 void plan_ce_dx(CePlan* p, bool b16) {
   p->dx_choice = pick_split_gemm(p->run, p->d, p->vp, 32, false, true);
   if (!b16) {
-    int64_t splits = 512 / (ceil_div(p->run, 64) * ceil_div(p->d, 64));
+    int64_t splits = (p->run > 64 ? 1024 : 512) / (ceil_div(p->run, 64) * ceil_div(p->d, 64));
     if (splits > p->vp / 512) splits = p->vp / 512;
     if (splits < 1) splits = 1;
     p->dx_choice.k_per_split = round_up(ceil_div(p->vp, splits), 64);
