@@ -82,8 +82,9 @@ __device__ __forceinline__ int swz_n16(int krow) { return ((krow & 3) << 2) | ((
 // leaves no work-group without a tile for as long as there are some, however many rows there are.
 // kParts: C is float, and what a work-group walks over are pairs of a tile and a part of the K range (k_per_split columns, three K tiles
 // at least, the last part what is left): part s is stored at C + s c_split_stride, from the accumulators as they are (64 bytes of a row
-// at a time; staged as float they would need LDS that the stages have).  Chunks past the part's end are sent out of range in whichever
-// K tile they lie.  Against the ring kernel's 128 x 128 tiles, us: 1024 x 4096 by 128000 columns 906 / 1780, 2048 x 2048 by 50257 409 / 661.
+// at a time; staged as float they would need LDS that the stages have).  A part runs its own K tiles (part_k_tiles).  Chunks past the
+// part's end are sent out of range in whichever K tile they lie; of K tiles that start there (a part of one or two has such) those of
+// both operands, by their lane offsets and from scalar offset 0: a scalar offset beyond the range is nothing to rely on.  Against the ring kernel's 128 x 128 tiles, us: 1024 x 4096 by 128000 columns 906 / 1780, 2048 x 2048 by 50257 409 / 661.
 template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore, int N1 = 12, int S1 = 4, int S0 = 4>
 __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, int n_slots) {
   // schedule of k-step 1: the barrier sits before its slot BAR_Q; N1 wave-loads go out after it, one every S1
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int KT = PARTS ? (int)(p.k_per_split / BK) : RAGGED_K ? (int)((p.K + BK - 1) / BK) : (int)(p.K / BK);
+  const int KT = PARTS ? 0 : RAGGED_K ? (int)((p.K + BK - 1) / BK) : (int)(p.K / BK);
 
   // ---- global -> LDS sources (relative to a tile's buffer resources) ----
   uint32_t a_src[A_LOADS], b_src[B_LOADS];
@@ -160,6 +161,15 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     if constexpr (PARTS) return kt * BK + chunk_k >= r.kn ? 0xFFFFFFF0u : 0u;
     else return RAGGED_K && kt == KT - 1 ? tail : 0u;
   };
+  // kParts: K tile kt starts past the part's end (and so past its rows of B: p.K is p.kb_rows in whole chunks)
+  auto b_past = [&](const TileRef& r, int kt) -> uint32_t {
+    if constexpr (PARTS) return kt * BK >= r.kn ? 0xFFFFFFF0u : 0u;
+    else return 0u;
+  };
+  auto k_offset = [&](const TileRef& r, int kt, uint32_t step) -> uint32_t {
+    if constexpr (PARTS) return kt * BK >= r.kn ? 0u : (uint32_t)kt * step;
+    else return (uint32_t)kt * step;
+  };
   auto tile_ref = [&](int idx) -> TileRef {
     int tm = 0, tn = 0;
     find_tile(idx, tm, tn);
@@ -181,8 +191,8 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     return r;
   };
   auto issue_one = [&](const TileRef& r, int g, int kt, uint32_t stage) {
-    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, PARTS ? a_src[g] | past_k(r, kt) : a_src[g], (uint32_t)kt * a_kstep, stage + (g * NW + wave) * 1024);
-    else buffer_to_lds_b128(r.b_rsrc, b_src[g - A_LOADS], (uint32_t)kt * b_kstep,
+    if (g < A_LOADS) buffer_to_lds_b128(r.a_rsrc, PARTS ? a_src[g] | past_k(r, kt) : a_src[g], k_offset(r, kt, a_kstep), stage + (g * NW + wave) * 1024);
+    else buffer_to_lds_b128(r.b_rsrc, PARTS ? b_src[g - A_LOADS] | b_past(r, kt) : b_src[g - A_LOADS], k_offset(r, kt, b_kstep),
                             stage + A_BYTES + ((g - A_LOADS) * NW + wave) * 1024);
   };
 
@@ -195,11 +205,11 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     const int part = g < A_LOADS ? g * NW * 1024 : A_BYTES + (g - A_LOADS) * NW * 1024;  // a constant per wave-load
     asm volatile("s_add_u32 m0, %1, %2" : "={m0}"(m0_token) : "s"(stage_wave), "s"(part) : "scc");
   };
-  auto issue_at_m0 = [&](const TileRef& r, int g, int kt, uint32_t oob) {  // oob: past_k(kt)
+  auto issue_at_m0 = [&](const TileRef& r, int g, int kt, uint32_t oob) {  // oob: past_k(r, kt)
     if (g < A_LOADS)
-      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K && A_KMAJOR ? a_src[g] | oob : a_src[g]), "s"(r.a_rsrc), "s"((uint32_t)kt * a_kstep), "{m0}"(m0_token) : "memory");
+      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K && A_KMAJOR ? a_src[g] | oob : a_src[g]), "s"(r.a_rsrc), "s"(k_offset(r, kt, a_kstep)), "{m0}"(m0_token) : "memory");
     else
-      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(RAGGED_K && B_KMAJOR ? b_src[g - A_LOADS] | oob : b_src[g - A_LOADS]), "s"(r.b_rsrc), "s"((uint32_t)kt * b_kstep), "{m0}"(m0_token) : "memory");
+      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(PARTS ? b_src[g - A_LOADS] | b_past(r, kt) : RAGGED_K && B_KMAJOR ? b_src[g - A_LOADS] | oob : b_src[g - A_LOADS]), "s"(r.b_rsrc), "s"(k_offset(r, kt, b_kstep)), "{m0}"(m0_token) : "memory");
   };
 
   // ---- LDS read offsets of the operands (see gemm16_tile) ----
@@ -439,15 +449,17 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     const int next_idx = next_slot(idx);
     const bool has_next = next_idx < n_slots;
     const TileRef next_t = has_next ? tile_ref(next_idx) : cur_t;
+    int tiles = KT;
+    if constexpr (PARTS) tiles = part_k_tiles(cur_t.kn);
     // K tile 0: multiplies onto zero and finishes the previous read-out (before the first output tile the staging
     // regions hold nothing and the output resource is empty, so those stores are dropped)
     ktile(par, cur_t, 1, cur_t, 2, T{}, T{}, F{});
-    // K tiles 1 .. KT - 2; the last of them already fetches the next output tile's first K tile
-    for (int kt = 1; kt + 1 < KT; ++kt) {
-      const bool wraps = kt + 2 >= KT;
+    // K tiles 1 .. tiles - 2; the last of them already fetches the next output tile's first K tile
+    for (int kt = 1; kt + 1 < tiles; ++kt) {
+      const bool wraps = kt + 2 >= tiles;
       ktile((kt + par) & 1, cur_t, kt + 1, wraps ? next_t : cur_t, wraps ? 0 : kt + 2, F{}, F{}, F{});
     }
-    const int kt = KT - 1;
+    const int kt = tiles - 1;
     if constexpr (EPI == Epilogue::kExpSums) ce_targets<TB>(p, target, cur_t.m0 + wm * TB * 16, l16);
     else set_output(cur_t);
     if constexpr (EPI == Epilogue::kGradient) {
@@ -457,7 +469,7 @@ __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, i
     if constexpr (EPI == Epilogue::kExpSums) ce_sums<TB, TB>(p, acc, target, cur_t.m0 + wm * TB * 16, cur_t.n0 + wn * TB * 16, l16, g4);
     if (!has_next) break;
     cur_t = next_t;
-    par = (par + KT) & 1;
+    par = (par + tiles) & 1;
     idx = next_idx;
   }
   // no tile follows: block rows 6 and 7 are read out here

@@ -169,6 +169,9 @@ static inline SplitChoice pick_split_gemm(int64_t M, int64_t N, int64_t K, int64
   return best;
 }
 
+// K tiles that the persistent kernel runs of a part of `columns` columns: its own, three at least, which its slot program spans.
+constexpr int part_k_tiles(int64_t columns) { return columns > 128 ? (int)((columns + 63) / 64) : 3; }
+
 // Tile of the products that form the cross entropy's logits, by an estimate like pick_gemm_tile's; a tile's cost holds its exponentials,
 // which the persistent kernel does between two tiles and two work-groups of a compute unit behind each other's products.
 enum class CeTile { k64x128, k128, k192x128, k256 };

@@ -40,6 +40,12 @@ int f32_sketch_splits(int64_t n, int64_t channels, int64_t r, int f32_factor) { 
   return p.stored ? (int)p.splits : 0;
 }
 int f32_shared_launch(int64_t M, int64_t N, int64_t n, int64_t out_n, int splits) { return f32_pair(M, N, splits, n, out_n); }
+void split_gemm(int64_t M, int64_t N, int64_t K, int64_t most_splits, int over_tokens, int persist_ok, int64_t* out) {
+  const SplitChoice c = pick_split_gemm(M, N, K, most_splits, over_tokens != 0, persist_ok != 0);
+  out[0] = (int64_t)c.tile; out[1] = c.one_round; out[2] = c.splits; out[3] = c.k_per_split;
+}
+int ce_tile(int64_t M, int64_t N, int64_t K) { return (int)pick_ce_tile(M, N, K).tile; }
+int ce_part_k_tiles(int64_t columns) { return part_k_tiles(columns); }
 int f32_sketch_fits(int64_t n, int64_t channels, int64_t r, int f32_factor) {
   const F32SketchPlan p = plan_f32_sketch(n, channels, r, f32_factor != 0);
   const int64_t partials = p.splits == 1 && f32_factor ? 0 : p.splits * channels * r;
@@ -59,6 +65,8 @@ def lib():
         so = ctypes.CDLL(out)
     for name in ("gemm_tile", "gemm_one_round", "f32_tile", "f32_sketch_splits", "f32_sketch_fits", "factor_tile", "f32_four_stages"):
         getattr(so, name).argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int]
+    so.split_gemm.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int] * 2 + [ctypes.c_void_p]
+    so.ce_tile.argtypes, so.ce_part_k_tiles.argtypes = [ctypes.c_int64] * 3, [ctypes.c_int64]
     so.sketch.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int, ctypes.c_void_p]
     so.f32_shared_launch.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int]
     return so
@@ -101,6 +109,36 @@ def factor_tile(m, n, k, bf16_c=True, added=False):
     """Kernel of a product of two gradient factors."""
     names = ("64x64", "128x64", "128x128", "192x128", "three-stage", "persistent", "")
     return names[lib().factor_tile(m, n, k, int(bf16_c) + 2 * int(added))] or gemm_tile(m, n, k, added or not bf16_c)[0]
+
+
+Split = collections.namedtuple("Split", "tile one_round parts k_per_part")
+GEMM_TILES = ("256x256", "256x192", "192x128", "128x128", "128x64", "64x64")
+
+
+def _split(m, n, k, most, over_tokens, persist):
+    out = (ctypes.c_int64 * 4)()
+    lib().split_gemm(m, n, k, most, int(over_tokens), int(persist), out)
+    return Split(GEMM_TILES[out[0]], bool(out[1]), out[2], out[3])
+
+
+def token_product(m, n, k, float_or_sum=False, parts=True):
+    """The bfloat16 product over k tokens, C [m, n]; float_or_sum: C is float, or added to."""
+    return _split(m, n, k, 64 if parts else 1, True, not float_or_sum and k > 128)
+
+
+def ce_input_gradient(tokens, d, piece):
+    """The bfloat16 product of the logits' gradient with a piece of the vocabulary's matrix."""
+    return _split(tokens, d, piece, 32, False, True)
+
+
+def ce_tile(tokens, columns, d):
+    """Tile of the bfloat16 products that form the logits."""
+    return ("64x128", "128x128", "192x128", "256x256")[lib().ce_tile(tokens, columns, d)]
+
+
+def ce_part_k_tiles(columns):
+    """K tiles of 64 that the persistent kernel runs of a part of so many columns."""
+    return lib().ce_part_k_tiles(columns)
 
 
 Sketch = collections.namedtuple("Sketch", "tuned slab columns tiles splits tokens two_sums room")
