@@ -250,6 +250,8 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
         if not (x.device == weight.device == target.device):
             raise ValueError("x, weight and target must be on one device")
         v, d = weight.shape
+        if x.shape[-1] != d:
+            raise ValueError(f"x has {x.shape[-1]} features, weight {d}")
         x2, w, t = _rows(x, d), _rows(weight, d), _aligned(target.reshape(-1))
         n, dev = x2.shape[0], x.device
         loss = torch.empty(n, dtype=torch.float32, device=dev)

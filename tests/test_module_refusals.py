@@ -1,0 +1,16 @@
+"""What the modules refuse before anything touches a GPU: the calls here are made on the CPU, and none of them gets as far as memory."""
+import pytest
+
+torch = pytest.importorskip("torch")
+ag = pytest.importorskip("paper_2605_01255_amd.autograd", reason="libacc.so not built")
+
+
+@pytest.mark.parametrize("width", [8, 32, 15, 0])
+def test_features_that_are_not_the_matrixs(width):
+    """Rows twice as wide are not two tokens each: there are targets for half of those."""
+    x, w, t = torch.zeros(4, width), torch.zeros(50, 16), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="features"):
+        ag.LinearCrossEntropyFunction.apply(x, w, t)
+    m = ag.LinearCrossEntropy(16, 50, dtype=torch.float32)
+    with pytest.raises(ValueError, match="features"):
+        m(x, t)
