@@ -42,6 +42,8 @@ class CompressedLinearFunction(torch.autograd.Function):
                 factor_sink=None):
         if x.dtype not in _CODES or weight.dtype != x.dtype:
             raise TypeError("x and weight must both be bfloat16 or both float32")
+        if not x.is_cuda or weight.device != x.device or (bias is not None and bias.device != x.device):
+            raise ValueError("x, weight and bias must be on one GPU")
         d_out, d_in = weight.shape
         x2 = x.reshape(-1, d_in)
         if not x2.is_contiguous():

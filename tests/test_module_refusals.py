@@ -14,3 +14,17 @@ def test_features_that_are_not_the_matrixs(width):
     m = ag.LinearCrossEntropy(16, 50, dtype=torch.float32)
     with pytest.raises(ValueError, match="features"):
         m(x, t)
+
+
+@pytest.mark.parametrize("compressor", ["rp", "rsvd", "e4m3", "int8"])
+def test_layers_that_are_not_on_a_gpu(compressor):
+    """A pointer into host memory, or into another GPU's, is none that a kernel may be given."""
+    x, w = torch.zeros(8, 16), torch.zeros(24, 16)
+    with pytest.raises(ValueError, match="one GPU"):
+        ag.CompressedLinearFunction.apply(x, w, None, 8, 0, compressor)
+    with pytest.raises(ValueError, match="one GPU"):
+        ag.CompressedLinearFunction.apply(x, w.to("meta"), None, 8, 0, compressor)
+    with pytest.raises(ValueError):
+        ag.LinearCrossEntropyFunction.apply(x, w, torch.zeros(8, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        ag.CompressedSwiGLUFunction.apply(x)
