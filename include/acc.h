@@ -332,7 +332,8 @@ int acc_gated_bwd_act8(const acc_gated_desc* desc, const void* dH, const void* Q
  * The backward call forms the logits again, piece by piece.  bfloat16: products of bfloat16 operands accumulated in float, dz
  * rounded to bfloat16 as their operand, dX and dW rounded once.  float: float throughout.
  *   targets [n]  int64, device.  Negative: the token has no loss (loss and stats 0, a zero row of dX, no part in dW, and what its row
- *                of X holds, infinities and NaN included, is not read into any sum).  v and above: loss NaN, no gradient.
+ *                of X holds, infinities and NaN included, is not read into any sum).  v and above: loss NaN, no gradient
+ *                (in the backward call as a token without a loss).
  *   loss [n]     float;  stats [2, n] float: lse, then the target's logit, which the backward call reads.
  *   dloss [n]    float, the gradient of every token's loss (1 / tokens with a loss for their mean).
  * n above 2^18, X of more than 2 GiB, or n times v above 2^35 is worked off in runs of tokens, and a bfloat16 dW is then rounded

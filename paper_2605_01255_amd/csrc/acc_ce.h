@@ -3,7 +3,8 @@
 //   dX = dz . W,  dW = dz^T . X.
 //
 // Tokens without a loss (negative targets) take no part: the others are gathered into a dense matrix first, so that products cost what
-// the tokens with a loss cost, and infinities or NaN in a padded token's row reach no sum (0 times NaN is NaN).
+// the tokens with a loss cost, and infinities or NaN in a padded token's row reach no sum (0 times NaN is NaN).  Nor do, in the
+// backward pass, tokens whose target lies beyond the vocabulary: their loss is NaN and they have no gradient.
 #pragma once
 #include "acc_common.h"
 #include "acc_gemm_ce.h"
@@ -21,19 +22,21 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// What a call knows of its tokens.  `order` lists the tokens with a loss in their order, then the others; null: all tokens as they
-// come.
+// What a call knows of its tokens.  `order` lists those that take part (with a loss; in a backward call with a gradient) in their order,
+// then the others; null: all tokens as they come.
 struct CeTokens {
   const int64_t* targets;   // [n]
   int n;
+  int64_t last;             // targets beyond take no part: none in a forward call, those beyond the vocabulary in a backward one
   int* order;               // [n]
-  int* count;               // tokens with a loss
+  int* count;               // tokens that take part
+  __device__ __forceinline__ bool takes_part(int64_t target) const { return target >= 0 && target <= last; }
   __device__ __forceinline__ int token(int64_t r) const { return order ? order[r] : (int)r; }
-  __device__ __forceinline__ bool lives(int64_t r) const { return order ? r < *count : r < n && targets[r] >= 0; }
+  __device__ __forceinline__ bool lives(int64_t r) const { return order ? r < *count : r < n && takes_part(targets[r]); }
 };
 
 // One work-group of 1024 threads, eight tokens of a thread at a time; the others fill the list from its end.
-// largest (with dloss, backward): the largest magnitude among the incoming gradients of tokens with a loss, 1 if there is none.  dz is
+// largest (with dloss, backward): the largest magnitude among the incoming gradients of the tokens that take part, 1 if there is none.  dz is
 // formed in units of it: the tokens' gradients are one value as a rule, which as part of dz would be rounded to bfloat16 the same way
 // in every row (an error of up to 2^-8 in the gradients that does not average out), and in its own units is 1.
 __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float* __restrict__ dloss, float* __restrict__ largest) {
@@ -57,7 +60,7 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
     int mine = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      keep[k] = target[k] >= 0;
+      keep[k] = t.takes_part(target[k]);
       mine += keep[k] && i0 + k < t.n ? 1 : 0;
     }
     int before = mine;   // inclusive scan over the wave
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
       waves_before += w < wave ? wave_kept[turn][w] : 0;
       total += wave_kept[turn][w];
     }
-    int at = kept + waves_before + before - mine;   // tokens with a loss before this thread's
+    int at = kept + waves_before + before - mine;   // tokens that take part before this thread's
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       if (i0 + k >= t.n) break;
@@ -95,8 +98,8 @@ __global__ __launch_bounds__(1024) void ce_select_kernel(CeTokens t, const float
   }
 }
 
-// What the products and the loss read of a token, in the order of the list; rows behind the last token with a loss are zero, up to
-// 256 of them for the products' least rows.  targets: -1 where there is no gradient.  per_row, in a backward call: lse, the target's
+// What the products and the loss read of a token, in the order of the list; rows behind the last one are zero, up to 256 of them
+// for the products' least rows.  targets: -1 where there is none in the vocabulary.  per_row, in a backward call: lse, the target's
 // logit and the incoming gradient (over *unit), `rows` of each.
 // SELECT: the selection as well, for up to kCeSelectHere tokens: every work-group finds its row's token by itself, from all targets, which
 // saves a launch that takes 4.5 us with the pause behind it.
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int at = i0 + k < t.n ? i0 + k : t.n - 1;
-      keep[k] = t.targets[at] >= 0 && i0 + k < t.n;
+      keep[k] = t.takes_part(t.targets[at]) && i0 + k < t.n;
       mine += keep[k] ? 1 : 0;
       if (unit) {
         const float g = dloss[at];
@@ -145,11 +148,11 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
       top = fmaxf(fmaxf(wave_largest[0], wave_largest[1]), fmaxf(wave_largest[2], wave_largest[3]));
       g_unit = top > 0.f ? top : 1.f;
     }
-    int at = before - mine;   // tokens with a loss before this thread's
+    int at = before - mine;   // tokens that take part before this thread's
 #pragma unroll
     for (int w = 0; w < 3; ++w) at += w < wave ? wave_kept[w] : 0;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {   // the others behind those with a loss
+    for (int k = 0; k < PER; ++k) {   // the others behind those that take part
       if (i0 + k < t.n && (keep[k] ? at : count + i0 + k - at) == r) token = i0 + k;
       at += keep[k] ? 1 : 0;
     }
@@ -173,8 +176,8 @@ __global__ __launch_bounds__(256) void ce_gather_kernel(CeTokens t, const T* __r
     targets[r] = target < V ? target : -1;
     if (stats) {
       per_row[r] = lives ? stats[i] : 0.f;
-      per_row[rows + r] = lives && target < V ? stats[stats_stride + i] : 0.f;
-      per_row[2 * rows + r] = lives && target < V ? dloss[i] / g_unit : 0.f;
+      per_row[rows + r] = lives ? stats[stats_stride + i] : 0.f;
+      per_row[2 * rows + r] = lives ? dloss[i] / g_unit : 0.f;
     }
   }
   if (sizeof(T) == 2 && !lives && r >= 256) return;   // the float32 products read every row

@@ -215,7 +215,7 @@ int plan_ce(const acc_ce_desc* d, CePlan* p) {
   if (p->run > by_strips) p->run = by_strips;
   if (p->run > p->n) p->run = p->n;
   p->rows = p->run < 256 ? 256 : p->run;
-  // rows of dz that are there whatever the number of tokens with a loss, zeros behind them: what the product over the tokens takes at
+  // rows of dz that are there whatever the number of tokens that take part, zeros behind them: what the product over the tokens takes at
   // least, three K tiles where it may run on the persistent kernel
   p->least_rows = p->run <= 128 ? 64 : 192;
   // a piece: at most kCePieceBytes of dz, and of W what a buffer resource reaches
@@ -279,18 +279,20 @@ struct CeRun {
   int64_t piece(int64_t v0) const { return p.v - v0 < p.vp ? p.v - v0 : p.vp; }
 };
 
-template <typename F> int ce_runs(const acc_ce_desc* desc, const CePlan& p, const int64_t* targets, void* workspace, hipStream_t stream, F&& f) {
+// last: as in CeTokens.
+template <typename F>
+int ce_runs(const acc_ce_desc* desc, const CePlan& p, const int64_t* targets, int64_t last, void* workspace, hipStream_t stream, F&& f) {
   Launcher L{stream};
   char* ws = (char*)workspace;
   for (int64_t t0 = 0; t0 < p.n; t0 += p.run) {
     const int64_t n = p.n - t0 < p.run ? p.n - t0 : p.run;
-    const CeRun run{desc, p, ws, t0, n, CeTokens{targets + t0, (int)n, (int*)(ws + p.order), (int*)(ws + p.count)}};
+    const CeRun run{desc, p, ws, t0, n, CeTokens{targets + t0, (int)n, last, (int*)(ws + p.order), (int*)(ws + p.count)}};
     f(run, L);
   }
   return L.status();
 }
 
-// The tokens with a loss, and what is read of them, into dense matrices.
+// The tokens that take part, and what is read of them, into dense matrices.
 void ce_gather(const CeRun& r, const void* X, const float* stats, const float* dloss, Launcher& L) {
   float* unit = (float*)(r.ws + r.p.unit);
   const bool units = dloss && r.desc->io_dtype == ACC_BF16;
@@ -519,7 +521,7 @@ int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, con
   if (!aligned16(X) || !aligned16(W) || !aligned16(targets) || !aligned16(loss) || !aligned16(stats) || !aligned16(workspace)) return ACC_ERR_ALIGN;
   if (!workspace || ws_bytes < p.forward) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
-  return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
+  return ce_runs(desc, p, targets, INT64_MAX, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
     float* per_row = (float*)(r.ws + r.p.per_row);
     if (desc->io_dtype == ACC_BF16) {
       // Where one tile of the product holds all tokens nothing is saved by leaving some out.  (A token's logits are its own, so what
@@ -560,7 +562,7 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
   if (!workspace || ws_bytes < p.backward) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
   const bool b16 = desc->io_dtype == ACC_BF16;
-  return ce_runs(desc, p, targets, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
+  return ce_runs(desc, p, targets, p.v - 1, workspace, (hipStream_t)stream, [&](const CeRun& r, Launcher& L) {
     ce_gather(r, X, stats, dloss, L);
     float* per_row = (float*)(r.ws + r.p.per_row);
     float* dxf = (float*)(r.ws + r.p.dx);
