@@ -260,12 +260,12 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(CeTokens t, const f
   }
 }
 
-// dz of one piece from its logits, in place, one work-group per row; rows without a token and columns from vp to ldz are zero.  A
-// target beyond the vocabulary has no gradient.
+// dz of one piece from its logits, in place, one work-group per row; rows without a token and columns from vp to ldz are zero.  A row
+// whose log-sum-exp is not finite gets NaN: its exponentials would be 0 wherever the logits are finite.
 __global__ __launch_bounds__(256) void ce_piece_grad_kernel(CeTokens t, float* __restrict__ Z, int64_t ldz, int64_t v0, int vp, int64_t rows,
                                                             const int64_t* __restrict__ targets, const float* __restrict__ per_row) {
   const int64_t r = blockIdx.x, target = targets[r];   // -1 where there is no token or no gradient
-  const float lse = per_row[r], zt = per_row[rows + r], g = per_row[2 * rows + r];
+  const float lse = per_row[r], zt = per_row[rows + r], g = isfinite(lse) ? per_row[2 * rows + r] : NAN;
   const float own = g * expm1f(zt - lse);
   for (int64_t c = 4 * threadIdx.x; c < ldz; c += 1024) {
     f32x4 x = *(const f32x4*)(Z + r * ldz + c);

@@ -24,3 +24,32 @@ def test_rows_whose_target_lies_beyond_the_vocabulary_reach_no_gradient(acc, n, 
     for a, b in zip(clean, c.backward(stats)):
         assert torch.equal(a, b)
     assert not c.backward(stats)[0][beyond].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,piece", [(40, 0), (333, 256)])
+@pytest.mark.parametrize("what", ["infinite logit", "NaN in its row", "nothing but minus infinity"])
+def test_a_log_sum_exp_that_is_not_finite_makes_its_gradients_nan(acc, n, piece, what, dtype):  # noqa: F811
+    """One token's row; the input gradients of the others stay as they are, bit for bit."""
+    import torch
+    c = Case(acc, n, 64, 600, dtype, piece=piece)
+    c.X[:, 0] = 0.0
+    c.W[:, 0] = 0.0
+    c.targets[9] = 3
+    clean = c.backward(c.forward()[1])
+    if what == "infinite logit":        # of column 11 alone; its other logits are finite
+        c.X[9, 0] = 3e38
+        c.W[11, 0] = 16.0
+    elif what == "NaN in its row":
+        c.X[9, 5] = float("nan")
+    else:
+        c.X[9, 0] = -3e38
+        c.W[:, 0] = 16.0
+    loss, stats = c.forward()
+    assert not bool(torch.isfinite(stats[0, 9])) and not bool(torch.isfinite(loss[9])) and int((~torch.isfinite(loss)).sum()) == 1
+    dX, dW = c.backward(stats)
+    assert bool(torch.isnan(dX[9]).all()) and bool(torch.isnan(dW).all())
+    if what == "NaN in its row":        # W is the same
+        others = torch.arange(n, device="cuda") != 9
+        assert torch.equal(dX[others], clean[0][others])
+    assert int(torch.isnan(dX).any(1).sum()) == 1
