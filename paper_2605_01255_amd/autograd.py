@@ -12,6 +12,7 @@ library, importing `binding` raises.
 from __future__ import annotations
 
 import itertools
+from typing import Optional
 
 import torch
 
@@ -138,14 +139,19 @@ class CompressedLinearFunction(torch.autograd.Function):
 class CompressedLinear(torch.nn.Module):
     """Drop-in for torch.nn.Linear (same parameter names and layout) that keeps only the compressed input
     for the backward pass.  Each forward call draws a fresh sketch seed from a per-module counter.  `rank` is that of the
-    "rp" and "rsvd" compressors; "e4m3" and "int8" have none."""
+    "rp" and "rsvd" compressors, which need one; "e4m3" and "int8" have none."""
 
-    def __init__(self, in_features: int, out_features: int, rank: int = 0, bias: bool = True, compressor: str = "rp",
+    def __init__(self, in_features: int, out_features: int, rank: Optional[int] = None, bias: bool = True, compressor: str = "rp",
                  seed: int = 0, power_iters: int = 0, device=None, dtype=torch.bfloat16, factored_grad: bool = False):
         super().__init__()
+        if compressor not in _FORMATS:
+            if rank is None:
+                raise TypeError(f"compressor '{compressor}' needs a rank")
+            if rank <= 0:
+                raise ValueError("rank must be positive")
         self.factored_grad = factored_grad
         self.grad_factors = None   # (left [in, rank], gr [out, rank]) of the last backward pass when factored_grad
-        self.in_features, self.out_features, self.rank = in_features, out_features, rank
+        self.in_features, self.out_features, self.rank = in_features, out_features, rank or 0
         self.compressor, self.power_iters = compressor, power_iters
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device, dtype=dtype))
         if bias:

@@ -28,3 +28,17 @@ def test_layers_that_are_not_on_a_gpu(compressor):
         ag.LinearCrossEntropyFunction.apply(x, w, torch.zeros(8, dtype=torch.int64))
     with pytest.raises(ValueError):
         ag.CompressedSwiGLUFunction.apply(x)
+
+
+def test_low_rank_compressors_need_a_rank():
+    for compressor in ("rp", "rsvd"):
+        with pytest.raises(TypeError, match="rank"):
+            ag.CompressedLinear(64, 32, compressor=compressor)
+        for rank in (0, -8):
+            with pytest.raises(ValueError, match="rank"):
+                ag.CompressedLinear(64, 32, rank, compressor=compressor)
+        assert ag.CompressedLinear(64, 32, 16, compressor=compressor).rank == 16
+    with pytest.raises(TypeError, match="rank"):
+        ag.CompressedLinear(64, 32)
+    for compressor in ("e4m3", "int8"):
+        assert ag.CompressedLinear(64, 32, compressor=compressor).rank == 0
