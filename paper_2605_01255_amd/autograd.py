@@ -69,6 +69,7 @@ class CompressedLinearFunction(torch.autograd.Function):
             if factor_sink is not None:
                 raise ValueError("an 8-bit checkpoint gives a full weight gradient, not a factored one")
             fmt = _FORMATS[compressor]
+            x2, w = _aligned(x2), _aligned(w)
             q, e = acc.alloc_act8(acc.make_act8_desc(n, d_in, io_dtype=code, format=fmt), dev)
             with torch.cuda.device(dev):
                 acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, q, e)

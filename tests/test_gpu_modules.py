@@ -20,3 +20,22 @@ def test_a_layer_on_two_devices_is_refused(mods, compressor):
     for args in ((x, w.cpu(), None), (x.cpu(), w, None), (x, w, torch.zeros(24))):
         with pytest.raises(ValueError, match="one GPU"):
             ag.CompressedLinearFunction.apply(*args, 8, 0, compressor)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_slices_that_are_not_aligned_for_the_8_bit_layer(mods, dtype, fmt):
+    """An input and a weight that start inside a longer vector, against copies of them."""
+    torch, ag = mods
+    tdt = getattr(torch, dtype)
+    torch.manual_seed(0)
+    xs, ws, g = (torch.randn(k, device="cuda").to(tdt) for k in (77 * 72 + 1, 40 * 72 + 3, 77 * 40))
+    assert xs[1:].data_ptr() % 16 and ws[3:].data_ptr() % 16
+    got = []
+    for x, w in ((xs[1:], ws[3:]), (xs[1:].clone(), ws[3:].clone())):
+        x, w = x.reshape(7, 11, 72).detach().requires_grad_(), w.reshape(40, 72).detach().requires_grad_()
+        y = ag.CompressedLinearFunction.apply(x, w, None, 0, 0, fmt)
+        y.backward(g.reshape(7, 11, 40))
+        got.append((y.detach(), x.grad, w.grad))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
