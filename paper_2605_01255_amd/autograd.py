@@ -71,8 +71,9 @@ class CompressedLinearFunction(torch.autograd.Function):
             fmt = _FORMATS[compressor]
             x2, w = _aligned(x2), _aligned(w)
             q, e = acc.alloc_act8(acc.make_act8_desc(n, d_in, io_dtype=code, format=fmt), dev)
-            with torch.cuda.device(dev):
-                acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, q, e)
+            if n:
+                with torch.cuda.device(dev):
+                    acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, q, e)
             ctx.save_for_backward(w, q, e)
         else:
             raise ValueError("compressor must be 'rp', 'rsvd', 'e4m3' or 'int8'")
@@ -123,6 +124,10 @@ class CompressedLinearFunction(torch.autograd.Function):
         dy2 = _aligned(dy2)
         dev, dt = dy2.device, dy2.dtype
         want_dx, want_dw = ctx.needs_input_grad[:2]
+        want_db = has_bias and ctx.needs_input_grad[2]
+        if n == 0:
+            return (dy2.new_empty(x_shape) if want_dx else None, dy2.new_zeros(d_out, d_in) if want_dw else None,
+                    dy2.new_zeros(d_out) if want_db else None, None, None, None, None, None)
         desc = acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=acc.ACC_FLAG_W_OUT_IN)
         dx = torch.empty(n, d_in, dtype=dt, device=dev) if want_dx else None
         dw = torch.empty(d_out, d_in, dtype=dt, device=dev) if want_dw else None
@@ -131,7 +136,7 @@ class CompressedLinearFunction(torch.autograd.Function):
             if want_dx or want_dw:
                 ws = _workspace(acc.acc_linear_act8_workspace_bytes(desc), dev) if want_dw else None
                 acc.acc_linear_bwd_act8(desc, _FORMATS[compressor], dy2, w, q, e, dx, dw, ws)
-            if has_bias and ctx.needs_input_grad[2]:
+            if want_db:
                 db = torch.empty(d_out, dtype=dt, device=dev)
                 acc.acc_linear_bias_grad(desc, dy2, db, _workspace(acc.acc_linear_workspace_bytes(desc, True), dev))
         return None if dx is None else dx.reshape(x_shape), dw, db, None, None, None, None, None

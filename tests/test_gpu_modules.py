@@ -39,3 +39,21 @@ def test_slices_that_are_not_aligned_for_the_8_bit_layer(mods, dtype, fmt):
         got.append((y.detach(), x.grad, w.grad))
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_an_empty_batch_for_the_8_bit_layer(mods, fmt, bias):
+    torch, ag = mods
+    lin = ag.CompressedLinear(72, 40, bias=bias, compressor=fmt, device="cuda")
+    x = torch.zeros(3, 0, 72, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    y = lin(x)
+    assert y.shape == (3, 0, 40) and y.dtype == torch.bfloat16
+    y.sum().backward()
+    assert x.grad.shape == (3, 0, 72) and lin.weight.grad.shape == (40, 72) and not lin.weight.grad.any()
+    if bias:
+        assert lin.bias.grad.shape == (40,) and not lin.bias.grad.any()
+    with torch.no_grad():
+        lin.weight.grad = None
+    lin(x.detach()).sum().backward()
+    assert not lin.weight.grad.any()
