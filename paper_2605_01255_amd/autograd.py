@@ -32,7 +32,7 @@ class CompressedLinearFunction(torch.autograd.Function):
     compressor "rp": the seeded Gaussian token sketch (unbiased; keeps Xs [in_features, rank] + the seed);
     compressor "rsvd": randomized range finder + projection (keeps U [tokens, rank] and V [in_features, rank]);
     compressor "e4m3" or "int8": an 8-bit checkpoint of the whole input (1 + 1 / 32 bytes per element, `rank` unused), from
-    which the weight gradient is formed in full.
+    which the weight gradient is formed in full; none is made for a weight that requires no gradient.
     `seed` must differ from call to call for the random projection to be unbiased over a training run.
     Linears that share an input (q/k/v, gate/up; Sec. 5.1) are compressed once by stacking their weights
     into one call.
@@ -70,11 +70,14 @@ class CompressedLinearFunction(torch.autograd.Function):
                 raise ValueError("an 8-bit checkpoint gives a full weight gradient, not a factored one")
             fmt = _FORMATS[compressor]
             x2, w = _aligned(x2), _aligned(w)
-            q, e = acc.alloc_act8(acc.make_act8_desc(n, d_in, io_dtype=code, format=fmt), dev)
+            if ctx.needs_input_grad[1]:
+                kept = acc.alloc_act8(acc.make_act8_desc(n, d_in, io_dtype=code, format=fmt), dev)
+            else:   # nothing is kept for a weight gradient that nobody forms
+                kept, flags = (), flags | acc.ACC_FLAG_SKIP_SKETCH
             if n:
                 with torch.cuda.device(dev):
-                    acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, q, e)
-            ctx.save_for_backward(w, q, e)
+                    acc.acc_linear_fwd_act8(acc.make_desc(n, d_in, d_out, 8, io_dtype=code, flags=flags), fmt, x2, w, y, *(kept or (None, None)))
+            ctx.save_for_backward(w, *kept)
         else:
             raise ValueError("compressor must be 'rp', 'rsvd', 'e4m3' or 'int8'")
         if bias is not None:
@@ -120,7 +123,8 @@ class CompressedLinearFunction(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def _backward_act8(ctx, dy2):
         compressor, n, d_in, d_out, _, _, code, has_bias, x_shape = ctx.meta
-        w, q, e = ctx.saved_tensors
+        w, *kept = ctx.saved_tensors
+        q, e = kept or (None, None)
         dy2 = _aligned(dy2)
         dev, dt = dy2.device, dy2.dtype
         want_dx, want_dw = ctx.needs_input_grad[:2]
@@ -168,7 +172,9 @@ class CompressedLinear(torch.nn.Module):
         self._seeds = itertools.count(int(seed) << 20)
 
     def forward(self, x):
-        return CompressedLinearFunction.apply(x, self.weight, self.bias, self.rank, next(self._seeds),
+        # (the function sees its weight's requires_grad, not whether gradients are recorded at all)
+        weight = self.weight if torch.is_grad_enabled() else self.weight.detach()
+        return CompressedLinearFunction.apply(x, weight, self.bias, self.rank, next(self._seeds),
                                               self.compressor, self.power_iters,
                                               self if self.factored_grad else None)
 

@@ -57,3 +57,32 @@ def test_an_empty_batch_for_the_8_bit_layer(mods, fmt, bias):
         lin.weight.grad = None
     lin(x.detach()).sum().backward()
     assert not lin.weight.grad.any()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_no_checkpoint_is_kept_for_a_gradient_that_nobody_forms(mods, fmt, monkeypatch):
+    """A frozen weight's layer keeps the weight alone, an evaluation pass makes no checkpoint; outputs and input gradients stay."""
+    torch, ag = mods
+    torch.manual_seed(0)
+    lin = ag.CompressedLinear(136, 264, compressor=fmt, device="cuda")
+    x, g = (torch.randn(77, k, device="cuda", dtype=torch.bfloat16) for k in (136, 264))
+    a = x.clone().requires_grad_()
+    y = lin(a)
+    y.backward(g)
+    db = lin.bias.grad
+    lin.bias.grad = None
+
+    def none(*args, **kw):
+        raise AssertionError("a checkpoint was made")
+
+    monkeypatch.setattr(ag.acc, "alloc_act8", none)
+    lin.weight.requires_grad_(False)
+    b, saved = x.clone().requires_grad_(), []
+    with torch.autograd.graph.saved_tensors_hooks(lambda z: (saved.append((tuple(z.shape), z.dtype)), z)[1], lambda z: z):
+        y2 = lin(b)
+    assert saved == [((264, 136), torch.bfloat16)]
+    y2.backward(g)
+    assert torch.equal(y, y2) and torch.equal(a.grad, b.grad) and torch.equal(db, lin.bias.grad)
+    lin.weight.requires_grad_(True)
+    with torch.no_grad():
+        assert torch.equal(y, lin(x))
