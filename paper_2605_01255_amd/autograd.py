@@ -301,10 +301,11 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
             return (torch.empty(shape, dtype=w.dtype, device=dev) if want_dx else None,
                     torch.zeros(v, d, dtype=w.dtype, device=dev) if want_dw else None, None)
         _, x2, t, stats = ctx.saved_tensors
+        if want_dx:   # the call has one row stride for x and dx: dense rows of both, or the gradient would hold the gaps too
+            x2 = x2.contiguous()
         desc = LinearCrossEntropyFunction._desc(ctx, x2, w)
         g = _aligned(dloss.reshape(-1).to(torch.float32))
-        ldx = x2.stride(0) if n > 1 else d
-        dx = torch.empty(n, ldx, dtype=w.dtype, device=dev)[:, :d] if want_dx else None   # rows as far apart as x's
+        dx = torch.empty(n, d, dtype=w.dtype, device=dev) if want_dx else None
         dw = torch.empty(v, d, dtype=w.dtype, device=dev) if want_dw else None
         with torch.cuda.device(dev):
             acc.acc_linear_ce_bwd(desc, x2, w, t, stats, g, dx, dw, _workspace(acc.acc_linear_ce_workspace_bytes(desc, True), dev))

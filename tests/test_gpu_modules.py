@@ -86,3 +86,20 @@ def test_no_checkpoint_is_kept_for_a_gradient_that_nobody_forms(mods, fmt, monke
     lin.weight.requires_grad_(True)
     with torch.no_grad():
         assert torch.equal(y, lin(x))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_the_cross_entropys_input_gradient_holds_no_more_than_it_is(mods, dtype):
+    """Of rows far apart: the gradient's memory is that of its elements, its bits those for dense rows."""
+    torch, ag = mods
+    torch.manual_seed(0)
+    tdt = getattr(torch, dtype)
+    wide, w = torch.randn(50, 4096, device="cuda").to(tdt), torch.randn(301, 72, device="cuda").to(tdt)
+    t = torch.randint(0, 301, (50,), device="cuda")
+    got = []
+    for x in (wide[:, :72], wide[:, :72].contiguous()):
+        x = x.detach().requires_grad_()
+        (dx,) = torch.autograd.grad(ag.LinearCrossEntropyFunction.apply(x, w, t).sum(), x)
+        assert dx.is_contiguous() and dx.untyped_storage().nbytes() == 50 * 72 * dx.element_size()
+        got.append(dx)
+    assert torch.equal(*got)
