@@ -307,8 +307,9 @@ int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY,
 /* The gated activation of an MLP with 8-bit checkpoints of its two inputs, the largest activations of a layer:
  *   H = silu(G) o U,  silu(g) = g / (1 + exp(-g));  Qg, Eg and Qu, Eu are the checkpoints of G and U [n, f]
  *   dU = dH o silu(G^);  dG = dH o U^ o s (1 + G^ (1 - s)),  s = 1 / (1 + exp(-G^))
- * and, where H != NULL in the backward call, H = silu(G^) o U^ again: the input of the product behind it, whose weight gradient
- * then needs nothing kept of its own.  G, U, dG and dU [n, ldg] may be two halves of the rows of one matrix (ldg = 2 f);
+ * and, where H != NULL in the backward call, H = silu(G^) o U^ again: the input of the product behind it.  acc_act8_pack makes of it
+ * the checkpoint that acc_linear_bwd_act8 reads for that product's weight gradient, for which nothing is then kept between the passes
+ * (it is the gradient for H of the checkpoints, not for the H of the forward call).  G, U, dG and dU [n, ldg] may be two halves of the rows of one matrix (ldg = 2 f);
  * H and dH are [n, ldh].  Outputs overlap no inputs.  Float arithmetic, one rounding. */
 typedef struct acc_gated_desc {
   int64_t n;         /* tokens, 1 .. 2^30                                                    */
