@@ -9,15 +9,16 @@ pytestmark = pytest.mark.gpu
 
 import plan_util as pu
 
-# rows, columns, tokens; tile, whether it is one round, whether there are parts.  The persistent kernel's form is for a bfloat16 result that
-# is written; the others of its size are in what the 128 x 128 and 192 x 128 tiles are asked for.
+# rows, columns, tokens; tile, whether it is one round, whether there are parts (the persistent kernel, for a bfloat16 result that is
+# written alone: below)
 FORMS = [
     (64, 64, 40, "64x64", True, False), (512, 2056, 40, "64x64", False, False), (64, 64, 2049, "64x64", True, True),
     (136, 2048, 8192, "64x64", False, True), (512, 512, 8192, "64x64", True, True),
     (512, 2056, 300, "128x64", True, False), (1544, 2048, 40, "128x64", False, False), (2048, 136, 8192, "128x64", True, True),
     (4136, 136, 8192, "128x64", False, True), (512, 512, 32768, "128x64", True, True),
     (1024, 4096, 8192, "128x128", True, False), (1544, 4096, 40, "128x128", False, False), (264, 2048, 16384, "128x128", False, True),
-    (1032, 4136, 3387, "192x128", True, False), (136, 4096, 16384, "192x128", True, True),
+    (1032, 4136, 3387, "192x128", True, False), (136, 57176, 40, "192x128", False, False), (136, 4096, 16384, "192x128", True, True),
+    (136, 12072, 7959, "192x128", False, True),
 ]
 
 
