@@ -278,7 +278,7 @@ typedef enum { ACC_ACT8_E4M3 = 0, ACC_ACT8_INT8 = 1 } acc_act8_format;
 typedef struct acc_act8_desc {
   int64_t n;         /* tokens, 1 .. 2^30, and n times c (in whole 64 channels) below 2^37   */
   int64_t c;         /* channels, a multiple of 8, at most 2^21                              */
-  int64_t ldx;       /* row stride of X in elements, a multiple of 8; 0 = c                  */
+  int64_t ldx;       /* row stride of X in elements, a multiple of 8, at most 2^24; 0 = c    */
   int32_t io_dtype;  /* acc_dtype of X                                                       */
   int32_t format;    /* acc_act8_format                                                      */
 } acc_act8_desc;
@@ -291,7 +291,7 @@ int acc_act8_unpack(const acc_act8_desc* desc, const void* Q, const void* E, voi
 /* The linear layer with an 8-bit checkpoint of its input: Y = X.W exact, then Q and E of X [n, d_in] as above
  * (ACC_FLAG_SKIP_SKETCH: linears that share an input keep one checkpoint; Q and E are left alone and may be NULL).
  * Of desc, r, seed, row_offset, ldf and factor_dtype have no meaning here (they must be valid); ACC_FLAG_ONE_LAUNCH is
- * ignored.  No workspace. */
+ * ignored.  No workspace.  Where a checkpoint is written or read n times d_in is bounded as in acc_act8_desc. */
 int acc_linear_fwd_act8(const acc_linear_desc* desc, int format, const void* X, const void* W, void* Y, void* Q, void* E,
                         void* stream);
 
@@ -312,10 +312,10 @@ int acc_linear_bwd_act8(const acc_linear_desc* desc, int format, const void* dY,
  * (it is the gradient for H of the checkpoints, not for the H of the forward call).  G, U, dG and dU [n, ldg] may be two halves of the rows of one matrix (ldg = 2 f);
  * H and dH are [n, ldh].  Outputs overlap no inputs.  Float arithmetic, one rounding. */
 typedef struct acc_gated_desc {
-  int64_t n;         /* tokens, 1 .. 2^30                                                    */
+  int64_t n;         /* tokens, 1 .. 2^30, and n times f (in whole 64 channels) below 2^37   */
   int64_t f;         /* channels, a multiple of 8, at most 2^21                              */
-  int64_t ldg;       /* row stride of G, U, dG and dU in elements, a multiple of 8; 0 = f    */
-  int64_t ldh;       /* row stride of H and dH in elements, a multiple of 8; 0 = f           */
+  int64_t ldg;       /* row stride of G, U, dG and dU in elements, a multiple of 8, at most 2^24; 0 = f */
+  int64_t ldh;       /* row stride of H and dH in elements, likewise; 0 = f                  */
   int32_t io_dtype;  /* acc_dtype of G, U, H, dH, dG and dU                                  */
   int32_t format;    /* acc_act8_format                                                      */
 } acc_gated_desc;

@@ -259,7 +259,9 @@ class CompressedSwiGLU(torch.nn.Module):
 class LinearCrossEntropyFunction(torch.autograd.Function):
     """Per-token softmax cross entropy (float32) of x @ weight.T against `target`, weight [vocabulary, features], without the
     logits (acc_linear_ce_fwd / acc_linear_ce_bwd).  Kept for the backward pass: x, weight, target and two floats a token.
-    Negative targets have no loss and no gradient."""
+    Negative targets have no loss and no gradient, those beyond the vocabulary a loss of NaN and no gradient.  With bfloat16
+    tensors the logits' gradient is rounded to bfloat16 before its products with weight and x; logits, losses and all sums are
+    float32."""
 
     @staticmethod
     def forward(ctx, x, weight, target):
