@@ -84,7 +84,8 @@ __device__ __forceinline__ int swz_n16(int krow) { return ((krow & 3) << 2) | ((
 // at least, the last part what is left): part s is stored at C + s c_split_stride, from the accumulators as they are (64 bytes of a row
 // at a time; staged as float they would need LDS that the stages have).  A part runs its own K tiles (part_k_tiles).  Chunks past the
 // part's end are sent out of range in whichever K tile they lie; of K tiles that start there (a part of one or two has such) those of
-// both operands, by their lane offsets and from scalar offset 0: a scalar offset beyond the range is nothing to rely on.  Against the ring kernel's 128 x 128 tiles, us: 1024 x 4096 by 128000 columns 906 / 1780, 2048 x 2048 by 50257 409 / 661.
+// both operands, by their lane offsets and from scalar offset 0: a scalar offset beyond the range is nothing to rely on.  Against the
+// ring kernel's 128 x 128 tiles, us: 1024 x 4096 by 128000 columns 878 / 1780, 2048 x 2048 by 50257 396 / 661.
 template <bool B_KMAJOR, bool RAGGED_K = false, bool A_KMAJOR = true, Epilogue EPI = Epilogue::kStore, int N1 = 12, int S1 = 4, int S0 = 4>
 __global__ __launch_bounds__(256) void gemm16_persist_kernel(FastGemmParams p, int n_slots) {
   // schedule of k-step 1: the barrier sits before its slot BAR_Q; N1 wave-loads go out after it, one every S1

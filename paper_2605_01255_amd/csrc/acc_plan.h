@@ -108,7 +108,7 @@ static inline FactorTile pick_factor_tile(int64_t M, int64_t N, int64_t K, bool 
 // tiles) and the input gradient of the cross entropy (the vocabulary is its K).  The least of estimates like pick_gemm_tile's, with tiles
 // x parts in the place of tiles, and for more than one part the launch that adds them up and their bytes, written and read at 4 TB/s.
 // A part has four K tiles at least.  Two operands that stay in no cache come through the L2s at 9.5 TB/s, which is what the smaller tiles
-// of the input gradient wait for (1024 x 4096 by 128000 columns on 128 x 128, 16.8 GB: 1780 us; on the persistent kernel 906).
+// of the input gradient wait for (1024 x 4096 by 128000 columns on 128 x 128, 16.8 GB: 1780 us; on the persistent kernel 878).
 // over_tokens: both operands are read transposed, at half the rate from LDS, which the smaller wave tiles wait for (2048 x 2048 over
 // 32768 tokens on 128 x 128, one work-group per compute unit: 0.63 us a K tile, where a K-contiguous operand takes 0.37; two work-groups
 // cover each other's: 297 us in four parts, 323 in one).  Measured us there on 256 x 256 / 192 x 128 / 128 x 128 / 128 x 64 / 64 x 64
