@@ -363,6 +363,56 @@ int acc_linear_ce_fwd(const acc_ce_desc* desc, const void* X, const void* W, con
 int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, const int64_t* targets, const float* stats,
                       const float* dloss, void* dX, void* dW, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- Attention over packed documents --------------------------------------------------------------------
+ * The operator between a decoder layer's projections.  Rows are tokens, several documents one after another; head h of a row is its
+ * columns h d .. h d + d - 1, so Q, K and V may be column blocks of one projection's rows, and dQ, dK and dV of its gradient's.
+ * Query heads share key heads in runs of heads / kv_heads.
+ *   z_ij = f(scale q_i.k_j) - slope_h |i - j|,  f(x) = cap tanh(x / cap), or x where cap is 0
+ *   lse_i = log sum_j exp z_ij over the keys j that i sees;  P_ij = exp(z_ij - lse_i);  O = P.V
+ *   dV = P^T.dO;  dS = P o (dO.V^T - delta) o f',  delta_i = dO_i.O_i;  dQ = scale dS.K;  dK = scale dS^T.Q   (summed over shared heads)
+ * Query i sees the keys of its own document; with ACC_ATTN_CAUSAL of those the ones with j <= i (with `window` also i - j < window)
+ * and, where `prefix` is given, the document's first prefix[document] tokens.
+ *   starts [docs + 1]  int64, device, ascending, of [0, n]: document e has the rows starts[e] .. starts[e + 1] - 1 and may have none.  NULL
+ *                      (docs 0): sequences of `seq` rows, the last one of what is left.  Rows of no document (before starts[0], from
+ *                      starts[docs] on) see nothing and are seen by none: their rows of O, dQ, dK and dV are zeros, their lse -infinity, and
+ *                      what their rows of Q, K, V and dO hold is not read.  Where the numbers do not ascend or lie outside [0, n] rows may
+ *                      stay unwritten; nothing else is touched.
+ *   prefix [documents] int64, device, or NULL; larger numbers mean the whole document, negative ones nothing.  Not with a window.
+ *   slopes [heads]     float, device, or NULL: no bias.  They get no gradient.
+ *   lse [heads, n]     float, which the backward call reads.
+ * What is not finite in a document's rows reaches its own rows only.  bfloat16: products of bfloat16 operands accumulated in float, softmax in
+ * float; P and dS are rounded to bfloat16 as operands of the products behind them, O, dQ, dK and dV once.  float: float throughout.
+ * The sums are taken in a fixed order. */
+#define ACC_ATTN_CAUSAL 1u
+typedef struct acc_attn_desc {
+  int64_t n;         /* rows, 1 .. 2^30                                                      */
+  int64_t heads;     /* query heads, a multiple of kv_heads, at most 2^15                    */
+  int64_t kv_heads;  /* key and value heads                                                  */
+  int64_t d;         /* channels of a head, a multiple of 8, at most 128                     */
+  int64_t ldq;       /* row stride of Q and dQ in elements, a multiple of 8, at most 2^18; 0 = heads d */
+  int64_t ldk;       /* of K and dK, likewise; 0 = kv_heads d                                */
+  int64_t ldv;       /* of V and dV, likewise; 0 = kv_heads d                                */
+  int64_t ldo;       /* of O and dO, likewise; 0 = heads d                                   */
+  int64_t docs;      /* documents of `starts`; 0: sequences of `seq` rows                    */
+  int64_t seq;       /* rows of a sequence, 0 = n; 0 where there are documents               */
+  int64_t window;    /* keys that a query sees at most, with ACC_ATTN_CAUSAL; 0 = no limit   */
+  float scale;       /* of the products, not negative; 0 = 1 / sqrt(d)                       */
+  float cap;         /* not negative; 0 = none                                               */
+  int32_t io_dtype;  /* acc_dtype of Q, K, V, O and their gradients                          */
+  uint32_t flags;    /* ACC_ATTN_CAUSAL                                                      */
+} acc_attn_desc;
+
+/* Bytes of device workspace of the forward (is_backward == 0; it may be 0) or backward call; 0 = invalid. */
+size_t acc_attn_workspace_bytes(const acc_attn_desc* desc, int is_backward);
+
+/* O [n, ldo] and lse are overwritten. */
+int acc_attn_fwd(const acc_attn_desc* desc, const void* Q, const void* K, const void* V, const int64_t* starts, const int64_t* prefix,
+                 const float* slopes, void* O, float* lse, void* workspace, size_t ws_bytes, void* stream);
+/* O and lse as acc_attn_fwd left them for the same inputs.  dQ [n, ldq], dK [n, ldk] and dV [n, ldv] are overwritten. */
+int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const void* V, const int64_t* starts, const int64_t* prefix,
+                 const float* slopes, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* workspace,
+                 size_t ws_bytes, void* stream);
+
 /* Test hook: the Philox integer stream behind S.  out is a device array of
  * ceil(n/4) * r * 4 uint32 laid out [token group q][column j][word w]. */
 int acc_philox_dump_u32(uint64_t seed, uint64_t row_offset, int64_t n, int64_t r, uint32_t* out,

@@ -23,6 +23,7 @@ ACC_STATIC_SCRATCH_BYTES = 32 << 20
 ACC_FP8_E4M3, ACC_FP8_E5M2 = 0, 1
 ACC_ACT8_BLOCK = 32
 ACC_ACT8_E4M3, ACC_ACT8_INT8 = 0, 1
+ACC_ATTN_CAUSAL = 1
 
 EXPORTS = ("acc_linear_workspace_bytes", "acc_linear_fwd", "acc_linear_fwd_static", "acc_linear_bwd", "acc_linear_dw",
            "acc_linear_fwd_fp8", "acc_linear_bwd_fp8",
@@ -32,6 +33,7 @@ EXPORTS = ("acc_linear_workspace_bytes", "acc_linear_fwd", "acc_linear_fwd_stati
            "acc_act8_pack", "acc_act8_unpack", "acc_linear_fwd_act8", "acc_linear_act8_workspace_bytes",
            "acc_linear_bwd_act8", "acc_gated_fwd_act8", "acc_gated_bwd_act8",
            "acc_linear_ce_workspace_bytes", "acc_linear_ce_fwd", "acc_linear_ce_bwd",
+           "acc_attn_workspace_bytes", "acc_attn_fwd", "acc_attn_bwd",
            "acc_philox_dump_u32", "acc_probe_mfma",
            "acc_sketch_dump", "acc_status_string", "acc_version")
 
@@ -69,6 +71,14 @@ class AccCeDesc(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("d", ctypes.c_int64), ("v", ctypes.c_int64), ("ldx", ctypes.c_int64),
                 ("ldw", ctypes.c_int64), ("piece", ctypes.c_int64), ("io_dtype", ctypes.c_int32),
                 ("dw_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class AccAttnDesc(ctypes.Structure):
+    """Mirror of `acc_attn_desc`."""
+    _fields_ = [("n", ctypes.c_int64), ("heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64),
+                ("docs", ctypes.c_int64), ("seq", ctypes.c_int64), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float), ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class AccError(RuntimeError):
@@ -138,6 +148,13 @@ _lib.acc_linear_ce_fwd.restype = ctypes.c_int
 _lib.acc_linear_ce_fwd.argtypes = [_cdp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.acc_linear_ce_bwd.restype = ctypes.c_int
 _lib.acc_linear_ce_bwd.argtypes = [_cdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_tdp = ctypes.POINTER(AccAttnDesc)
+_lib.acc_attn_workspace_bytes.restype = _sz
+_lib.acc_attn_workspace_bytes.argtypes = [_tdp, ctypes.c_int]
+_lib.acc_attn_fwd.restype = ctypes.c_int
+_lib.acc_attn_fwd.argtypes = [_tdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.acc_attn_bwd.restype = ctypes.c_int
+_lib.acc_attn_bwd.argtypes = [_tdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.acc_philox_dump_u32.restype = ctypes.c_int
 _lib.acc_philox_dump_u32.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, _vp, _vp]
 _lib.acc_sketch_dump.restype = ctypes.c_int
@@ -395,6 +412,32 @@ def acc_linear_ce_bwd(desc, X, W, targets, stats, dloss, dX, dW, workspace, stre
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.acc_linear_ce_bwd(ctypes.byref(desc), _ptr(X), _ptr(W), _ptr(targets), _ptr(stats), _ptr(dloss),
                                   _ptr(dX), _ptr(dW), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def make_attn_desc(n, heads, kv_heads, d, ldq=0, ldk=0, ldv=0, ldo=0, docs=0, seq=0, window=0, scale=0.0, cap=0.0, io_dtype=ACC_BF16,
+                   flags=ACC_ATTN_CAUSAL) -> AccAttnDesc:
+    return AccAttnDesc(n, heads, kv_heads, d, ldq, ldk, ldv, ldo, docs, seq, window, scale, cap, io_dtype, flags)
+
+
+def acc_attn_workspace_bytes(desc: AccAttnDesc, is_backward: bool) -> int:
+    return int(_lib.acc_attn_workspace_bytes(ctypes.byref(desc), 1 if is_backward else 0))
+
+
+def acc_attn_fwd(desc, Q, K, V, starts, prefix, slopes, O, lse, workspace, stream=None, ws_bytes=None):
+    """Enqueue O and lse of attention over the documents of `starts` (int64; None: sequences of desc.seq rows); prefix (int64) and
+    slopes (float32) may be None."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_attn_fwd(ctypes.byref(desc), _ptr(Q), _ptr(K), _ptr(V), _ptr(starts), _ptr(prefix), _ptr(slopes), _ptr(O), _ptr(lse),
+                             _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def acc_attn_bwd(desc, Q, K, V, starts, prefix, slopes, O, lse, dO, dQ, dK, dV, workspace, stream=None, ws_bytes=None):
+    """Enqueue dQ, dK and dV from what acc_attn_fwd read and wrote, and the gradient of O."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_attn_bwd(ctypes.byref(desc), _ptr(Q), _ptr(K), _ptr(V), _ptr(starts), _ptr(prefix), _ptr(slopes), _ptr(O), _ptr(lse),
+                             _ptr(dO), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def acc_philox_dump_u32(seed, row_offset, n, r, out, stream=None):
