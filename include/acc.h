@@ -413,6 +413,61 @@ int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
                  const float* slopes, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* workspace,
                  size_t ws_bytes, void* stream);
 
+/* ---- The vocabulary's table ------------------------------------------------------------------------------
+ * The lookup at the other end of a model, in the layout of acc_linear_ce_fwd's W, with which it may be tied:
+ *   Y_i = scale W[ids_i];   dW[w] (+)= scale sum of dY_i over the tokens i with ids_i = w, in their order
+ *   ids [n]  int64, device.  Negative: no word (padding): a row of zeros, and its row of dY is not read.  v and above: a row of NaN, no
+ *            gradient.
+ * Float arithmetic, one rounding.  The sums are taken in a fixed order, however often a word occurs. */
+typedef struct acc_embed_desc {
+  int64_t n;         /* tokens, 1 .. 2^30, and n times d below 2^35                          */
+  int64_t d;         /* features, a multiple of 8, at most 2^16                              */
+  int64_t v;         /* words, 1 .. 2^21                                                     */
+  int64_t ldw;       /* row stride of W (and not of dW, which is dense) in elements, a multiple of 8, at most 2^18; 0 = d */
+  int64_t ldy;       /* row stride of Y and dY, likewise; 0 = d                              */
+  float scale;       /* finite                                                               */
+  int32_t io_dtype;  /* acc_dtype of W, Y and dY                                             */
+  int32_t dw_dtype;  /* acc_dtype of dW                                                      */
+  uint32_t flags;    /* ACC_FLAG_DW_ACCUMULATE: dW += (acc_embed_bwd), rows of other words stay as they are */
+  uint32_t reserved; /* 0                                                                    */
+} acc_embed_desc;
+
+int acc_embed_fwd(const acc_embed_desc* desc, const void* W, const int64_t* ids, void* Y, void* stream);
+/* dW [v, d]; without ACC_FLAG_DW_ACCUMULATE zeros for words without a token.  workspace: ws_bytes >= acc_embed_workspace_bytes(desc) (0 = invalid). */
+size_t acc_embed_workspace_bytes(const acc_embed_desc* desc);
+int acc_embed_bwd(const acc_embed_desc* desc, const int64_t* ids, const void* dY, void* dW, void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- The norm over all gradients, and clipping -----------------------------------------------------------
+ * acc_grad_norm: the 2-norm over any number of dense gradients and of gradients that are left as the two factors of acc_linear_bwd,
+ * dW = left.Gr, whose product is not formed: |left.Gr|^2 = sum (left^T.left) o (Gr.Gr^T).
+ *   out[0] = norm;  out[1] = min(1, max_norm / (norm + 1e-6)), NaN where the norm is not a number   (two floats, device)
+ * acc_grad_scale: dst = src times *factor (a float, device: &out[1]), rounded once; dst may be src, and then nothing is written where the
+ * factor is 1.  Of a factored gradient it scales Gr (or left, not both), as a tensor.
+ * Squares of dense gradients are summed in double, so the norm is finite wherever the gradients are; those of factors in float, their
+ * products and everything behind them in double.  The sums are taken in a fixed order.
+ * The tables are read before the call returns; their tensors have no order and may be of any size, dense, aligned to their elements. */
+typedef struct acc_grad_tensor {
+  const void* src;
+  void* dst;         /* of acc_grad_scale                                                    */
+  int64_t count;     /* elements, at most 2^39; 0 = none                                     */
+  int32_t dtype;     /* acc_dtype of src                                                     */
+  int32_t dst_dtype; /* acc_dtype of dst (src's where dst is src)                            */
+} acc_grad_tensor;
+typedef struct acc_grad_factors {
+  const void* left;  /* [d_in, r]                                                            */
+  const void* gr;    /* [r, d_out], or [d_out, r] with ACC_FLAG_W_OUT_IN                     */
+  int64_t d_in, d_out, r;   /* multiples of 8, at most 2^21, 2^21 and 2^13                   */
+  int64_t ldl, ldg;  /* row strides of left and gr in elements, multiples of 8, at most 2^22; 0 = dense rows */
+  int32_t dtype;     /* acc_dtype of both                                                    */
+  uint32_t flags;    /* ACC_FLAG_W_OUT_IN                                                    */
+} acc_grad_factors;
+
+/* Bytes of device workspace of acc_grad_norm; 0 = invalid. */
+size_t acc_grad_norm_workspace_bytes(const acc_grad_tensor* tensors, int64_t count, const acc_grad_factors* factors, int64_t pairs);
+int acc_grad_norm(const acc_grad_tensor* tensors, int64_t count, const acc_grad_factors* factors, int64_t pairs, float max_norm, float* out,
+                  void* workspace, size_t ws_bytes, void* stream);
+int acc_grad_scale(const acc_grad_tensor* tensors, int64_t count, const float* factor, void* stream);
+
 /* Test hook: the Philox integer stream behind S.  out is a device array of
  * ceil(n/4) * r * 4 uint32 laid out [token group q][column j][word w]. */
 int acc_philox_dump_u32(uint64_t seed, uint64_t row_offset, int64_t n, int64_t r, uint32_t* out,

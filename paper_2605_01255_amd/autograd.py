@@ -342,6 +342,196 @@ class LinearCrossEntropy(torch.nn.Module):
         return f"in_features={self.weight.shape[1]}, vocabulary={self.weight.shape[0]}, reduction={self.reduction}"
 
 
+class DocumentAttentionFunction(torch.autograd.Function):
+    """Attention of the rows of x [..., (heads + 2 kv_heads) d] (queries, keys and values side by side, as one projection gives them)
+    within documents (acc_attn_fwd / acc_attn_bwd); the module's docstring has the masks.  Kept for the backward pass: x, the output and a
+    float a row and head."""
+
+    @staticmethod
+    def forward(ctx, x, starts, prefix, slopes, heads: int, kv_heads: int, causal: bool, window: int, cap: float, scale: float):
+        if x.dtype not in _CODES:
+            raise TypeError("x must be bfloat16 or float32")
+        if x.dim() < 2 or x.shape[-1] % (heads + 2 * kv_heads):
+            raise ValueError(f"x must be [..., rows, channels], channels a multiple of {heads + 2 * kv_heads}")
+        if not x.is_cuda or any(t is not None and t.device != x.device for t in (starts, prefix, slopes)):
+            raise ValueError("x and its masks must be on one GPU")
+        if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or slopes.requires_grad):
+            raise ValueError("slopes must be float32, one per query head, and get no gradient")
+        if starts is not None and (starts.dim() != 1 or starts.numel() < 2 or starts.is_floating_point()):
+            raise ValueError("starts must hold the first row of every document and the end of the last")
+        seq = 0 if starts is not None else x.shape[-2]
+        documents = starts.numel() - 1 if starts is not None else x.shape[:-2].numel()
+        if prefix is not None and (prefix.shape != (documents,) or prefix.is_floating_point()):
+            raise ValueError("prefix must have one number per document")
+        width = x.shape[-1]
+        d = width // (heads + 2 * kv_heads)
+        x2 = _rows(x, width)
+        n, dev = x2.shape[0], x.device
+        ctx.meta = (n, heads, kv_heads, d, x.shape, dict(docs=0 if starts is None else documents, seq=seq, window=window, scale=scale, cap=cap,
+                                                         io_dtype=_CODES[x.dtype], flags=acc.ACC_ATTN_CAUSAL if causal else 0))
+        o = torch.empty(n, heads * d, dtype=x.dtype, device=dev)
+        if n == 0:
+            return o.reshape(*x.shape[:-1], heads * d)
+        whole = lambda t, dt: None if t is None else _aligned(t.to(dt))  # noqa: E731
+        masks = whole(starts, torch.int64), whole(prefix, torch.int64), whole(slopes, torch.float32)
+        lse = torch.empty(heads, n, dtype=torch.float32, device=dev)
+        desc = DocumentAttentionFunction._desc(ctx, x2)
+        with torch.cuda.device(dev):
+            acc.acc_attn_fwd(desc, *DocumentAttentionFunction._split(ctx, x2), *masks, o, lse,
+                             _workspace(acc.acc_attn_workspace_bytes(desc, False), dev))
+        ctx.save_for_backward(x2, o, lse, *masks)
+        return o.reshape(*x.shape[:-1], heads * d)
+
+    @staticmethod
+    def _desc(ctx, x2):
+        n, heads, kv_heads, d, _, more = ctx.meta
+        ld = x2.stride(0) if n > 1 else x2.shape[1]
+        return acc.make_attn_desc(n, heads, kv_heads, d, ldq=ld, ldk=ld, ldv=ld, **more)
+
+    @staticmethod
+    def _split(ctx, t):
+        _, heads, kv_heads, d, _, _ = ctx.meta
+        return t.split((heads * d, kv_heads * d, kv_heads * d), 1)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        n, heads, _, d, shape, _ = ctx.meta
+        dev = do.device
+        if n == 0:
+            return (do.new_empty(shape), *[None] * 9)
+        x2, o, lse, *masks = ctx.saved_tensors
+        x2 = x2.contiguous()   # the call has one row stride for x and dx
+        dx = torch.empty_like(x2)
+        do2 = _aligned(do.reshape(n, heads * d))
+        desc = DocumentAttentionFunction._desc(ctx, x2)
+        with torch.cuda.device(dev):
+            acc.acc_attn_bwd(desc, *DocumentAttentionFunction._split(ctx, x2), *masks, o, lse, do2, *DocumentAttentionFunction._split(ctx, dx),
+                             _workspace(acc.acc_attn_workspace_bytes(desc, True), dev))
+        return (dx.reshape(shape), *[None] * 9)
+
+
+class DocumentAttention(torch.nn.Module):
+    """The attention between a decoder layer's projections: [..., (heads + 2 kv_heads) d] -> [..., heads d].
+
+    forward(x) takes x [..., rows, channels] as sequences of their own; forward(x, starts) all its rows as one after another, documents
+    beginning at the rows `starts` holds (int64, the last number is where the last one ends; rows outside give zeros).  A row sees its
+    document's rows up to itself (`causal`), at most `window` of them (0: no limit), and always the document's first `prefix` ones
+    (int64, one number per document).  Scores, times `scale` (None: 1 / sqrt(d)), are capped by cap tanh(score / cap) (0: not), and with
+    `slopes` (float32, one per head; True: 2^(-8 h / heads) for h = 1 .. heads) fall by slope times the distance."""
+
+    def __init__(self, heads: int, kv_heads: Optional[int] = None, causal: bool = True, window: int = 0, cap: float = 0.0, scale: Optional[float] = None,
+                 slopes=None, device=None):
+        super().__init__()
+        kv_heads = heads if kv_heads is None else kv_heads
+        if heads <= 0 or kv_heads <= 0 or heads % kv_heads:
+            raise ValueError("heads must be a multiple of kv_heads")
+        if window < 0 or cap < 0 or (scale is not None and not scale > 0):
+            raise ValueError("window and cap must not be negative, scale must be positive")
+        if window and not causal:
+            raise ValueError("a window needs causal attention")
+        self.heads, self.kv_heads, self.causal, self.window, self.cap, self.scale = heads, kv_heads, causal, window, cap, scale
+        if slopes is True:
+            slopes = 2.0 ** (-8.0 * torch.arange(1, heads + 1, dtype=torch.float32) / heads)
+        self.register_buffer("slopes", None if slopes is None or slopes is False else torch.as_tensor(slopes, dtype=torch.float32).to(device))
+
+    def forward(self, x, starts=None, prefix=None):
+        if prefix is not None and (not self.causal or self.window):
+            raise ValueError("a prefix needs causal attention without a window")
+        slopes = None if self.slopes is None else self.slopes.float()   # (a module cast to bfloat16 has cast them too)
+        return DocumentAttentionFunction.apply(x, starts, prefix, slopes, self.heads, self.kv_heads, self.causal, self.window, self.cap,
+                                               self.scale or 0.0)
+
+    def extra_repr(self):
+        return f"heads={self.heads}, kv_heads={self.kv_heads}, causal={self.causal}, window={self.window}, cap={self.cap}"
+
+
+class EmbeddingFunction(torch.autograd.Function):
+    """scale * weight[ids] and its gradient, a dense matrix summed over equal ids in their order (acc_embed_fwd / acc_embed_bwd).  Negative
+    ids give zeros and no gradient, those beyond the vocabulary NaN and no gradient."""
+
+    @staticmethod
+    def forward(ctx, ids, weight, scale: float = 1.0):
+        if weight.dtype not in _CODES:
+            raise TypeError("weight must be bfloat16 or float32")
+        if ids.dtype not in (torch.int64, torch.int32):
+            raise TypeError("ids must be int64 or int32")
+        if not weight.is_cuda or ids.device != weight.device:
+            raise ValueError("ids and weight must be on one GPU")
+        v, d = weight.shape
+        w, i = _rows(weight, d), _aligned(ids.reshape(-1).to(torch.int64))
+        n, dev = i.numel(), weight.device
+        y = torch.empty(n, d, dtype=weight.dtype, device=dev)
+        ctx.meta = (n, d, v, scale, weight.dtype)
+        if n:
+            with torch.cuda.device(dev):
+                acc.acc_embed_fwd(acc.make_embed_desc(n, d, v, ldw=_ld(w), scale=scale, io_dtype=_CODES[weight.dtype]), w, i, y)
+        ctx.save_for_backward(i)
+        return y.reshape(*ids.shape, d)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        n, d, v, scale, dt = ctx.meta
+        if not ctx.needs_input_grad[1]:
+            return None, None, None
+        dev = dy.device
+        if n == 0:
+            return None, torch.zeros(v, d, dtype=dt, device=dev), None
+        ids, = ctx.saved_tensors
+        dy2 = _rows(dy, d)
+        desc = acc.make_embed_desc(n, d, v, ldy=_ld(dy2), scale=scale, io_dtype=_CODES[dt])
+        dw = torch.empty(v, d, dtype=dt, device=dev)
+        with torch.cuda.device(dev):
+            acc.acc_embed_bwd(desc, ids, dy2, dw, _workspace(acc.acc_embed_workspace_bytes(desc), dev))
+        return None, dw, None
+
+
+class Embedding(torch.nn.Module):
+    """The vocabulary's table at a model's input: torch.nn.Embedding's parameter and layout, which LinearCrossEntropy's weight shares, rows
+    times `scale`.  Negative ids are padding (zeros, no gradient)."""
+
+    def __init__(self, vocabulary: int, features: int, scale: float = 1.0, device=None, dtype=torch.bfloat16):
+        super().__init__()
+        self.scale = scale
+        self.weight = torch.nn.Parameter(torch.empty(vocabulary, features, device=device, dtype=dtype))
+        torch.nn.init.normal_(self.weight, std=0.02)
+
+    def forward(self, ids):
+        return EmbeddingFunction.apply(ids, self.weight, self.scale)
+
+    def extra_repr(self):
+        return f"vocabulary={self.weight.shape[0]}, features={self.weight.shape[1]}, scale={self.scale}"
+
+
+@torch.no_grad()
+def clip_grad_norm_(parameters, max_norm: float, modules=()):
+    """torch.nn.utils.clip_grad_norm_ (2-norm) in two passes over the gradients, and over the factored ones of `modules`
+    (CompressedLinear with factored_grad) without their products: every gradient is scaled in place by min(1, max_norm / (norm + 1e-6)),
+    of factored ones the small factor.  Returns the norm, a float32 tensor; nothing waits for the GPU."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
+    grads = list({id(p): p.grad for p in parameters if p.grad is not None}.values())
+    pairs = [m.grad_factors for m in {id(m): m for m in modules}.values() if m.grad_factors is not None]
+    every = grads + [t for pair in pairs for t in pair]
+    if not every:
+        return torch.zeros(())
+    dev = every[0].device
+    if any(t.is_sparse or t.dtype not in _CODES for t in every):
+        raise TypeError("gradients must be dense, bfloat16 or float32")
+    if not every[0].is_cuda or any(t.device != dev for t in every):
+        raise ValueError("all gradients must be on one GPU")
+    dense = [g if g.is_contiguous() else g.contiguous() for g in grads]
+    result = torch.empty(2, dtype=torch.float32, device=dev)
+    tables = acc.make_grad_list(dense), acc.make_factor_list(*([p[i] for p in pairs] for i in (0, 1)), acc.ACC_FLAG_W_OUT_IN)
+    with torch.cuda.device(dev):
+        acc.acc_grad_norm(*tables, max_norm, result, _workspace(acc.acc_grad_norm_workspace_bytes(*tables), dev))
+        acc.acc_grad_scale(acc.make_grad_list(dense + [gr for _, gr in pairs]), result[1:])
+    for g, copy in zip(grads, dense):
+        if copy is not g:
+            g.copy_(copy)
+    return result[0]
+
+
 class LowRankAdamW:
     """Update strategy (ii) of Sec. 4 for `CompressedLinear(..., factored_grad=True)` modules: AdamW whose moments
     have the shape [out_features, proj_rank]; the weights are updated in place by acc_lowrank_adamw_step, and no

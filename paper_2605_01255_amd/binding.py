@@ -34,6 +34,8 @@ EXPORTS = ("acc_linear_workspace_bytes", "acc_linear_fwd", "acc_linear_fwd_stati
            "acc_linear_bwd_act8", "acc_gated_fwd_act8", "acc_gated_bwd_act8",
            "acc_linear_ce_workspace_bytes", "acc_linear_ce_fwd", "acc_linear_ce_bwd",
            "acc_attn_workspace_bytes", "acc_attn_fwd", "acc_attn_bwd",
+           "acc_embed_fwd", "acc_embed_workspace_bytes", "acc_embed_bwd",
+           "acc_grad_norm_workspace_bytes", "acc_grad_norm", "acc_grad_scale",
            "acc_philox_dump_u32", "acc_probe_mfma",
            "acc_sketch_dump", "acc_status_string", "acc_version")
 
@@ -79,6 +81,25 @@ class AccAttnDesc(ctypes.Structure):
                 ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64),
                 ("docs", ctypes.c_int64), ("seq", ctypes.c_int64), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
                 ("cap", ctypes.c_float), ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class AccEmbedDesc(ctypes.Structure):
+    """Mirror of `acc_embed_desc`."""
+    _fields_ = [("n", ctypes.c_int64), ("d", ctypes.c_int64), ("v", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldy", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("io_dtype", ctypes.c_int32), ("dw_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
+class AccGradTensor(ctypes.Structure):
+    """Mirror of `acc_grad_tensor`."""
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("dst_dtype", ctypes.c_int32)]
+
+
+class AccGradFactors(ctypes.Structure):
+    """Mirror of `acc_grad_factors`."""
+    _fields_ = [("left", ctypes.c_void_p), ("gr", ctypes.c_void_p), ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64), ("r", ctypes.c_int64),
+                ("ldl", ctypes.c_int64), ("ldg", ctypes.c_int64), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class AccError(RuntimeError):
@@ -155,6 +176,19 @@ _lib.acc_attn_fwd.restype = ctypes.c_int
 _lib.acc_attn_fwd.argtypes = [_tdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.acc_attn_bwd.restype = ctypes.c_int
 _lib.acc_attn_bwd.argtypes = [_tdp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_edp, _gtp, _gfp = ctypes.POINTER(AccEmbedDesc), ctypes.POINTER(AccGradTensor), ctypes.POINTER(AccGradFactors)
+_lib.acc_embed_fwd.restype = ctypes.c_int
+_lib.acc_embed_fwd.argtypes = [_edp, _vp, _vp, _vp, _vp]
+_lib.acc_embed_workspace_bytes.restype = _sz
+_lib.acc_embed_workspace_bytes.argtypes = [_edp]
+_lib.acc_embed_bwd.restype = ctypes.c_int
+_lib.acc_embed_bwd.argtypes = [_edp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.acc_grad_norm_workspace_bytes.restype = _sz
+_lib.acc_grad_norm_workspace_bytes.argtypes = [_gtp, ctypes.c_int64, _gfp, ctypes.c_int64]
+_lib.acc_grad_norm.restype = ctypes.c_int
+_lib.acc_grad_norm.argtypes = [_gtp, ctypes.c_int64, _gfp, ctypes.c_int64, ctypes.c_float, _vp, _vp, _sz, _vp]
+_lib.acc_grad_scale.restype = ctypes.c_int
+_lib.acc_grad_scale.argtypes = [_gtp, ctypes.c_int64, _vp, _vp]
 _lib.acc_philox_dump_u32.restype = ctypes.c_int
 _lib.acc_philox_dump_u32.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, _vp, _vp]
 _lib.acc_sketch_dump.restype = ctypes.c_int
@@ -438,6 +472,71 @@ def acc_attn_bwd(desc, Q, K, V, starts, prefix, slopes, O, lse, dO, dQ, dK, dV, 
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.acc_attn_bwd(ctypes.byref(desc), _ptr(Q), _ptr(K), _ptr(V), _ptr(starts), _ptr(prefix), _ptr(slopes), _ptr(O), _ptr(lse),
                              _ptr(dO), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def make_embed_desc(n, d, v, ldw=0, ldy=0, scale=1.0, io_dtype=ACC_BF16, dw_dtype=None, flags=0) -> AccEmbedDesc:
+    return AccEmbedDesc(n, d, v, ldw, ldy, scale, io_dtype, io_dtype if dw_dtype is None else dw_dtype, flags, 0)
+
+
+def acc_embed_fwd(desc, W, ids, Y, stream=None):
+    """Enqueue Y = scale W[ids] (ids int64)."""
+    _check(_lib.acc_embed_fwd(ctypes.byref(desc), _ptr(W), _ptr(ids), _ptr(Y), _stream(stream)))
+
+
+def acc_embed_workspace_bytes(desc: AccEmbedDesc) -> int:
+    return int(_lib.acc_embed_workspace_bytes(ctypes.byref(desc)))
+
+
+def acc_embed_bwd(desc, ids, dY, dW, workspace, stream=None, ws_bytes=None):
+    """Enqueue dW (+)= scale times the sums of dY over the tokens of a word."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_embed_bwd(ctypes.byref(desc), _ptr(ids), _ptr(dY), _ptr(dW), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def _code(t):
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("gradients are bfloat16 or float32")
+    return ACC_BF16 if t.dtype == torch.bfloat16 else ACC_F32
+
+
+def make_grad_list(tensors, outs=None):
+    """The table of acc_grad_norm and acc_grad_scale: dense tensors and where they go when scaled (None: in place)."""
+    for a, b in zip(tensors, tensors if outs is None else outs, strict=True):
+        if not a.is_contiguous() or not b.is_contiguous() or a.numel() != b.numel():
+            raise ValueError("gradients and their outputs must be contiguous and of one size")
+    outs = tensors if outs is None else outs
+    return (AccGradTensor * len(tensors))(*((a.data_ptr(), b.data_ptr(), a.numel(), _code(a), _code(b)) for a, b in zip(tensors, outs)))
+
+
+def make_factor_list(left, gr, flags=0):
+    """The table of factored gradients: left [d_in, r] and gr [r, d_out] ([d_out, r] with ACC_FLAG_W_OUT_IN), rows of any stride."""
+    rows = []
+    for x, g in zip(left, gr, strict=True):
+        d_out, r = g.shape if flags & ACC_FLAG_W_OUT_IN else g.shape[::-1]
+        if x.dtype != g.dtype or x.shape[1] != r:
+            raise ValueError("the factors of a gradient have one type and one rank")
+        if x.stride(1) != 1 or g.stride(1) != 1:
+            raise ValueError("the factors' rows must be contiguous")
+        rows.append((x.data_ptr(), g.data_ptr(), x.shape[0], d_out, r, x.stride(0) if x.shape[0] > 1 else 0, g.stride(0) if g.shape[0] > 1 else 0,
+                     _code(x), flags))
+    return (AccGradFactors * len(rows))(*rows)
+
+
+def acc_grad_norm_workspace_bytes(tensors, factors) -> int:
+    return int(_lib.acc_grad_norm_workspace_bytes(tensors, len(tensors), factors, len(factors)))
+
+
+def acc_grad_norm(tensors, factors, max_norm, out, workspace, stream=None, ws_bytes=None):
+    """Enqueue out[0] = the norm over the tables' gradients and out[1] = min(1, max_norm / (norm + 1e-6)) (float32)."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.acc_grad_norm(tensors, len(tensors), factors, len(factors), float(max_norm), _ptr(out), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def acc_grad_scale(tensors, factor, stream=None):
+    """Enqueue the table's outputs = its gradients times factor[0] (float32)."""
+    _check(_lib.acc_grad_scale(tensors, len(tensors), _ptr(factor), _stream(stream)))
 
 
 def acc_philox_dump_u32(seed, row_offset, n, r, out, stream=None):

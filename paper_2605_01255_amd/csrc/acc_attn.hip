@@ -112,7 +112,7 @@ int acc_attn_fwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    L.launch_lds(attn_fwd_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), (size_t)4 * AttnTile<T, DB>::BYTES, p);
+    L.launch_lds(attn_fwd_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
   });
   return L.status();
 }
@@ -139,7 +139,7 @@ int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    const size_t lds = 4 * AttnTile<T, DB>::BYTES;
+    const size_t lds = 4 * Tile32<T, DB>::BYTES;
     L.launch_lds(attn_dq_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), lds, p);
     L.launch_lds(attn_dkv_kernel<T, DB, kWaves>, dim3((unsigned)plan.kv_groups), dim3(kWaves * 64), lds + 2 * 512, p);
   });

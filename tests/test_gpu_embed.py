@@ -1,0 +1,159 @@
+"""The vocabulary's table through the C ABI against float64.  A product is rounded twice at most (2^-24, then half a step of the result's
+type); a sum of k terms in float is off by at most 2^-24 k times the sum of magnitudes."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def acc():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2605_01255_amd import binding
+    return binding
+
+
+class Case:
+    def __init__(self, acc, ids, d, v, dtype="bf16", dw="bf16", scale=1.5, ldw=0, ldy=0, add=False, seed=0):
+        import torch
+        self.acc, self.dtype, self.dw, self.scale, self.add = acc, dtype, dw, scale, add
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.tdt, self.wdt = (torch.bfloat16 if t == "bf16" else torch.float32 for t in (dtype, dw))
+        wide = lambda rows, ld, cols, dt: torch.randn(rows, ld or cols, generator=g, device="cuda").to(dt)  # noqa: E731
+        self.ids = torch.as_tensor(ids, dtype=torch.int64, device="cuda")
+        self.n, self.d, self.v = len(self.ids), d, v
+        self.W, self.dY = wide(v, ldw, d, self.tdt), wide(self.n, ldy, d, self.tdt)
+        self.Y = torch.full((self.n, ldy or d), 7.0, dtype=self.tdt, device="cuda")
+        self.old = torch.randn(v, d, generator=g, device="cuda").to(self.wdt)
+        code = lambda t: acc.ACC_BF16 if t == "bf16" else acc.ACC_F32  # noqa: E731
+        self.desc = acc.make_embed_desc(self.n, d, v, ldw=ldw, ldy=ldy, scale=scale, io_dtype=code(dtype), dw_dtype=code(dw),
+                                        flags=acc.ACC_FLAG_DW_ACCUMULATE if add else 0)
+        self.ws = torch.empty(acc.acc_embed_workspace_bytes(self.desc), dtype=torch.uint8, device="cuda")
+
+    def run(self, stream=None):
+        import torch
+        self.ws.fill_(0xFF)
+        dW = self.old.clone() if self.add else torch.full_like(self.old, float("nan"))
+        self.acc.acc_embed_fwd(self.desc, self.W, self.ids, self.Y, stream=stream)
+        self.acc.acc_embed_bwd(self.desc, self.ids, self.dY, dW, self.ws, stream=stream)
+        torch.cuda.synchronize()
+        return self.Y[:, :self.d], dW
+
+    def check(self):
+        import torch
+        Y, dW = self.run()
+        word = (self.ids >= 0) & (self.ids < self.v)
+        ids = self.ids[word]
+        want = self.W[:, :self.d].double()[ids] * self.scale
+        off = (Y[word].double() - want).abs()
+        assert bool((off <= (STEP[self.dtype] + 2.0 ** -23) * want.abs()).all())
+        assert not Y[self.ids < 0].any() and bool(torch.isnan(Y[self.ids >= self.v]).all())
+        dy = self.dY[word, :self.d].double()
+        sums = torch.zeros(self.v, self.d, dtype=torch.float64, device="cuda").index_add_(0, ids, dy) * self.scale
+        sizes = torch.zeros(self.v, self.d, dtype=torch.float64, device="cuda").index_add_(0, ids, dy.abs()) * abs(self.scale)
+        counts = torch.bincount(ids, minlength=self.v).double().unsqueeze(1)
+        if self.add:
+            sums, sizes = sums + self.old.double(), sizes + self.old.double().abs()
+        bound = (counts + 3) * 2.0 ** -24 * sizes + STEP[self.dw] * sums.abs() * (1 + 2.0 ** -8)
+        off = (dW.double() - sums).abs()
+        assert bool((off <= bound).all()), float((off / bound.clamp_min(1e-30)).max())
+        rest = counts.squeeze(1) == 0
+        assert torch.equal(dW[rest], self.old[rest] if self.add else torch.zeros_like(self.old[rest]))
+
+
+def _words(n, v, seed=0, power=True):
+    """Numbers of words as unequal as in text."""
+    import torch
+    u = torch.rand(n, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+    return ((v ** u if power else u * v + 1).long().clamp(1, v) - 1).tolist()
+
+
+@pytest.mark.parametrize("dtype,dw", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("n,d,v", [(1, 8, 1), (1, 64, 1000), (2, 8, 3), (31, 24, 50), (32, 40, 7), (33, 520, 1001), (65, 1032, 300), (200, 2056, 257),
+                                   (1000, 136, 256), (4097, 64, 5000), (3000, 72, 100000), (900, 4104, 65)])
+def test_tables_and_batches_of_any_size(acc, n, d, v, dtype, dw):
+    Case(acc, _words(n, v), d, v, dtype, dw).check()
+
+
+@pytest.mark.parametrize("dtype,dw", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("what", ["one word", "two words in turn", "all words", "no word", "a few of many", "runs of 32", "a long run between short ones"])
+def test_words_of_any_frequency(acc, what, add, dtype, dw):
+    n, v = 1500, 2000
+    ids = {"one word": [777] * n, "two words in turn": [5, 261] * (n // 2), "all words": list(range(v))[::-1], "no word": [-1] * n,
+           "a few of many": [3] + [-1] * 700 + [1999, 3, 0], "runs of 32": [i // 32 * 256 for i in range(200)],
+           "a long run between short ones": [1, 2, 3] + [9] * 333 + [10, 11] * 20}[what]
+    Case(acc, ids, 104, v, dtype, dw, add=add).check()
+
+
+@pytest.mark.parametrize("dtype,dw", [("bf16", "f32"), ("f32", "bf16")])
+def test_numbers_that_are_no_words(acc, dtype, dw):
+    """Padding and numbers beyond the table; what their rows of dY hold reaches nothing."""
+    ids = _words(300, 500)
+    for at, x in ((0, -1), (7, -100), (50, 500), (51, 501), (120, 1 << 31), (121, (1 << 40) + 3), (200, -(1 << 62)), (299, (1 << 63) - 1)):
+        ids[at] = x
+    c = Case(acc, ids, 72, 500, dtype, dw)
+    c.dY[(c.ids < 0) | (c.ids >= 500)] = float("nan")
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides(acc, dtype):
+    c = Case(acc, _words(150, 90), 40, 90, dtype, "f32", ldw=56, ldy=64)
+    c.check()
+    assert bool((c.Y[:, 40:] == 7.0).all())
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -2.0, 1e-3, 64.0])
+def test_scales(acc, scale):
+    Case(acc, _words(100, 40), 48, 40, "bf16", "f32", scale=scale).check()
+
+
+@pytest.mark.parametrize("v", [16384 // 16 * 256, 16384 // 16 * 256 + 1, 1 << 21])
+def test_tables_so_large_that_fewer_waves_sort(acc, v):
+    ids = _words(700, v, power=False) + [v - 1, v - 1, 0, 255, 256]
+    Case(acc, ids, 8, v, "bf16", "bf16").check()
+
+
+def test_what_is_not_finite_stays_in_its_word(acc):
+    import torch
+    ids = _words(400, 30)
+    c = Case(acc, ids, 64, 30, "bf16", "f32")
+    clean = c.run()[1]
+    c.dY[ids.index(3)] = float("inf")
+    out = c.run()[1]
+    others = torch.arange(30, device="cuda") != 3
+    assert torch.equal(out[others], clean[others]) and not torch.isfinite(out[3]).any()
+
+
+def test_the_same_bits_on_another_stream_and_in_a_graph(acc):
+    import torch
+    c = Case(acc, _words(3000, 700) + [-1] * 40, 264, 700, "bf16", "bf16", add=True)
+    first = [t.clone() for t in c.run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = c.run(stream=side)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    dW, graph = c.old.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        acc.acc_embed_fwd(c.desc, c.W, c.ids, c.Y)
+        acc.acc_embed_bwd(c.desc, c.ids, c.dY, dW, c.ws)
+    for _ in range(3):
+        dW.copy_(c.old)
+        c.Y.fill_(math.nan)
+        c.ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dW, first[1]) and torch.equal(c.Y, first[0])
+        Case(acc, _words(50, 9), 16, 9).check()   # the program's own work between the replays
+    c.ids.copy_(c.ids.flip(0))                    # other words, the same graph
+    dW.copy_(c.old)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = c.run()
+    assert torch.equal(dW, want[1])
