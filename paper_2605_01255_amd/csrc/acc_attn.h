@@ -333,25 +333,37 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
 }
 
 // ---- backward: gradients of the keys and values --------------------------------------------------------------
-// A work-group has NW x 32 keys of one key head, whose rows stay in registers, and goes over the queries of the heads that share it, so that
-// the sum over them is taken in its accumulators.
-template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, 1) void attn_dkv_kernel(AttnParams p) {
+// A work-group has 128 keys of one key head, 32 for each of four waves, and goes over the queries of the heads that share it, so that the sum
+// over them is taken in its accumulators.  bfloat16: eight waves, two for the same keys, which take the two halves of a tile of queries and add
+// their sums up at the end; the keys' rows stay in LDS.  (Two waves a SIMD need 256 registers each, of which the sums take 128: with the
+// keys' rows in registers too there is one, and nothing runs while it waits.)  float: four waves, the keys' rows in registers.
+template <typename T, int DB> struct DkvLayout {
+  using Tile = Tile32<T, DB>;
+  static constexpr int HALVES = sizeof(T) == 2 ? 2 : 1, NW = 4 * HALVES, BM = 128, BQ = Tile::BN;
+  static constexpr int KEYS = HALVES == 2 ? 2 * (BM / Tile::BN) * Tile::BYTES : 0;   // bytes of K and V
+  static constexpr int STAGE = 2 * Tile::BYTES + 512;   // queries, their outputs' gradients, log-sum-exps and deltas
+  static constexpr int SUMS = HALVES == 2 ? 4 * DB * 16 * 64 * 4 : 0;   // one half's sums of one tensor
+  static constexpr int BYTES = KEYS + 2 * STAGE > SUMS ? KEYS + 2 * STAGE : SUMS;
+};
+
+template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW * 64), (DkvLayout<T, DB>::HALVES)) void attn_dkv_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;
-  constexpr int BM = NW * 32, BQ = Tile::BN, QB = BQ / 32;
-  constexpr int STAGE = 2 * Tile::BYTES + 512;   // queries, their outputs' gradients, log-sum-exps and deltas
+  using Layout = DkvLayout<T, DB>;
+  constexpr int NW = Layout::NW, BM = Layout::BM, BQ = Layout::BQ, STAGE = Layout::STAGE;
+  constexpr bool IN_LDS = Layout::HALVES == 2;
+  constexpr int QB = BQ / 32 / Layout::HALVES;   // blocks of queries of a wave
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave & 3, half = wave >> 2;
   const AttnRows w = attn_rows<BM>(p, p.kv_heads, lane, false);
   if (w.empty) return;
-  const int w0 = w.first + wave * 32;
+  const int w0 = w.first + key_wave * 32;
   const int w1 = w0 + 31 < w.end ? w0 + 31 : w.end - 1;
   const int mine = w0 + c < w.end ? w0 + c : w.end - 1;
   const bool there = w0 + c < w.end;
 
-  typename DirectFrag<T>::type kf[Tile::STEPS], vf[Tile::STEPS];
-  load_row<T, DB>(kf, (const T*)p.k + (int64_t)w.head * p.d, mine, p.ldk, p.d, h, !w.dead);
-  load_row<T, DB>(vf, (const T*)p.v + (int64_t)w.head * p.d, mine, p.ldv, p.d, h, !w.dead);
+  const T* kbase = (const T*)p.k + (int64_t)w.head * p.d;
+  const T* vbase = (const T*)p.v + (int64_t)w.head * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
   const int q_lo = queries_lo(p, w, w.first), q_hi = w.dead ? q_lo : queries_hi(p, w, last);
   const int lo = queries_lo(p, w, mine), span = queries_hi(p, w, mine) - lo;
@@ -363,13 +375,30 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, 1) v
   const Tile32Reads<T, DB> at(lane);
   const Tile32Loader<T, DB, NW> qload(lane, wave, p.ldq, p.d), dload(lane, wave, p.ldo, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
+  typename DirectFrag<T>::type kf[IN_LDS ? 1 : Tile::STEPS], vf[IN_LDS ? 1 : Tile::STEPS];
+  const char *ks = smem, *vs = smem + Layout::KEYS / 2;
+  if constexpr (IN_LDS) {
+    if (!w.dead) {
+      const Tile32Loader<T, DB, NW> kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
+#pragma unroll
+      for (int i = 0; i < BM / Tile::BN; ++i) {
+        const int row = w.first + i * Tile::BN;   // (a tile behind the document's end is not read)
+        if (row >= w.end) continue;
+        kload.issue(kbase, row, w.end - row, p.ldk, p.d, lds + i * Tile::BYTES, wave);
+        vload.issue(vbase, row, w.end - row, p.ldv, p.d, lds + Layout::KEYS / 2 + i * Tile::BYTES, wave);
+      }
+    }
+  } else {
+    load_row<T, DB>(kf, kbase, mine, p.ldk, p.d, h, !w.dead);
+    load_row<T, DB>(vf, vbase, mine, p.ldv, p.d, h, !w.dead);
+  }
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{};
   const int per_head = (q_hi - q_lo + BQ - 1) / BQ, tiles = per_head * p.group;
   auto issue = [&](int head, int tile, int t) {
     const int row = q_lo + tile * BQ;
-    const uint32_t stage = lds + (t & 1) * STAGE;
+    const uint32_t stage = lds + Layout::KEYS + (t & 1) * STAGE;
     qload.issue((const T*)p.q + (int64_t)head * p.d, row, q_hi - row, p.ldq, p.d, stage, wave);
     dload.issue((const T*)p.dout + (int64_t)head * p.d, row, q_hi - row, p.ldo, p.d, stage + Tile::BYTES, wave);
     if (wave < 2) {
@@ -391,20 +420,26 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, 1) v
     __syncthreads();
     advance(next_head, next_tile);
     if (t + 1 < tiles) issue(next_head, next_tile, t + 1);
-    const int q0 = q_lo + tile * BQ;
-    if (w0 >= w.end || q0 >= any_hi || q0 + BQ <= any_lo) continue;
-    const char* qs = smem + (t & 1) * STAGE;
+    const int q0 = q_lo + tile * BQ + half * QB * 32;   // this wave's queries
+    if (w0 >= w.end || q0 >= any_hi || q0 + QB * 32 <= any_lo) continue;
+    const char* qs = smem + Layout::KEYS + (t & 1) * STAGE + half * QB * 32 * Tile::PITCH;
     const char* ds = qs + Tile::BYTES;
-    const float* stats = (const float*)(ds + Tile::BYTES);
+    const float* stats = (const float*)(smem + Layout::KEYS + (t & 1) * STAGE + 2 * Tile::BYTES) + half * QB * 32;
     const float slope2 = p.slopes ? p.slopes[head] * kLog2e : 0.f;
-    const bool masked = q0 < full_lo || q0 + BQ > full_hi;
+    const bool masked = q0 < full_lo || q0 + QB * 32 > full_hi;
     static_for<0, QB>([&](auto block) {
       constexpr int b = decltype(block)::value;
       f32x16 s{}, dp{}, by{};
 #pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) mma(s, at.row(qs, b, st), kf[st]);
+      for (int st = 0; st < Tile::STEPS; ++st) {
+        if constexpr (IN_LDS) mma(s, at.row(qs, b, st), at.row(ks, key_wave, st));
+        else mma(s, at.row(qs, b, st), kf[st]);
+      }
 #pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) mma(dp, at.row(ds, b, st), vf[st]);
+      for (int st = 0; st < Tile::STEPS; ++st) {
+        if constexpr (IN_LDS) mma(dp, at.row(ds, b, st), at.row(vs, key_wave, st));
+        else mma(dp, at.row(ds, b, st), vf[st]);
+      }
       if (shaped) s = shape_scores<T, true>(p, s, slope2, q0 + 32 * b + 4 * h, mine, &by);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -432,6 +467,25 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, 1) v
         }
       }
     });
+  }
+  if constexpr (IN_LDS) {   // the second half's sums to the first
+    wait_vmcnt0();
+    float* sums = (float*)smem + key_wave * DB * 16 * 64 + lane;
+    auto meet = [&](f32x16* x) {
+      __syncthreads();
+      if (half) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) for_regs([&](int r) { sums[(db * 16 + r) * 64] = x[db][r]; });
+      }
+      __syncthreads();
+      if (!half) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) for_regs([&](int r) { x[db][r] += sums[(db * 16 + r) * 64]; });
+      }
+    };
+    meet(dk);
+    meet(dv);
+    if (half) return;
   }
   if (!there) return;
   store_row<T, DB>((T*)p.dk + (int64_t)mine * p.ldk + (int64_t)w.head * p.d, dk, p.scale, p.d, h);

@@ -141,7 +141,7 @@ int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
     constexpr int DB = decltype(db)::value;
     const size_t lds = 4 * Tile32<T, DB>::BYTES;
     L.launch_lds(attn_dq_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), lds, p);
-    L.launch_lds(attn_dkv_kernel<T, DB, kWaves>, dim3((unsigned)plan.kv_groups), dim3(kWaves * 64), lds + 2 * 512, p);
+    L.launch_lds(attn_dkv_kernel<T, DB>, dim3((unsigned)plan.kv_groups), dim3(DkvLayout<T, DB>::NW * 64), (size_t)DkvLayout<T, DB>::BYTES, p);
   });
   return L.status();
 }
