@@ -190,11 +190,9 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
     const char* vs = ks + Tile::BYTES;
     f32x16 s[KB];
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      s[b] = f32x16{};
-#pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) mma(s[b], at.row(ks, b, st), qf[st]);
-    }
+    for (int b = 0; b < KB; ++b) s[b] = f32x16{};
+    products<KB * Tile::STEPS, 4>([&](auto i) { return at.row(ks + Tile::block(i.value / Tile::STEPS), i.value % Tile::STEPS); },
+                                  [&](auto i, auto k) { mma(s[i.value / Tile::STEPS], k, qf[i.value % Tile::STEPS]); });
     if (shaped) {
 #pragma unroll
       for (int b = 0; b < KB; ++b) s[b] = shape_scores<T, false>(p, s[b], slope2, k0 + 32 * b + 4 * h, mine, nullptr);
@@ -225,14 +223,11 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
         s[b][r] = fast_exp2(__builtin_fmaf(s[b][r], c2, minus));
         l += s[b][r];
       });
+    typename TransFrag<T>::type pf[2 * KB];
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const auto pf = step_operand<T>(s[b], u);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) mma(o[db], at.column(vs, 2 * b + u, db), pf);
-      }
+    for (int u = 0; u < 2 * KB; ++u) pf[u] = step_operand<T>(s[u / 2], u & 1);
+    products<2 * KB * DB, 4>([&](auto i) { return at.column(vs, i.value / DB, i.value % DB); },
+                             [&](auto i, auto v) { mma(o[i.value % DB], v, pf[i.value / DB]); });
   }
   if (!there) return;
   l = half_sum(l);
@@ -310,10 +305,11 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
     static_for<0, KB>([&](auto block) {
       constexpr int b = decltype(block)::value;
       f32x16 s{}, dp{}, by{};
-#pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) mma(s, at.row(ks, b, st), qf[st]);
-#pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) mma(dp, at.row(vs, b, st), df[st]);
+      products<2 * Tile::STEPS, 4>([&](auto i) { return at.row((i.value < Tile::STEPS ? ks : vs) + Tile::block(b), i.value % Tile::STEPS); },
+                                   [&](auto i, auto x) {
+                                     if constexpr (i.value < Tile::STEPS) mma(s, x, qf[i.value]);
+                                     else mma(dp, x, df[i.value - Tile::STEPS]);
+                                   });
       if (shaped) s = shape_scores<T, true>(p, s, slope2, k0 + 32 * b + 4 * h, mine, &by);
       for_regs([&](int r) { s[r] = fast_exp2(__builtin_fmaf(s[r], c2, minus)) * (dp[r] - delta); });
       if (p.cap2 > 0.f) s *= by;
@@ -321,12 +317,9 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
         const int base = k0 + 32 * b + 4 * h - lo;
         for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[r] = 0.f; });
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const auto sf = step_operand<T>(s, u);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) mma(dq[db], at.column(ks, 2 * b + u, db), sf);
-      }
+      const typename TransFrag<T>::type sf[2] = {step_operand<T>(s, 0), step_operand<T>(s, 1)};
+      products<2 * DB, 4>([&](auto i) { return at.column(ks, 2 * b + i.value / DB, i.value % DB); },
+                          [&](auto i, auto k) { mma(dq[i.value % DB], k, sf[i.value / DB]); });
     });
   }
   if (there) store_row<T, DB>((T*)p.dq + (int64_t)mine * p.ldq + (int64_t)w.head * p.d, dq, p.scale, p.d, h);
@@ -376,7 +369,7 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
   const Tile32Loader<T, DB, NW> qload(lane, wave, p.ldq, p.d), dload(lane, wave, p.ldo, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   typename DirectFrag<T>::type kf[IN_LDS ? 1 : Tile::STEPS], vf[IN_LDS ? 1 : Tile::STEPS];
-  const char *ks = smem, *vs = smem + Layout::KEYS / 2;
+  const char *ks = smem + Tile::block(key_wave), *vs = ks + Layout::KEYS / 2;   // this wave's keys
   if constexpr (IN_LDS) {
     if (!w.dead) {
       const Tile32Loader<T, DB, NW> kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
@@ -422,7 +415,7 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
     if (t + 1 < tiles) issue(next_head, next_tile, t + 1);
     const int q0 = q_lo + tile * BQ + half * QB * 32;   // this wave's queries
     if (w0 >= w.end || q0 >= any_hi || q0 + QB * 32 <= any_lo) continue;
-    const char* qs = smem + Layout::KEYS + (t & 1) * STAGE + half * QB * 32 * Tile::PITCH;
+    const char* qs = smem + Layout::KEYS + (t & 1) * STAGE + Tile::block(half * QB);
     const char* ds = qs + Tile::BYTES;
     const float* stats = (const float*)(smem + Layout::KEYS + (t & 1) * STAGE + 2 * Tile::BYTES) + half * QB * 32;
     const float slope2 = p.slopes ? p.slopes[head] * kLog2e : 0.f;
@@ -430,15 +423,21 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
     static_for<0, QB>([&](auto block) {
       constexpr int b = decltype(block)::value;
       f32x16 s{}, dp{}, by{};
-#pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) {
-        if constexpr (IN_LDS) mma(s, at.row(qs, b, st), at.row(ks, key_wave, st));
-        else mma(s, at.row(qs, b, st), kf[st]);
-      }
-#pragma unroll
-      for (int st = 0; st < Tile::STEPS; ++st) {
-        if constexpr (IN_LDS) mma(dp, at.row(ds, b, st), at.row(vs, key_wave, st));
-        else mma(dp, at.row(ds, b, st), vf[st]);
+      using Frag = typename DirectFrag<T>::type;
+      if constexpr (IN_LDS) {
+        struct Pair { Frag q, k; };
+        products<2 * Tile::STEPS, 3>(
+            [&](auto i) {
+              constexpr bool second = i.value >= Tile::STEPS;
+              return Pair{at.row((second ? ds : qs) + Tile::block(b), i.value % Tile::STEPS), at.row(second ? vs : ks, i.value % Tile::STEPS)};
+            },
+            [&](auto i, const Pair& x) { mma(i.value < Tile::STEPS ? s : dp, x.q, x.k); });
+      } else {
+        products<2 * Tile::STEPS, 4>([&](auto i) { return at.row((i.value < Tile::STEPS ? qs : ds) + Tile::block(b), i.value % Tile::STEPS); },
+                                     [&](auto i, const Frag& x) {
+                                       if constexpr (i.value < Tile::STEPS) mma(s, x, kf[i.value]);
+                                       else mma(dp, x, vf[i.value - Tile::STEPS]);
+                                     });
       }
       if (shaped) s = shape_scores<T, true>(p, s, slope2, q0 + 32 * b + 4 * h, mine, &by);
 #pragma unroll
@@ -457,15 +456,12 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
         const int base = q0 + 32 * b + 4 * h - lo;
         for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[r] = dp[r] = 0.f; });
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const auto pf = step_operand<T>(s, u), sf = step_operand<T>(dp, u);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          mma(dv[db], at.column(ds, 2 * b + u, db), pf);
-          mma(dk[db], at.column(qs, 2 * b + u, db), sf);
-        }
-      }
+      const typename TransFrag<T>::type pf[2] = {step_operand<T>(s, 0), step_operand<T>(s, 1)}, sf[2] = {step_operand<T>(dp, 0), step_operand<T>(dp, 1)};
+      products<4 * DB, 4>([&](auto i) { return at.column(i.value & 1 ? qs : ds, 2 * b + i.value / 2 / DB, i.value / 2 % DB); },
+                          [&](auto i, auto x) {
+                            if constexpr (i.value & 1) mma(dk[i.value / 2 % DB], x, sf[i.value / 2 / DB]);
+                            else mma(dv[i.value / 2 % DB], x, pf[i.value / 2 / DB]);
+                          });
     });
   }
   if constexpr (IN_LDS) {   // the second half's sums to the first

@@ -223,8 +223,8 @@ template <typename T> __global__ __launch_bounds__(256, 1) void gram_kernel(Gram
         typename DirectFrag<T>::type af[2], bf[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {   // 32 rows each, one tile after another
-          af[i] = at.row(smem, 2 * wi + i, st);
-          bf[i] = at.row(smem + HALVES * Tile::BYTES, 2 * wj + i, st);
+          af[i] = at.row(smem + Tile::block(2 * wi + i), st);
+          bf[i] = at.row(smem + HALVES * Tile::BYTES + Tile::block(2 * wj + i), st);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)

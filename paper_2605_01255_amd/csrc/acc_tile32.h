@@ -7,20 +7,24 @@ namespace acc {
 // f of 0 .. 15 as constants: registers of a block, which an ordinary loop may be unrolled too late to keep out of scratch memory.
 template <typename F> __device__ __forceinline__ void for_regs(F&& f) { static_for<0, 16>(f); }
 
-// A row of a tile takes PITCH bytes of LDS, a power of two; 16-byte chunk c of row r lies at chunk c ^ row_swizzle(r).  Direct reads of one
-// chunk of 16 rows, and transposing reads of 4 rows x 32 columns, then fall on all 64 banks.
-template <int PITCH> __device__ __forceinline__ int row_swizzle(int row) {
-  if constexpr (PITCH == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-  else return ((row & 3) << 2) | ((row >> 2) & 3);
-}
+// A tile lies in LDS as super-rows of 256 bytes (a row; two rows, r and r + 32, where a row has 128; half a row where it has 512), four of
+// them to a transfer of 1024 bytes and 16 bytes of room behind it: 16-byte chunk c of super-row r is at
+// 1040 (r / 4) + 256 (c / 4) + 64 (r % 4) + 16 (c % 4).  Direct reads of one chunk of 16 rows, and transposing reads of 4 rows x 32 columns,
+// fall on all 64 banks, a transfer takes 64 bytes of a row at a time, and every operand is at a fixed distance from one address a lane (a
+// swizzle by exclusive or needs sixteen addresses, or an instruction a read).
+constexpr int kTileGroup = 1040;
 
 template <typename T, int DB> struct Tile32 {
   static constexpr int ROW = DB * 32 * (int)sizeof(T);
   static constexpr int PITCH = ROW <= 128 ? 128 : ROW <= 256 ? 256 : 512;
-  static constexpr int CHUNKS = PITCH / 16, ROWS_PER_LOAD = 1024 / PITCH, PER_CHUNK = 16 / (int)sizeof(T);
+  static constexpr int PER_CHUNK = 16 / (int)sizeof(T);
   static constexpr int STEPS = DB * 32 / (2 * PER_CHUNK);   // direct operands along the channels
   static constexpr int BN = sizeof(T) == 2 ? 64 : 32;       // rows of a tile
-  static constexpr int BYTES = BN * PITCH;
+  static constexpr int GROUPS = BN * PITCH / 1024, BYTES = GROUPS * kTileGroup;
+  // blocks of 32 rows of one or several tiles one after another
+  __device__ __forceinline__ static constexpr int block(int b) {
+    return PITCH == 128 ? (b >> 1) * BYTES + (b & 1) * 512 : PITCH == 256 ? b * 8 * kTileGroup : b * BYTES;
+  }
 };
 
 template <typename T> struct DirectFrag { using type = bf16x8; };
@@ -42,48 +46,51 @@ __device__ __forceinline__ void mma(f32x16& c, f32x8 a, f32x8 b) {
 // This lane's places in a tile.
 template <typename T, int DB> struct Tile32Reads {
   using Tile = Tile32<T, DB>;
-  static constexpr int TRANS = sizeof(T) == 2 ? 2 : 4;
-  int direct[Tile::STEPS];
-  int trans[DB][TRANS];
+  static constexpr int PITCH = Tile::PITCH, G = kTileGroup;
+  int direct, trans;
   // columns are counted from 32-channel block `from` on
   __device__ __forceinline__ explicit Tile32Reads(int lane, int from = 0) {
     const int c = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int s = 0; s < Tile::STEPS; ++s) direct[s] = c * Tile::PITCH + (((2 * s + h) ^ row_swizzle<Tile::PITCH>(c)) << 4);
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int t = 0; t < TRANS; ++t) {
-        if constexpr (sizeof(T) == 2) {   // rows 4 h + 8 t .. + 3 of a step of 16
-          const int row = 4 * h + 8 * t + ((lane & 15) >> 2), col = (from + db) * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-          trans[db][t] = row * Tile::PITCH + (((col >> 3) ^ row_swizzle<Tile::PITCH>(row)) << 4) + (col & 7) * 2;
-        } else {   // rows 4 h + t and 8 more
-          const int row = 4 * h + t, col = (from + db) * 32 + c;
-          trans[db][t] = row * Tile::PITCH + (((col >> 2) ^ row_swizzle<Tile::PITCH>(row)) << 4) + (col & 3) * 4;
-        }
-      }
+    direct = (c >> 2) * G + (c & 3) * 64 + h * 16;
+    if constexpr (sizeof(T) == 2) trans = h * G + ((lane >> 2) & 3) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8 + from * 256;
+    else trans = h * G + (c >> 4) * 256 + (c & 15) * 4 + columns(from);
   }
-  // rows 32 block + l % 32, channels of step s
-  __device__ __forceinline__ typename DirectFrag<T>::type row(const char* tile, int block, int s) const {
-    return *(const typename DirectFrag<T>::type*)(tile + direct[s] + block * 32 * Tile::PITCH);
+  __device__ __forceinline__ static constexpr int columns(int db) {
+    if constexpr (sizeof(T) == 2) return db * 256;
+    else return (db >> 1) * 8 * G + (db & 1) * 512;
+  }
+  // rows 32 block + l % 32 (tile: where block 0 begins), channels of step s
+  __device__ __forceinline__ typename DirectFrag<T>::type row(const char* tile, int s) const {
+    return *(const typename DirectFrag<T>::type*)(tile + direct + (2 * s >> 4) * 8 * G + ((2 * s & 15) >> 2) * 256 + (2 * s & 3) * 16);
   }
   // channels 32 db + l % 32, rows 16 u + (0 .. 15) in the accumulators' order
   __device__ __forceinline__ typename TransFrag<T>::type column(const char* tile, int u, int db) const {
+    const char* at = tile + trans + columns(db) + (PITCH == 128 ? (u & 1) * 4 * G + (u >> 1) * 512 : u * 4 * G);
     if constexpr (sizeof(T) == 2) {
-      const s16x4 lo = lds_read_tr16_b64(tile, trans[db][0] + u * 16 * Tile::PITCH);
-      const s16x4 hi = lds_read_tr16_b64(tile, trans[db][1] + u * 16 * Tile::PITCH);
+      const s16x4 lo = lds_read_tr16_b64(at, 0);
+      const s16x4 hi = lds_read_tr16_b64(at, 2 * G);
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       f32x8 v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {   // 8 rows further on the swizzle's low bits are the other way round
-        const int base = e < 4 ? trans[db][e] : trans[db][e - 4] ^ (2 << 4);
-        v[e] = *(const float*)(tile + base + (u * 16 + (e < 4 ? 0 : 8)) * Tile::PITCH);
-      }
+      for (int e = 0; e < 8; ++e) v[e] = *(const float*)(at + (e >> 2) * 2 * G + (e & 3) * 64);
       return v;
     }
   }
 };
+
+// N products in their order, product i on what read(i) gives, read AHEAD products before.  The fences keep the order: left alone the compiler
+// puts each read right in front of its product and waits for it.
+template <int N, int AHEAD, typename Read, typename Product> __device__ __forceinline__ void products(Read&& read, Product&& product) {
+  decltype(read(std::integral_constant<int, 0>{})) ring[AHEAD];
+  static_for<0, (AHEAD < N ? AHEAD : N)>([&](auto i) { ring[i.value] = read(i); });
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<0, N>([&](auto i) {
+    product(i, ring[i.value % AHEAD]);
+    if constexpr (i.value + AHEAD < N) ring[i.value % AHEAD] = read(std::integral_constant<int, i.value + AHEAD>{});
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
 
 // The eight accumulators of step u as an operand.  bfloat16: each rounded once, as the product takes them.
 template <typename T> __device__ __forceinline__ typename TransFrag<T>::type step_operand(f32x16 x, int u) {
@@ -128,14 +135,15 @@ template <typename T, int DB> __device__ __forceinline__ void store_row(T* row, 
 // Rows of a matrix to LDS tiles.  `there` rows from `row` on of which the tile takes BN; the rest, and channels behind d, become zeros.
 template <typename T, int DB, int NW> struct Tile32Loader {
   using Tile = Tile32<T, DB>;
-  static constexpr int LOADS = Tile::BYTES / 1024 / NW;
-  static_assert(LOADS * 1024 * NW == Tile::BYTES, "whole loads");
+  static constexpr int LOADS = Tile::GROUPS / NW;
+  static_assert(LOADS * NW == Tile::GROUPS, "whole transfers");
   uint32_t src[LOADS];
   __device__ __forceinline__ Tile32Loader(int lane, int wave, int64_t ld, int d) {
 #pragma unroll
     for (int t = 0; t < LOADS; ++t) {
-      const int row = (t * NW + wave) * Tile::ROWS_PER_LOAD + lane / Tile::CHUNKS;
-      const int chunk = (lane % Tile::CHUNKS) ^ row_swizzle<Tile::PITCH>(row);
+      const int super = 4 * (t * NW + wave) + ((lane >> 2) & 3), cc = (lane >> 4) * 4 + (lane & 3);
+      const int row = Tile::PITCH == 128 ? super + 32 * (cc >> 3) : Tile::PITCH == 256 ? super : super & 31;
+      const int chunk = Tile::PITCH == 128 ? cc & 7 : Tile::PITCH == 256 ? cc : cc + 16 * (super >> 5);
       src[t] = chunk * Tile::PER_CHUNK < d ? (uint32_t)(row * (int)ld * (int)sizeof(T) + (chunk << 4)) : 0xFFFFFFF0u;
     }
   }
@@ -143,7 +151,7 @@ template <typename T, int DB, int NW> struct Tile32Loader {
     const int rows = there < Tile::BN ? there : Tile::BN;
     const u32x4 rsrc = make_rsrc(base + row * ld, ((int64_t)(rows - 1) * ld + d) * (int64_t)sizeof(T));
 #pragma unroll
-    for (int t = 0; t < LOADS; ++t) buffer_to_lds_b128(rsrc, src[t], 0, lds + (t * NW + wave) * 1024);
+    for (int t = 0; t < LOADS; ++t) buffer_to_lds_b128(rsrc, src[t], 0, lds + (t * NW + wave) * kTileGroup);
   }
 };
 
