@@ -24,16 +24,19 @@ struct AttnParams {
   const void *q, *k, *v, *dout;
   const void* o_in;
   void *o, *dq, *dk, *dv;
-  float *lse, *delta;
+  float *lse, *minus, *delta;   // minus: -log-sum-exp in units of log 2 (backward)
   const int64_t *starts, *prefix;
   const float* slopes;
   int64_t ldq, ldk, ldv, ldo;   // elements
   int n, docs, seq;             // docs == 0: sequences of seq rows
   int heads, kv_heads, group, d;
   int tiles;                    // of one head, those that hold no row included
+  int strands, strand_tiles;    // of one key head's tiles
   int causal, window;
   float c2, scale;              // scale log2 e, scale
   float cap2, inv_cap;          // cap log2 e (0: none), scale / cap
+  float* part;                  // [parts][2][n][kv_heads d]: dK and dV of a part of the query heads that share them
+  int parts;
 };
 
 // ---- which rows a work-group has -----------------------------------------------------------------------------
@@ -44,18 +47,20 @@ struct AttnRows {
   bool empty, dead;    // no row at all; rows of no document
 };
 
-// Work-group -> head and tile.  An XCD (work-groups are dealt round-robin to the eight) has a contiguous run of (head, tile), so that its
-// L2 holds the few heads it is at; last tiles first, which have the most keys where the mask is causal.
+// Work-group -> head and tile.  An XCD (work-groups are dealt round-robin to the eight) has a contiguous run of (key head, strand, tile, `share`
+// query heads on it), so that its L2 holds the keys and values that its work-groups are at.  Where the key heads are no multiple of eight
+// their tiles are dealt to several strands, or one XCD would have a head's long tiles and the next its short ones.  Last tiles first, which have
+// the most keys where the mask is causal.
 // A document's tiles start at its first row.  Tile number t belongs to document e (0: the rows before the first, docs + 1: those behind the
 // last) where e is the last with b_e / BM + e <= t, b_e its first row: these numbers rise by at least the document's tiles from one to the next.
-template <int BM> __device__ __forceinline__ AttnRows attn_rows(const AttnParams& p, int heads, int lane, bool last_first) {
+template <int BM> __device__ __forceinline__ AttnRows attn_rows(const AttnParams& p, int share, int lane, bool last_first) {
   AttnRows w{};
-  const int64_t total = (int64_t)heads * p.tiles, per = (total + 7) >> 3;
-  const int64_t id = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  w.empty = (int64_t)(blockIdx.x >> 3) >= per || id >= total;
+  const int per = gridDim.x >> 3, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int each = p.strand_tiles * share, strand = id / each, in = id - strand * each;
+  w.head = strand / p.strands * share + in % share;
+  int t = in / share * p.strands + strand % p.strands;
+  w.empty = t >= p.tiles;
   if (w.empty) return w;
-  w.head = (int)(id / p.tiles);
-  int t = (int)(id - (int64_t)w.head * p.tiles);
   if (last_first) t = p.tiles - 1 - t;
   int doc, tile;
   if (p.docs == 0) {
@@ -121,13 +126,13 @@ __device__ __forceinline__ int queries_hi(const AttnParams& p, const AttnRows& w
 template <typename T, bool GRAD>
 __device__ __forceinline__ f32x16 shape_scores(const AttnParams& p, f32x16 s, float slope2, int at, int own, f32x16* slope_of_cap) {
   if (p.cap2 > 0.f) {
-    f32x16 x = s * p.inv_cap, inv;
+    f32x16 x = s * here(p.inv_cap), inv;   // (in a vector register: sixteen copies of a scalar one are kept otherwise)
     for_regs([&](int r) { inv[r] = __builtin_amdgcn_rcpf(1.f + fast_exp2(x[r] * (2.f * kLog2e))); });   // (1 - tanh x) / 2
-    if constexpr (sizeof(T) == 2) s = p.cap2 * (1.f - 2.f * inv);
+    if constexpr (sizeof(T) == 2) s = here(p.cap2) * (1.f - 2.f * inv);
     else for_regs([&](int r) { s[r] = p.cap2 * tanhf(x[r]); });
     if constexpr (GRAD) *slope_of_cap = 4.f * inv * (1.f - inv);
   } else {
-    s *= p.c2;
+    s *= here(p.c2);
   }
   if (slope2 != 0.f) {
     const float gap = (float)(at - own);
@@ -135,6 +140,8 @@ __device__ __forceinline__ f32x16 shape_scores(const AttnParams& p, f32x16 s, fl
   }
   return s;
 }
+
+constexpr float kSlack = 8.f;
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.
@@ -144,7 +151,7 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   constexpr int BM = NW * 32, BN = Tile::BN, KB = BN / 32;
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const AttnRows w = attn_rows<BM>(p, p.heads, lane, true);
+  const AttnRows w = attn_rows<BM>(p, p.group, lane, true);
   if (w.empty) return;
   const int kv = w.head / p.group;
   const int w0 = w.first + wave * 32;                        // this wave's rows
@@ -165,7 +172,8 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const float slope2 = p.slopes ? p.slopes[w.head] * kLog2e : 0.f, c2 = shaped ? 1.f : p.c2;
 
   const Tile32Reads<T, DB> at(lane);
-  const Tile32Loader<T, DB, NW> kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
+  using KVLoader = Tile32Loader<T, DB, NW>;
+  const KVLoader kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   f32x16 o[DB];
 #pragma unroll
@@ -173,62 +181,114 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   float m = -INFINITY, l = 0.f;
 
   const int tiles = (k_hi - k_lo + BN - 1) / BN;
-  auto issue = [&](int t) {
-    const int row = k_lo + t * BN;
-    const uint32_t stage = lds + (t & 1) * 2 * Tile::BYTES;
-    kload.issue(kbase, row, k_hi - row, p.ldk, p.d, stage, wave);
-    vload.issue(vbase, row, k_hi - row, p.ldv, p.d, stage + Tile::BYTES, wave);
+  constexpr int PIECES = 2 * KVLoader::LOADS;
+  Tile32Run<T, DB, NW> krun(kbase, k_lo, k_hi - k_lo, p.ldk, p.d), vrun(vbase, k_lo, k_hi - k_lo, p.ldv, p.d);
+  uint32_t stage = lds;
+  auto next = [&](int t) {   // tile t's transfers
+    stage = lds + (t & 1) * 2 * Tile::BYTES;
+    krun.advance(t, tiles);
+    vrun.advance(t, tiles);
   };
-  if (tiles > 0) issue(0);
+  auto piece = [&](int i) {
+    if (i < KVLoader::LOADS) kload.one(krun.rsrc, i, stage, wave);
+    else vload.one(vrun.rsrc, i - KVLoader::LOADS, stage + Tile::BYTES, wave);
+  };
+  auto pieces = [&]() {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) piece(i);
+  };
+  if (tiles > 0) pieces();
   for (int t = 0; t < tiles; ++t) {
     wait_vmcnt0();
     __syncthreads();
-    if (t + 1 < tiles) issue(t + 1);
+    next(t + 1);   // (behind the last one: no rows, zeros)
     const int k0 = k_lo + t * BN;
-    if (w0 >= w.end || k0 >= any_hi || k0 + BN <= any_lo) continue;
+    if (w0 >= w.end || k0 >= any_hi || k0 + BN <= any_lo) {
+      pieces();
+      continue;
+    }
     const char* ks = smem + (t & 1) * 2 * Tile::BYTES;
     const char* vs = ks + Tile::BYTES;
+    const bool masked = k0 < full_lo || k0 + BN > full_hi;
     f32x16 s[KB];
 #pragma unroll
     for (int b = 0; b < KB; ++b) s[b] = f32x16{};
-    products<KB * Tile::STEPS, 4>([&](auto i) { return at.row(ks + Tile::block(i.value / Tile::STEPS), i.value % Tile::STEPS); },
-                                  [&](auto i, auto k) { mma(s[i.value / Tile::STEPS], k, qf[i.value % Tile::STEPS]); });
-    if (shaped) {
+    typename TransFrag<T>::type pf[2];
+    float minus = 0.f, by = 1.f;
+    bool changed = false;
+    // Block b's scores to what their exponentials are taken of.  The maximum that they are relative to is raised where a score is kSlack
+    // (powers of 2) above it, not for every new one: probabilities up to 2^kSlack are as exact, and O is hardly ever multiplied.
+    auto begin = [&](auto block) {
+      constexpr int b = block.value;
+      if (shaped) s[b] = shape_scores<T, false>(p, s[b], slope2, k0 + 32 * b + 4 * h, mine, nullptr);
+      if (masked) {
+        const int base = k0 + 32 * b + 4 * h - lo;
+        for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[b][r] = -INFINITY; });
+      }
+      float top = fmaxf(s[b][0], s[b][1]);
+      static_for<2, 16>([&](auto r) { top = fmaxf(top, s[b][r.value]); });
+      top = half_max(top) * c2;
+      changed = __any(top > m + kSlack);
+      if (changed) {
+        const float next = fmaxf(m, top);
+        by = fast_exp2(m - (next == -INFINITY ? 0.f : next));
+        m = next;
+        l *= by;
+      }
+      minus = m == -INFINITY ? 0.f : -m;
+    };
+    auto exponential = [&](int b, int r) {
+      s[b][r] = here(fast_exp2(__builtin_fmaf(s[b][r], c2, minus)));
+      l += s[b][r];
+    };
+    auto rescale = [&]() {
+      if (!changed) return;
 #pragma unroll
-      for (int b = 0; b < KB; ++b) s[b] = shape_scores<T, false>(p, s[b], slope2, k0 + 32 * b + 4 * h, mine, nullptr);
-    }
-    if (k0 < full_lo || k0 + BN > full_hi) {
-      const int base = k0 + 4 * h - lo;
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-        for_regs([&](int r) { if ((uint32_t)(base + 32 * b + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[b][r] = -INFINITY; });
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-      for_regs([&](int r) { top = fmaxf(top, s[b][r]); });
-    top = half_max(top) * c2;
-    if (__any(top > m)) {
-      const float next = fmaxf(m, top), by = fast_exp2(m - (next == -INFINITY ? 0.f : next));
-      m = next;
-      l *= by;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-        o[db] *= by;
-    }
-    const float minus = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-      for_regs([&](int r) {
-        s[b][r] = fast_exp2(__builtin_fmaf(s[b][r], c2, minus));
-        l += s[b][r];
-      });
-    typename TransFrag<T>::type pf[2 * KB];
-#pragma unroll
-    for (int u = 0; u < 2 * KB; ++u) pf[u] = step_operand<T>(s[u / 2], u & 1);
-    products<2 * KB * DB, 4>([&](auto i) { return at.column(vs, i.value / DB, i.value % DB); },
-                             [&](auto i, auto v) { mma(o[i.value % DB], v, pf[i.value / DB]); });
+      for (int db = 0; db < DB; ++db) o[db] *= by;
+    };
+    auto pack = [&](int b) {
+      pf[0] = here(step_operand<T>(s[b], 0));
+      pf[1] = here(step_operand<T>(s[b], 1));
+    };
+    // scores of block 0, of block 1 (block 0's exponentials), O of block 0 (block 1's exponentials), O of block 1
+    constexpr int LS = Tile::STEPS, LO = 2 * DB;
+    products<KB * (LS + LO), sizeof(T) == 2 ? 4 : 1>(
+        [&](auto i) {
+          if constexpr (i.value < KB * LS) return widened(at.row(ks + Tile::block(i.value / LS), i.value % LS));
+          else return at.column(vs, (i.value - KB * LS) / DB, (i.value - KB * LS) % DB);
+        },
+        [&](auto i, auto x) {
+          if constexpr (i.value < KB * LS) mma(s[i.value / LS], narrowed<T>(x), qf[i.value % LS]);
+          else mma(o[(i.value - KB * LS) % DB], x, pf[(i.value - KB * LS) / DB % 2]);
+        },
+        [&](auto i) {
+          // the next tile's transfers a few products apart: one after another they hold the wave up
+          constexpr int apart = KB * (LS + LO) / PIECES;
+          if constexpr (i.value % apart == 0 && i.value / apart < PIECES) piece(i.value / apart);
+          if constexpr (KB == 2) {
+            constexpr int phase = i.value < 2 * LS ? i.value / LS : 2 + (i.value - 2 * LS) / LO;
+            constexpr int step = i.value < 2 * LS ? i.value % LS : (i.value - 2 * LS) % LO, steps = phase < 2 ? LS : LO;
+            if constexpr (phase == 1 || phase == 2) {
+              constexpr int b = phase - 1;
+              if constexpr (step == 0) {
+                begin(std::integral_constant<int, b>{});
+                if constexpr (b == 0) rescale();
+              }
+              spread<step, steps>([&](int r) { exponential(b, r); });
+              if constexpr (step == steps - 1) {
+                pack(b);
+                if constexpr (b == 1) rescale();   // block 0's part is in O
+              }
+            }
+          } else if constexpr (i.value == LS - 1) {
+            begin(std::integral_constant<int, 0>{});
+            rescale();
+            for_regs([&](int r) { exponential(0, r); });
+            pack(0);
+          }
+        });
   }
+  wait_vmcnt0();
   if (!there) return;
   l = half_sum(l);
   store_row<T, DB>((T*)p.o + (int64_t)mine * p.ldo + (int64_t)w.head * p.d, o, l == 0.f ? 0.f : 1.f / l, p.d, h);
@@ -243,7 +303,7 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   constexpr int BM = NW * 32, BN = Tile::BN, KB = BN / 32;
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const AttnRows w = attn_rows<BM>(p, p.heads, lane, true);
+  const AttnRows w = attn_rows<BM>(p, p.group, lane, true);
   if (w.empty) return;
   const int kv = w.head / p.group;
   const int w0 = w.first + wave * 32;
@@ -265,9 +325,12 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
     delta = half_sum(delta);
   }
   const int64_t row = (int64_t)w.head * p.n + mine;
-  if (there && h == 0) p.delta[row] = delta;
-  const float lse2 = w.dead ? 0.f : p.lse[row] * kLog2e;
-  const float minus = lse2 == -INFINITY ? -INFINITY : -lse2;   // a row without keys has no probabilities
+  const float lse = w.dead ? -INFINITY : p.lse[row];
+  const float minus = lse == -INFINITY ? -INFINITY : lse * -kLog2e;   // a row without keys has no probabilities
+  if (there && h == 0) {
+    p.delta[row] = delta;
+    p.minus[row] = minus;
+  }
 
   const T* kbase = (const T*)p.k + (int64_t)kv * p.d;
   const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
@@ -280,48 +343,100 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const float slope2 = p.slopes ? p.slopes[w.head] * kLog2e : 0.f, c2 = shaped ? 1.f : p.c2;
 
   const Tile32Reads<T, DB> at(lane);
-  const Tile32Loader<T, DB, NW> kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
+  using KVLoader = Tile32Loader<T, DB, NW>;
+  const KVLoader kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   f32x16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{};
   const int tiles = (k_hi - k_lo + BN - 1) / BN;
-  auto issue = [&](int t) {
-    const int r = k_lo + t * BN;
-    const uint32_t stage = lds + (t & 1) * 2 * Tile::BYTES;
-    kload.issue(kbase, r, k_hi - r, p.ldk, p.d, stage, wave);
-    vload.issue(vbase, r, k_hi - r, p.ldv, p.d, stage + Tile::BYTES, wave);
+  constexpr int PIECES = 2 * KVLoader::LOADS;
+  Tile32Run<T, DB, NW> krun(kbase, k_lo, k_hi - k_lo, p.ldk, p.d), vrun(vbase, k_lo, k_hi - k_lo, p.ldv, p.d);
+  uint32_t stage = lds;
+  auto next = [&](int t) {   // tile t's transfers
+    stage = lds + (t & 1) * 2 * Tile::BYTES;
+    krun.advance(t, tiles);
+    vrun.advance(t, tiles);
   };
-  if (tiles > 0) issue(0);
+  auto piece = [&](int i) {
+    if (i < KVLoader::LOADS) kload.one(krun.rsrc, i, stage, wave);
+    else vload.one(vrun.rsrc, i - KVLoader::LOADS, stage + Tile::BYTES, wave);
+  };
+  auto pieces = [&]() {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) piece(i);
+  };
+  if (tiles > 0) pieces();
   for (int t = 0; t < tiles; ++t) {
     wait_vmcnt0();
     __syncthreads();
-    if (t + 1 < tiles) issue(t + 1);
+    next(t + 1);   // (behind the last one: no rows, zeros)
     const int k0 = k_lo + t * BN;
-    if (w0 >= w.end || k0 >= any_hi || k0 + BN <= any_lo) continue;
+    if (w0 >= w.end || k0 >= any_hi || k0 + BN <= any_lo) {
+      pieces();
+      continue;
+    }
     const char* ks = smem + (t & 1) * 2 * Tile::BYTES;
     const char* vs = ks + Tile::BYTES;
     const bool masked = k0 < full_lo || k0 + BN > full_hi;
-    static_for<0, KB>([&](auto block) {
-      constexpr int b = decltype(block)::value;
-      f32x16 s{}, dp{}, by{};
-      products<2 * Tile::STEPS, 4>([&](auto i) { return at.row((i.value < Tile::STEPS ? ks : vs) + Tile::block(b), i.value % Tile::STEPS); },
-                                   [&](auto i, auto x) {
-                                     if constexpr (i.value < Tile::STEPS) mma(s, x, qf[i.value]);
-                                     else mma(dp, x, df[i.value - Tile::STEPS]);
-                                   });
-      if (shaped) s = shape_scores<T, true>(p, s, slope2, k0 + 32 * b + 4 * h, mine, &by);
-      for_regs([&](int r) { s[r] = fast_exp2(__builtin_fmaf(s[r], c2, minus)) * (dp[r] - delta); });
-      if (p.cap2 > 0.f) s *= by;
+    f32x16 s[KB], dp[KB], by{};
+#pragma unroll
+    for (int b = 0; b < KB; ++b) s[b] = dp[b] = f32x16{};
+    typename TransFrag<T>::type sf[2];
+    auto shape = [&](auto block) {
+      constexpr int b = block.value;
+      if (shaped) s[b] = shape_scores<T, true>(p, s[b], slope2, k0 + 32 * b + 4 * h, mine, &by);
+    };
+    auto probability = [&](int b, int r) { s[b][r] = here(fast_exp2(__builtin_fmaf(s[b][r], c2, minus))); };
+    auto gradient = [&](int b, int r) { s[b][r] = here(s[b][r] * (dp[b][r] - delta)); };
+    auto pack = [&](auto block) {
+      constexpr int b = block.value;
+      if (p.cap2 > 0.f) s[b] *= by;
       if (masked) {
         const int base = k0 + 32 * b + 4 * h - lo;
-        for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[r] = 0.f; });
+        for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[b][r] = 0.f; });
       }
-      const typename TransFrag<T>::type sf[2] = {step_operand<T>(s, 0), step_operand<T>(s, 1)};
-      products<2 * DB, 4>([&](auto i) { return at.column(ks, 2 * b + i.value / DB, i.value % DB); },
-                          [&](auto i, auto k) { mma(dq[i.value % DB], k, sf[i.value / DB]); });
-    });
+      sf[0] = here(step_operand<T>(s[b], 0));
+      sf[1] = here(step_operand<T>(s[b], 1));
+    };
+    // scores and dP of block 0 (its probabilities), scores of block 1 (block 0's dS), dP of block 1 (its probabilities), dQ of block 0 (block 1's
+    // dS), dQ of block 1
+    constexpr int LS = Tile::STEPS, LO = 2 * DB;
+    products<KB * (2 * LS + LO), sizeof(T) == 2 ? 3 : 1>(
+        [&](auto i) {
+          if constexpr (i.value < KB * 2 * LS) return widened(at.row((i.value / LS & 1 ? vs : ks) + Tile::block(i.value / (2 * LS)), i.value % LS));
+          else return at.column(ks, (i.value - KB * 2 * LS) / DB, (i.value - KB * 2 * LS) % DB);
+        },
+        [&](auto i, auto x) {
+          if constexpr (i.value < KB * 2 * LS) {
+            if constexpr (i.value / LS & 1) mma(dp[i.value / (2 * LS)], narrowed<T>(x), df[i.value % LS]);
+            else mma(s[i.value / (2 * LS)], narrowed<T>(x), qf[i.value % LS]);
+          } else {
+            mma(dq[(i.value - KB * 2 * LS) % DB], x, sf[(i.value - KB * 2 * LS) / DB % 2]);
+          }
+        },
+        [&](auto i) {
+          using std::integral_constant;
+          constexpr int apart = KB * (2 * LS + LO) / PIECES;
+          if constexpr (i.value % apart == 0 && i.value / apart < PIECES) piece(i.value / apart);
+          constexpr int last_score = KB * 2 * LS, phase = i.value < last_score ? i.value / LS : KB * 2 + (i.value - last_score) / LO;
+          constexpr int step = i.value < last_score ? i.value % LS : (i.value - last_score) % LO, steps = phase < KB * 2 ? LS : LO;
+          if constexpr (phase < KB * 2 && (phase & 1)) {
+            if constexpr (step == 0) shape(integral_constant<int, phase / 2>{});
+            spread<step, steps>([&](int r) { probability(phase / 2, r); });
+          }
+          if constexpr (KB == 2 && (phase == 2 || phase == 4)) {
+            constexpr int b = phase / 2 - 1;
+            spread<step, steps>([&](int r) { gradient(b, r); });
+            if constexpr (step == steps - 1) pack(integral_constant<int, b>{});
+          }
+          if constexpr (KB == 1 && phase == 1 && step == steps - 1) {
+            for_regs([&](int r) { gradient(0, r); });
+            pack(integral_constant<int, 0>{});
+          }
+        });
   }
+  wait_vmcnt0();
   if (there) store_row<T, DB>((T*)p.dq + (int64_t)mine * p.ldq + (int64_t)w.head * p.d, dq, p.scale, p.d, h);
 }
 
@@ -330,33 +445,35 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
 // over them is taken in its accumulators.  bfloat16: eight waves, two for the same keys, which take the two halves of a tile of queries and add
 // their sums up at the end; the keys' rows stay in LDS.  (Two waves a SIMD need 256 registers each, of which the sums take 128: with the
 // keys' rows in registers too there is one, and nothing runs while it waits.)  float: four waves, the keys' rows in registers.
-template <typename T, int DB> struct DkvLayout {
+template <typename T, int DB, int KW> struct DkvLayout {
   using Tile = Tile32<T, DB>;
-  static constexpr int HALVES = sizeof(T) == 2 ? 2 : 1, NW = 4 * HALVES, BM = 128, BQ = Tile::BN;
+  static constexpr int HALVES = sizeof(T) == 2 ? 2 : 1, NW = KW * HALVES, BM = 32 * KW, BQ = Tile::BN;
   static constexpr int KEYS = HALVES == 2 ? 2 * (BM / Tile::BN) * Tile::BYTES : 0;   // bytes of K and V
   static constexpr int STAGE = 2 * Tile::BYTES + 512;   // queries, their outputs' gradients, log-sum-exps and deltas
-  static constexpr int SUMS = HALVES == 2 ? 4 * DB * 16 * 64 * 4 : 0;   // one half's sums of one tensor
+  static constexpr int SUMS = HALVES == 2 ? KW * DB * 16 * 64 * 4 : 0;   // one half's sums of one tensor
   static constexpr int BYTES = KEYS + 2 * STAGE > SUMS ? KEYS + 2 * STAGE : SUMS;
 };
 
-template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW * 64), (DkvLayout<T, DB>::HALVES)) void attn_dkv_kernel(AttnParams p) {
+template <typename T, int DB, int KW>
+__global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, KW>::HALVES)) void attn_dkv_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;
-  using Layout = DkvLayout<T, DB>;
+  using Layout = DkvLayout<T, DB, KW>;
   constexpr int NW = Layout::NW, BM = Layout::BM, BQ = Layout::BQ, STAGE = Layout::STAGE;
   constexpr bool IN_LDS = Layout::HALVES == 2;
   constexpr int QB = BQ / 32 / Layout::HALVES;   // blocks of queries of a wave
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave & 3, half = wave >> 2;
-  const AttnRows w = attn_rows<BM>(p, p.kv_heads, lane, false);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave % KW, half = wave / KW;
+  const AttnRows w = attn_rows<BM>(p, p.parts, lane, false);
   if (w.empty) return;
+  const int kv = w.head / p.parts, part = w.head - kv * p.parts, group = p.group / p.parts;   // its query heads
   const int w0 = w.first + key_wave * 32;
   const int w1 = w0 + 31 < w.end ? w0 + 31 : w.end - 1;
   const int mine = w0 + c < w.end ? w0 + c : w.end - 1;
   const bool there = w0 + c < w.end;
 
-  const T* kbase = (const T*)p.k + (int64_t)w.head * p.d;
-  const T* vbase = (const T*)p.v + (int64_t)w.head * p.d;
+  const T* kbase = (const T*)p.k + (int64_t)kv * p.d;
+  const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
   const int q_lo = queries_lo(p, w, w.first), q_hi = w.dead ? q_lo : queries_hi(p, w, last);
   const int lo = queries_lo(p, w, mine), span = queries_hi(p, w, mine) - lo;
@@ -366,7 +483,6 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
   const float c2 = shaped ? 1.f : p.c2;
 
   const Tile32Reads<T, DB> at(lane);
-  const Tile32Loader<T, DB, NW> qload(lane, wave, p.ldq, p.d), dload(lane, wave, p.ldo, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   typename DirectFrag<T>::type kf[IN_LDS ? 1 : Tile::STEPS], vf[IN_LDS ? 1 : Tile::STEPS];
   const char *ks = smem + Tile::block(key_wave), *vs = ks + Layout::KEYS / 2;   // this wave's keys
@@ -388,84 +504,135 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{};
-  const int per_head = (q_hi - q_lo + BQ - 1) / BQ, tiles = per_head * p.group;
-  auto issue = [&](int head, int tile, int t) {
-    const int row = q_lo + tile * BQ;
-    const uint32_t stage = lds + Layout::KEYS + (t & 1) * STAGE;
-    qload.issue((const T*)p.q + (int64_t)head * p.d, row, q_hi - row, p.ldq, p.d, stage, wave);
-    dload.issue((const T*)p.dout + (int64_t)head * p.d, row, q_hi - row, p.ldo, p.d, stage + Tile::BYTES, wave);
-    if (wave < 2) {
-      const int rows = q_hi - row < BQ ? q_hi - row : BQ;
-      const u32x4 rsrc = make_rsrc((wave ? p.delta : p.lse) + (int64_t)head * p.n + row, rows * 4);
-      buffer_to_lds_b32(rsrc, lane * 4, stage + 2 * Tile::BYTES + wave * 256);
+  const int per_head = (q_hi - q_lo + BQ - 1) / BQ, tiles = per_head * group;
+  using QLoader = Tile32Loader<T, DB, NW>;
+  const QLoader qload(lane, wave, p.ldq, p.d), dload(lane, wave, p.ldo, p.d);
+  constexpr int PIECES = 2 * QLoader::LOADS + 1;
+  const int64_t first_head = (int64_t)kv * p.group + part * group;
+  Tile32Run<T, DB, NW> qrun((const T*)p.q + first_head * p.d, q_lo, q_hi - q_lo, p.ldq, p.d), drun((const T*)p.dout + first_head * p.d, q_lo, q_hi - q_lo, p.ldo, p.d);
+  u32x4 srows = make_rsrc((wave ? p.delta : p.minus) + first_head * p.n + q_lo, (q_hi - q_lo) * 4);
+  uint32_t stage = lds + Layout::KEYS, stats_at = lane * 4;
+  // the transfers of the tile of queries behind the one that they are at; the last head's last tile is followed by tiles without rows
+  auto next = [&](int tile, int t) {
+    stage = lds + Layout::KEYS + (t & 1) * STAGE;
+    if (tile == 0 && t < tiles) {
+      qrun.back(per_head, (int64_t)p.d * sizeof(T));
+      drun.back(per_head, (int64_t)p.d * sizeof(T));
+      const uint64_t at = ((uint64_t)srows[1] << 32 | srows[0]) + (uint64_t)p.n * 4;
+      srows[0] = (uint32_t)at;
+      srows[1] = (uint32_t)(at >> 32);
+      stats_at = lane * 4;
+    } else {
+      qrun.advance(t < tiles ? tile : per_head, per_head);
+      drun.advance(t < tiles ? tile : per_head, per_head);
+      stats_at += BQ * 4;
     }
   };
-  int head = w.head * p.group, tile = 0, next_head = head, next_tile = 0;
-  auto advance = [&](int& a, int& b) {
-    if (++b == per_head) {
-      b = 0;
-      ++a;
-    }
+  auto piece = [&](int i) {
+    if (i < QLoader::LOADS) qload.one(qrun.rsrc, i, stage, wave);
+    else if (i < 2 * QLoader::LOADS) dload.one(drun.rsrc, i - QLoader::LOADS, stage + Tile::BYTES, wave);
+    else if (wave < 2) buffer_to_lds_b32(srows, stats_at, stage + 2 * Tile::BYTES + wave * 256);
   };
-  if (tiles > 0) issue(head, 0, 0);
-  for (int t = 0; t < tiles; ++t, advance(head, tile)) {
+  auto pieces = [&]() {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) piece(i);
+  };
+  int head = (int)first_head, tile = 0, next_tile = 0;
+  if (tiles > 0) pieces();
+  for (int t = 0; t < tiles; ++t) {
     wait_vmcnt0();
     __syncthreads();
-    advance(next_head, next_tile);
-    if (t + 1 < tiles) issue(next_head, next_tile, t + 1);
+    if (t > 0) {
+      head += next_tile == 0;
+      tile = next_tile;
+    }
+    next_tile = tile + 1 == per_head ? 0 : tile + 1;
+    next(next_tile, t + 1);
     const int q0 = q_lo + tile * BQ + half * QB * 32;   // this wave's queries
-    if (w0 >= w.end || q0 >= any_hi || q0 + QB * 32 <= any_lo) continue;
+    if (w0 >= w.end || q0 >= any_hi || q0 + QB * 32 <= any_lo) {
+      pieces();
+      continue;
+    }
     const char* qs = smem + Layout::KEYS + (t & 1) * STAGE + Tile::block(half * QB);
     const char* ds = qs + Tile::BYTES;
     const float* stats = (const float*)(smem + Layout::KEYS + (t & 1) * STAGE + 2 * Tile::BYTES) + half * QB * 32;
     const float slope2 = p.slopes ? p.slopes[head] * kLog2e : 0.f;
     const bool masked = q0 < full_lo || q0 + QB * 32 > full_hi;
     static_for<0, QB>([&](auto block) {
-      constexpr int b = decltype(block)::value;
+      constexpr int b = block.value;
       f32x16 s{}, dp{}, by{};
-      using Frag = typename DirectFrag<T>::type;
-      if constexpr (IN_LDS) {
-        struct Pair { Frag q, k; };
-        products<2 * Tile::STEPS, 3>(
-            [&](auto i) {
-              constexpr bool second = i.value >= Tile::STEPS;
-              return Pair{at.row((second ? ds : qs) + Tile::block(b), i.value % Tile::STEPS), at.row(second ? vs : ks, i.value % Tile::STEPS)};
-            },
-            [&](auto i, const Pair& x) { mma(i.value < Tile::STEPS ? s : dp, x.q, x.k); });
-      } else {
-        products<2 * Tile::STEPS, 4>([&](auto i) { return at.row((i.value < Tile::STEPS ? qs : ds) + Tile::block(b), i.value % Tile::STEPS); },
-                                     [&](auto i, const Frag& x) {
-                                       if constexpr (i.value < Tile::STEPS) mma(s, x, kf[i.value]);
-                                       else mma(dp, x, vf[i.value - Tile::STEPS]);
-                                     });
-      }
-      if (shaped) s = shape_scores<T, true>(p, s, slope2, q0 + 32 * b + 4 * h, mine, &by);
+      f32x4 minus[4], delta[4];
+      using Frag = typename TransFrag<T>::type;
+      Frag pf[2], sf[2];
+      struct Pair { Frag x, y; };
+      struct Single { Frag x; };
+      using Operands = std::conditional_t<IN_LDS, Pair, Single>;
+      // scores, dP (the probabilities), dV (dS), dK
+      constexpr int LS = Tile::STEPS, LO = 2 * DB;
+      products<2 * LS + 2 * LO, sizeof(T) == 2 ? 2 : 1>(
+          [&](auto i) {
+            Operands o;
+            if constexpr (i.value < 2 * LS) {
+              o.x = widened(at.row((i.value < LS ? qs : ds) + Tile::block(b), i.value % LS));
+              if constexpr (IN_LDS) o.y = widened(at.row(i.value < LS ? ks : vs, i.value % LS));
+            } else {
+              o.x = at.column(i.value < 2 * LS + LO ? ds : qs, 2 * b + (i.value - 2 * LS) % LO / DB, (i.value - 2 * LS) % DB);
+            }
+            return o;
+          },
+          [&](auto i, const Operands& o) {
+            if constexpr (i.value < 2 * LS) {
+              f32x16& to = i.value < LS ? s : dp;
+              if constexpr (IN_LDS) mma(to, narrowed<T>(o.x), narrowed<T>(o.y));
+              else mma(to, narrowed<T>(o.x), i.value < LS ? kf[i.value % LS] : vf[i.value % LS]);
+            } else if constexpr (i.value < 2 * LS + LO) {
+              mma(dv[(i.value - 2 * LS) % DB], o.x, pf[(i.value - 2 * LS) / DB]);
+            } else {
+              mma(dk[(i.value - 2 * LS) % DB], o.x, sf[(i.value - 2 * LS - LO) / DB]);
+            }
+          },
+          [&](auto i) {
+            constexpr int apart = (2 * LS + 2 * LO) / PIECES;
+            if constexpr (b == 0 && i.value % apart == 0 && i.value / apart < PIECES) piece(i.value / apart);
+            constexpr int phase = i.value < 2 * LS ? i.value / LS : 2 + (i.value - 2 * LS) / LO;
+            constexpr int step = i.value < 2 * LS ? i.value % LS : (i.value - 2 * LS) % LO, steps = phase < 2 ? LS : LO;
+            if constexpr (phase == 0 && step == 0) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 lse = *(const f32x4*)(stats + 32 * b + 8 * g + 4 * h), delta = *(const f32x4*)(stats + 64 + 32 * b + 8 * g + 4 * h);
+              for (int g = 0; g < 4; ++g) minus[g] = *(const f32x4*)(stats + 32 * b + 8 * g + 4 * h);
+            }
+            if constexpr (phase == 1) {
+              if constexpr (step == 0) {
+                if (shaped) s = shape_scores<T, true>(p, s, slope2, q0 + 32 * b + 4 * h, mine, &by);
+              }
+              spread<step, steps>([&](int r) { s[r] = here(fast_exp2(__builtin_fmaf(s[r], c2, minus[r >> 2][r & 3]))); });
+              if constexpr (step == steps - 1) {
+                if (masked) {
+                  const int base = q0 + 32 * b + 4 * h - lo;
+                  for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[r] = 0.f; });
+                }
+                pf[0] = here(step_operand<T>(s, 0));
+                pf[1] = here(step_operand<T>(s, 1));
+                if (p.cap2 > 0.f) s *= by;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * g + e;
-          const float minus = lse[e] == -INFINITY ? -INFINITY : lse[e] * -kLog2e;
-          s[r] = fast_exp2(__builtin_fmaf(s[r], c2, minus));
-          dp[r] = s[r] * (dp[r] - delta[e]);
-        }
-      }
-      if (p.cap2 > 0.f) dp *= by;
-      if (masked) {
-        const int base = q0 + 32 * b + 4 * h - lo;
-        for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[r] = dp[r] = 0.f; });
-      }
-      const typename TransFrag<T>::type pf[2] = {step_operand<T>(s, 0), step_operand<T>(s, 1)}, sf[2] = {step_operand<T>(dp, 0), step_operand<T>(dp, 1)};
-      products<4 * DB, 4>([&](auto i) { return at.column(i.value & 1 ? qs : ds, 2 * b + i.value / 2 / DB, i.value / 2 % DB); },
-                          [&](auto i, auto x) {
-                            if constexpr (i.value & 1) mma(dk[i.value / 2 % DB], x, sf[i.value / 2 / DB]);
-                            else mma(dv[i.value / 2 % DB], x, pf[i.value / 2 / DB]);
-                          });
+                for (int g = 0; g < 4; ++g) delta[g] = *(const f32x4*)(stats + 64 + 32 * b + 8 * g + 4 * h);
+              }
+            }
+            if constexpr (phase == 2) {
+              spread<step, steps>([&](int r) { dp[r] = here(s[r] * (dp[r] - delta[r >> 2][r & 3])); });
+              if constexpr (step == steps - 1) {
+                if (masked) {   // (a probability of zero does not make what is not finite zero)
+                  const int base = q0 + 32 * b + 4 * h - lo;
+                  for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) dp[r] = 0.f; });
+                }
+                sf[0] = here(step_operand<T>(dp, 0));
+                sf[1] = here(step_operand<T>(dp, 1));
+              }
+            }
+          });
     });
   }
+  wait_vmcnt0();
   if constexpr (IN_LDS) {   // the second half's sums to the first
-    wait_vmcnt0();
     float* sums = (float*)smem + key_wave * DB * 16 * 64 + lane;
     auto meet = [&](f32x16* x) {
       __syncthreads();
@@ -484,8 +651,36 @@ template <typename T, int DB> __global__ __launch_bounds__((DkvLayout<T, DB>::NW
     if (half) return;
   }
   if (!there) return;
-  store_row<T, DB>((T*)p.dk + (int64_t)mine * p.ldk + (int64_t)w.head * p.d, dk, p.scale, p.d, h);
-  store_row<T, DB>((T*)p.dv + (int64_t)mine * p.ldv + (int64_t)w.head * p.d, dv, 1.f, p.d, h);
+  if (p.parts > 1) {
+    float* to = p.part + ((int64_t)part * 2 * p.n + mine) * p.kv_heads * p.d + (int64_t)kv * p.d;
+    store_row<float, DB>(to, dk, p.scale, p.d, h);
+    store_row<float, DB>(to + (int64_t)p.n * p.kv_heads * p.d, dv, 1.f, p.d, h);
+    return;
+  }
+  store_row<T, DB>((T*)p.dk + (int64_t)mine * p.ldk + (int64_t)kv * p.d, dk, p.scale, p.d, h);
+  store_row<T, DB>((T*)p.dv + (int64_t)mine * p.ldv + (int64_t)kv * p.d, dv, 1.f, p.d, h);
+}
+
+// dK and dV from the parts of several groups of query heads, four channels a lane.
+template <typename T> __global__ __launch_bounds__(256) void attn_parts_kernel(AttnParams p) {
+  const int width = p.kv_heads * p.d, quads = width / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)2 * p.n * quads) return;
+  const bool values = i >= (int64_t)p.n * quads;
+  const int64_t row = (values ? i - (int64_t)p.n * quads : i) / quads;
+  const int c = (int)(i % quads) * 4;
+  const float* from = p.part + i * 4;
+  f32x4 sum = *(const f32x4*)from;
+  for (int k = 1; k < p.parts; ++k) sum += *(const f32x4*)(from + (int64_t)k * 2 * p.n * width);
+  T* to = values ? (T*)p.dv + row * p.ldv + c : (T*)p.dk + row * p.ldk + c;
+  if constexpr (sizeof(T) == 2) {
+    bf16x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (bf16)sum[e];
+    *(bf16x4*)to = v;
+  } else {
+    *(f32x4*)to = sum;
+  }
 }
 
 }  // namespace acc

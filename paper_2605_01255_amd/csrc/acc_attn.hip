@@ -9,18 +9,27 @@
 namespace acc {
 namespace {
 
-constexpr int kWaves = 4;   // of a work-group
+// Work-groups of a kernel whose work-groups have `rows` rows of one of p.kv_heads * share heads.
+struct AttnGrid {
+  int tiles, strands, strand_tiles;
+  int64_t groups;
+};
+AttnGrid attn_grid(const acc_attn_desc* d, int64_t seq, int64_t rows, int64_t share) {
+  const int64_t tiles = d->docs ? d->n / rows + d->docs + 2 : ceil_div(d->n, seq) * ceil_div(seq, rows);
+  int strands = 1;
+  while (d->kv_heads * strands % 8) strands *= 2;
+  const int64_t strand_tiles = ceil_div(tiles, strands), groups = d->kv_heads * strands * strand_tiles * share;
+  return AttnGrid{(int)(tiles < INT32_MAX ? tiles : INT32_MAX), strands, (int)(strand_tiles < INT32_MAX ? strand_tiles : INT32_MAX), groups};
+}
 
 struct AttnPlan {
   AttnParams p;
-  int64_t groups, kv_groups;   // work-groups over the queries, over the keys
-  size_t delta, backward;      // workspace
+  int waves, key_waves;                // of a work-group: over the queries; over the keys (their halves apart)
+  AttnGrid queries, keys;
+  size_t minus, delta, part, backward; // workspace
 };
 
-int64_t attn_tiles(const acc_attn_desc* d, int64_t seq, int64_t rows) {
-  if (d->docs) return d->n / rows + d->docs + 2;
-  return ceil_div(d->n, seq) * ceil_div(seq, rows);
-}
+constexpr int64_t kFewGroups = 512, kFewKeyGroups = 512;
 
 int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   if (!d || (d->flags & ~(uint32_t)ACC_ATTN_CAUSAL)) return ACC_ERR_INVALID_ARG;
@@ -41,10 +50,6 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
     if (ld % 8 || ld > 1 << 18) return ACC_ERR_SHAPE;
   if (p.ldq < d->heads * d->d || p.ldo < d->heads * d->d || p.ldk < d->kv_heads * d->d || p.ldv < d->kv_heads * d->d) return ACC_ERR_SHAPE;
   const int64_t seq = d->seq && d->seq < d->n ? d->seq : d->n;
-  const int64_t tiles = attn_tiles(d, seq, 32 * kWaves);
-  plan->groups = round_up(d->heads * tiles, 8);
-  plan->kv_groups = round_up(d->kv_heads * tiles, 8);
-  if (plan->groups >= 1 << 24) return ACC_ERR_SHAPE;
   p.n = (int)d->n;
   p.docs = (int)d->docs;
   p.seq = (int)seq;
@@ -52,15 +57,28 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   p.kv_heads = (int)d->kv_heads;
   p.group = p.heads / p.kv_heads;
   p.d = (int)d->d;
-  p.tiles = (int)tiles;
   p.causal = causal;
   p.window = d->window > d->n ? 0 : (int)d->window;   // no row is that far away
   p.scale = d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->d);
   p.c2 = p.scale * kLog2e;
   p.cap2 = d->cap * kLog2e;
   p.inv_cap = d->cap > 0.f ? p.scale / d->cap : 0.f;
-  plan->delta = 0;
-  plan->backward = (size_t)round_up(d->heads * d->n * 4, 256);
+  const bool b16 = d->io_dtype == ACC_BF16;
+  // Work-groups of 64 rows, not of 128, for float, whose products take sixteen times as long as their rows' transfers, and where those of 128
+  // leave compute units idle.
+  plan->waves = b16 && attn_grid(d, seq, 128, p.group).groups >= kFewGroups ? 4 : 2;
+  plan->queries = attn_grid(d, seq, 32 * plan->waves, p.group);
+  plan->key_waves = b16 && attn_grid(d, seq, 128, 1).groups >= kFewKeyGroups ? 4 : 2;
+  // Query heads that share keys are dealt to several work-groups where there are few, and their sums added up by a kernel of its own.
+  p.parts = 1;
+  for (int parts = 2; parts <= p.group; ++parts)
+    if (p.group % parts == 0 && attn_grid(d, seq, 32 * plan->key_waves, p.parts).groups < kFewKeyGroups) p.parts = parts;
+  plan->keys = attn_grid(d, seq, 32 * plan->key_waves, p.parts);
+  if (plan->queries.groups >= 1 << 24 || plan->keys.groups >= 1 << 24) return ACC_ERR_SHAPE;
+  plan->minus = 0;
+  plan->delta = (size_t)round_up(d->heads * d->n * 4, 256);
+  plan->part = 2 * plan->delta;
+  plan->backward = plan->part + (p.parts > 1 ? (size_t)p.parts * 2 * d->n * d->kv_heads * d->d * 4 : 0);
   return ACC_OK;
 }
 
@@ -80,6 +98,20 @@ template <typename F> void with_attn(const acc_attn_desc* d, F&& f) {
   };
   if (d->io_dtype == ACC_BF16) typed(bf16{});
   else typed(float{});
+}
+
+// f(waves as a constant); float has two.
+template <typename T, typename F> void with_waves(int waves, F&& f) {
+  if constexpr (sizeof(T) == 2) {
+    if (waves == 4) return f(std::integral_constant<int, 4>{});
+  }
+  f(std::integral_constant<int, 2>{});
+}
+
+void on_grid(AttnParams& p, const AttnGrid& g) {
+  p.tiles = g.tiles;
+  p.strands = g.strands;
+  p.strand_tiles = g.strand_tiles;
 }
 
 }  // namespace
@@ -112,7 +144,11 @@ int acc_attn_fwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    L.launch_lds(attn_fwd_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
+    on_grid(p, plan.queries);
+    with_waves<T>(plan.waves, [&](auto nw) {
+      constexpr int NW = decltype(nw)::value;
+      L.launch_lds(attn_fwd_kernel<T, DB, NW>, dim3((unsigned)plan.queries.groups), dim3(NW * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
+    });
   });
   return L.status();
 }
@@ -134,14 +170,25 @@ int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   AttnParams p = plan.p;
   p.q = Q; p.k = K; p.v = V; p.o_in = O; p.lse = const_cast<float*>(lse); p.dout = dO;
   p.dq = dQ; p.dk = dK; p.dv = dV;
+  p.minus = (float*)((char*)workspace + plan.minus);
   p.delta = (float*)((char*)workspace + plan.delta);
+  p.part = (float*)((char*)workspace + plan.part);
   p.starts = starts; p.prefix = prefix; p.slopes = slopes;
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    const size_t lds = 4 * Tile32<T, DB>::BYTES;
-    L.launch_lds(attn_dq_kernel<T, DB, kWaves>, dim3((unsigned)plan.groups), dim3(kWaves * 64), lds, p);
-    L.launch_lds(attn_dkv_kernel<T, DB>, dim3((unsigned)plan.kv_groups), dim3(DkvLayout<T, DB>::NW * 64), (size_t)DkvLayout<T, DB>::BYTES, p);
+    on_grid(p, plan.queries);
+    with_waves<T>(plan.waves, [&](auto nw) {
+      constexpr int NW = decltype(nw)::value;
+      L.launch_lds(attn_dq_kernel<T, DB, NW>, dim3((unsigned)plan.queries.groups), dim3(NW * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
+    });
+    on_grid(p, plan.keys);
+    with_waves<T>(plan.key_waves, [&](auto nw) {
+      constexpr int KW = decltype(nw)::value;
+      using Layout = DkvLayout<T, DB, KW>;
+      L.launch_lds(attn_dkv_kernel<T, DB, KW>, dim3((unsigned)plan.keys.groups), dim3(Layout::NW * 64), (size_t)Layout::BYTES, p);
+    });
+    if (p.parts > 1) L(attn_parts_kernel<T>, dim3((unsigned)ceil_div((int64_t)2 * p.n * p.kv_heads * p.d / 4, 256)), dim3(256), p);
   });
   return L.status();
 }

@@ -32,6 +32,13 @@ template <> struct DirectFrag<float> { using type = f32x4; };
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T> struct TransFrag { using type = bf16x8; };
 template <> struct TransFrag<float> { using type = f32x8; };
+// A direct operand where transposed ones go too.
+__device__ __forceinline__ bf16x8 widened(bf16x8 x) { return x; }
+__device__ __forceinline__ f32x8 widened(f32x4 x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1); }
+template <typename T> __device__ __forceinline__ typename DirectFrag<T>::type narrowed(typename TransFrag<T>::type x) {
+  if constexpr (sizeof(T) == 2) return x;
+  else return __builtin_shufflevector(x, x, 0, 1, 2, 3);
+}
 
 __device__ __forceinline__ void mma(f32x16& c, bf16x8 a, bf16x8 b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ void mma(f32x16& c, f32x4 a, f32x4 b) {
@@ -79,17 +86,32 @@ template <typename T, int DB> struct Tile32Reads {
   }
 };
 
-// N products in their order, product i on what read(i) gives, read AHEAD products before.  The fences keep the order: left alone the compiler
-// puts each read right in front of its product and waits for it.
-template <int N, int AHEAD, typename Read, typename Product> __device__ __forceinline__ void products(Read&& read, Product&& product) {
+// N products in their order: product(i, what read(i) gave AHEAD products before), and behind each of them work(i), what the vector pipe does
+// while the matrix pipe is busy.  The fences keep the order: left alone the compiler puts each read right in front of its product, and the
+// vector work in one piece behind them all.  (A product holds the vector pipe for 8 of its 32 clocks where instructions of the same wave
+// follow it, for 17 where another wave's do: 8 multiply-adds for a product take 24.4 ns in one wave, 26.9 from two, of 15.8 and 18.8 alone.)
+template <int N, int AHEAD, typename Read, typename Product, typename Work>
+__device__ __forceinline__ void products(Read&& read, Product&& product, Work&& work) {
   decltype(read(std::integral_constant<int, 0>{})) ring[AHEAD];
   static_for<0, (AHEAD < N ? AHEAD : N)>([&](auto i) { ring[i.value] = read(i); });
   __builtin_amdgcn_sched_barrier(0);
   static_for<0, N>([&](auto i) {
     product(i, ring[i.value % AHEAD]);
     if constexpr (i.value + AHEAD < N) ring[i.value % AHEAD] = read(std::integral_constant<int, i.value + AHEAD>{});
+    work(i);
     __builtin_amdgcn_sched_barrier(0);
   });
+}
+
+// x, computed here: what is only used behind a branch is moved there otherwise, past the fences.
+template <typename V> __device__ __forceinline__ V here(V x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// f(r) for the registers of a block that fall to step j of `steps`, the first of which is left out.
+template <int J, int STEPS, typename F> __device__ __forceinline__ void spread(F&& f) {
+  if constexpr (J > 0) static_for<16 * (J - 1) / (STEPS - 1), 16 * J / (STEPS - 1)>([&](auto r) { f((int)r.value); });
 }
 
 // The eight accumulators of step u as an operand.  bfloat16: each rounded once, as the product takes them.
@@ -147,11 +169,47 @@ template <typename T, int DB, int NW> struct Tile32Loader {
       src[t] = chunk * Tile::PER_CHUNK < d ? (uint32_t)(row * (int)ld * (int)sizeof(T) + (chunk << 4)) : 0xFFFFFFF0u;
     }
   }
+  __device__ __forceinline__ static u32x4 rows(const T* base, int64_t row, int there, int64_t ld, int d) {
+    return make_rsrc(base + row * ld, bytes(there, ld, d));
+  }
+  __device__ __forceinline__ static int64_t bytes(int there, int64_t ld, int d) {
+    return there > 0 ? ((int64_t)((there < Tile::BN ? there : Tile::BN) - 1) * ld + d) * (int64_t)sizeof(T) : 0;
+  }
+  // transfer t of LOADS
+  __device__ __forceinline__ void one(const u32x4& rsrc, int t, uint32_t lds, int wave) const { buffer_to_lds_b128(rsrc, src[t], 0, lds + (t * NW + wave) * kTileGroup); }
   __device__ __forceinline__ void issue(const T* base, int64_t row, int there, int64_t ld, int d, uint32_t lds, int wave) const {
-    const int rows = there < Tile::BN ? there : Tile::BN;
-    const u32x4 rsrc = make_rsrc(base + row * ld, ((int64_t)(rows - 1) * ld + d) * (int64_t)sizeof(T));
+    const u32x4 rsrc = rows(base, row, there, ld, d);
 #pragma unroll
-    for (int t = 0; t < LOADS; ++t) buffer_to_lds_b128(rsrc, src[t], 0, lds + (t * NW + wave) * kTileGroup);
+    for (int t = 0; t < LOADS; ++t) one(rsrc, t, lds, wave);
+  }
+};
+
+// One tile after another of a run of rows: the resource moves on by additions (made anew from row and count it is three times the scalar
+// instructions of a tile's transfers).  Behind the last tile there are no rows.
+template <typename T, int DB, int NW> struct Tile32Run {
+  using Loader = Tile32Loader<T, DB, NW>;
+  u32x4 rsrc;
+  uint32_t step, whole, rest;   // bytes of BN rows from the first to the first, of a whole tile, of the last one
+  __device__ __forceinline__ Tile32Run(const T* base, int64_t row, int count, int64_t ld, int d) {
+    constexpr int BN = Loader::Tile::BN;
+    step = __builtin_amdgcn_readfirstlane((uint32_t)(BN * ld * (int64_t)sizeof(T)));
+    whole = __builtin_amdgcn_readfirstlane((uint32_t)Loader::bytes(BN, ld, d));
+    rest = __builtin_amdgcn_readfirstlane((uint32_t)Loader::bytes(count - (count - 1) / BN * BN, ld, d));
+    rsrc = make_rsrc(base + row * ld, count > BN ? whole : rest);
+  }
+  // to tile t of `tiles`, the one behind that it is at
+  __device__ __forceinline__ void advance(int t, int tiles) {
+    const uint64_t at = ((uint64_t)rsrc[1] << 32 | rsrc[0]) + step;
+    rsrc[0] = (uint32_t)at;
+    rsrc[1] = (uint32_t)(at >> 32);
+    rsrc[2] = t + 1 < tiles ? whole : t + 1 == tiles ? rest : 0;
+  }
+  // the same rows of a matrix `bytes` further on
+  __device__ __forceinline__ void back(int tiles, int64_t bytes) {
+    const uint64_t at = ((uint64_t)rsrc[1] << 32 | rsrc[0]) + bytes - (uint64_t)(tiles - 1) * step;
+    rsrc[0] = (uint32_t)at;
+    rsrc[1] = (uint32_t)(at >> 32);
+    rsrc[2] = tiles > 1 ? whole : rest;
   }
 };
 
