@@ -35,7 +35,9 @@ struct AttnParams {
   int causal, window;
   float c2, scale;              // scale log2 e, scale
   float cap2, inv_cap;          // cap log2 e (0: none), scale / cap
-  float* part;                  // [parts][2][n][kv_heads d]: dK and dV of a part of the query heads that share them
+  // Where there are few work-groups each one's tiles are dealt to `parts` of them, which leave float sums here: [parts][n][heads d] (O, dQ) or
+  // [parts][2][n][kv_heads d] (dK, dV); part_stats [parts][2][heads][n]: the forward pass' maxima and sums of exponentials.
+  float *part, *part_stats;
   int parts;
 };
 
@@ -121,6 +123,17 @@ __device__ __forceinline__ int queries_hi(const AttnParams& p, const AttnRows& w
   return p.window && p.window < w.end - j ? j + p.window : w.end;
 }
 
+__device__ __forceinline__ void store_quad(float* to, f32x4 x) { *(f32x4*)to = x; }
+__device__ __forceinline__ void store_quad(bf16* to, f32x4 x) { *(bf16x4*)to = __builtin_convertvector(x, bf16x4); }
+
+// The part'th of `parts` runs of whole tiles of rows lo .. hi - 1.
+template <int BN> __device__ __forceinline__ void part_of(int& lo, int& hi, int part, int parts) {
+  if (parts == 1) return;
+  const int tiles = (hi - lo + BN - 1) / BN, from = tiles * part / parts, to = tiles * (part + 1) / parts;
+  hi = to < tiles ? lo + to * BN : hi;
+  lo += from * BN;
+}
+
 // Scores of one block (S, row 4 h of it at `at`, this lane's own row `own`) to their logits in units of log 2, in place, and the cap's
 // derivative; where there is neither cap nor bias they stay products, and the factor p.c2 is applied with the subtraction of the maximum.
 template <typename T, bool GRAD>
@@ -151,8 +164,10 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   constexpr int BM = NW * 32, BN = Tile::BN, KB = BN / 32;
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const AttnRows w = attn_rows<BM>(p, p.group, lane, true);
+  AttnRows w = attn_rows<BM>(p, p.group * p.parts, lane, true);
   if (w.empty) return;
+  const int part = w.head % p.parts;
+  w.head /= p.parts;
   const int kv = w.head / p.group;
   const int w0 = w.first + wave * 32;                        // this wave's rows
   const int w1 = w0 + 31 < w.end ? w0 + 31 : w.end - 1;
@@ -164,7 +179,8 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const T* kbase = (const T*)p.k + (int64_t)kv * p.d;
   const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
-  const int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
+  int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
+  part_of<BN>(k_lo, k_hi, part, p.parts);
   const int lo = keys_lo(p, w, mine), span = keys_hi(p, w, mine) - lo;
   const int full_lo = keys_lo(p, w, w1), full_hi = keys_hi(p, w, w0);       // tiles inside are seen whole by the wave
   const int any_lo = keys_lo(p, w, w0), any_hi = keys_hi(p, w, w1);         // tiles outside not at all
@@ -291,8 +307,36 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   wait_vmcnt0();
   if (!there) return;
   l = half_sum(l);
+  if (p.parts > 1) {
+    store_row<float, DB>(p.part + ((int64_t)part * p.n + mine) * p.heads * p.d + (int64_t)w.head * p.d, o, 1.f, p.d, h);
+    p.part_stats[((int64_t)(2 * part + h) * p.heads + w.head) * p.n + mine] = h ? l : m;
+    return;
+  }
   store_row<T, DB>((T*)p.o + (int64_t)mine * p.ldo + (int64_t)w.head * p.d, o, l == 0.f ? 0.f : 1.f / l, p.d, h);
   if (h == 0) p.lse[(int64_t)w.head * p.n + mine] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// O and the log-sum-exps from the parts, four channels a lane.
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+  const int quads = p.d / 4, row_quads = p.heads * quads;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)p.n * row_quads) return;
+  const int64_t row = i / row_quads;
+  const int head = (int)(i % row_quads) / quads, c = (int)(i % row_quads) * 4;
+  const float* stats = p.part_stats + (int64_t)head * p.n + row;
+  const int64_t side = (int64_t)p.heads * p.n;
+  float m = -INFINITY;
+  for (int k = 0; k < p.parts; ++k) m = fmaxf(m, stats[2 * k * side]);
+  float l = 0.f;
+  f32x4 sum{};
+  for (int k = 0; k < p.parts; ++k) {
+    const float by = m == -INFINITY ? 1.f : fast_exp2(stats[2 * k * side] - m);
+    l += by * stats[(2 * k + 1) * side];
+    sum += by * *(const f32x4*)(p.part + (int64_t)k * p.n * row_quads * 4 + i * 4);
+  }
+  sum *= l == 0.f ? 0.f : 1.f / l;
+  store_quad((T*)p.o + row * p.ldo + c, sum);
+  if (c % p.d == 0) p.lse[(int64_t)head * p.n + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---- backward: gradient of the queries -----------------------------------------------------------------------
@@ -303,8 +347,10 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   constexpr int BM = NW * 32, BN = Tile::BN, KB = BN / 32;
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const AttnRows w = attn_rows<BM>(p, p.group, lane, true);
+  AttnRows w = attn_rows<BM>(p, p.group * p.parts, lane, true);
   if (w.empty) return;
+  const int part = w.head % p.parts;
+  w.head /= p.parts;
   const int kv = w.head / p.group;
   const int w0 = w.first + wave * 32;
   const int w1 = w0 + 31 < w.end ? w0 + 31 : w.end - 1;
@@ -335,7 +381,8 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const T* kbase = (const T*)p.k + (int64_t)kv * p.d;
   const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
-  const int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
+  int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
+  part_of<BN>(k_lo, k_hi, part, p.parts);
   const int lo = keys_lo(p, w, mine), span = keys_hi(p, w, mine) - lo;
   const int full_lo = keys_lo(p, w, w1), full_hi = keys_hi(p, w, w0);
   const int any_lo = keys_lo(p, w, w0), any_hi = keys_hi(p, w, w1);
@@ -437,7 +484,9 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
         });
   }
   wait_vmcnt0();
-  if (there) store_row<T, DB>((T*)p.dq + (int64_t)mine * p.ldq + (int64_t)w.head * p.d, dq, p.scale, p.d, h);
+  if (!there) return;
+  if (p.parts > 1) store_row<float, DB>(p.part + ((int64_t)part * p.n + mine) * p.heads * p.d + (int64_t)w.head * p.d, dq, p.scale, p.d, h);
+  else store_row<T, DB>((T*)p.dq + (int64_t)mine * p.ldq + (int64_t)w.head * p.d, dq, p.scale, p.d, h);
 }
 
 // ---- backward: gradients of the keys and values --------------------------------------------------------------
@@ -466,7 +515,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_wave = wave % KW, half = wave / KW;
   const AttnRows w = attn_rows<BM>(p, p.parts, lane, false);
   if (w.empty) return;
-  const int kv = w.head / p.parts, part = w.head - kv * p.parts, group = p.group / p.parts;   // its query heads
+  const int kv = w.head / p.parts, part = w.head - kv * p.parts;
   const int w0 = w.first + key_wave * 32;
   const int w1 = w0 + 31 < w.end ? w0 + 31 : w.end - 1;
   const int mine = w0 + c < w.end ? w0 + c : w.end - 1;
@@ -504,14 +553,18 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{};
-  const int per_head = (q_hi - q_lo + BQ - 1) / BQ, tiles = per_head * group;
+  // this part's tiles: of query head `head` from `tile` on, then those of the heads behind it
+  const int per_head = (q_hi - q_lo + BQ - 1) / BQ, all = per_head * p.group;
+  const int from = (int)((int64_t)all * part / p.parts), tiles = (int)((int64_t)all * (part + 1) / p.parts) - from;
+  int head = kv * p.group + (per_head ? from / per_head : 0), tile = per_head ? from % per_head : 0, next_tile = 0;
   using QLoader = Tile32Loader<T, DB, NW>;
   const QLoader qload(lane, wave, p.ldq, p.d), dload(lane, wave, p.ldo, p.d);
   constexpr int PIECES = 2 * QLoader::LOADS + 1;
-  const int64_t first_head = (int64_t)kv * p.group + part * group;
-  Tile32Run<T, DB, NW> qrun((const T*)p.q + first_head * p.d, q_lo, q_hi - q_lo, p.ldq, p.d), drun((const T*)p.dout + first_head * p.d, q_lo, q_hi - q_lo, p.ldo, p.d);
-  u32x4 srows = make_rsrc((wave ? p.delta : p.minus) + first_head * p.n + q_lo, (q_hi - q_lo) * 4);
-  uint32_t stage = lds + Layout::KEYS, stats_at = lane * 4;
+  Tile32Run<T, DB, NW> qrun((const T*)p.q + (int64_t)head * p.d, q_lo, q_hi - q_lo, p.ldq, p.d), drun((const T*)p.dout + (int64_t)head * p.d, q_lo, q_hi - q_lo, p.ldo, p.d);
+  qrun.skip(tile, per_head);
+  drun.skip(tile, per_head);
+  u32x4 srows = make_rsrc((wave ? p.delta : p.minus) + (int64_t)head * p.n + q_lo, (q_hi - q_lo) * 4);
+  uint32_t stage = lds + Layout::KEYS, stats_at = (tile * BQ + lane) * 4;
   // the transfers of the tile of queries behind the one that they are at; the last head's last tile is followed by tiles without rows
   auto next = [&](int tile, int t) {
     stage = lds + Layout::KEYS + (t & 1) * STAGE;
@@ -537,7 +590,6 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) piece(i);
   };
-  int head = (int)first_head, tile = 0, next_tile = 0;
   if (tiles > 0) pieces();
   for (int t = 0; t < tiles; ++t) {
     wait_vmcnt0();
@@ -596,7 +648,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
             if constexpr (b == 0 && i.value % apart == 0 && i.value / apart < PIECES) piece(i.value / apart);
             constexpr int phase = i.value < 2 * LS ? i.value / LS : 2 + (i.value - 2 * LS) / LO;
             constexpr int step = i.value < 2 * LS ? i.value % LS : (i.value - 2 * LS) % LO, steps = phase < 2 ? LS : LO;
-            if constexpr (phase == 0 && step == 0) {
+            if constexpr (phase == (IN_LDS ? 0 : 1) && step == 0) {
 #pragma unroll
               for (int g = 0; g < 4; ++g) minus[g] = *(const f32x4*)(stats + 32 * b + 8 * g + 4 * h);
             }
@@ -661,26 +713,17 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   store_row<T, DB>((T*)p.dv + (int64_t)mine * p.ldv + (int64_t)kv * p.d, dv, 1.f, p.d, h);
 }
 
-// dK and dV from the parts of several groups of query heads, four channels a lane.
-template <typename T> __global__ __launch_bounds__(256) void attn_parts_kernel(AttnParams p) {
-  const int width = p.kv_heads * p.d, quads = width / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)2 * p.n * quads) return;
-  const bool values = i >= (int64_t)p.n * quads;
-  const int64_t row = (values ? i - (int64_t)p.n * quads : i) / quads;
-  const int c = (int)(i % quads) * 4;
-  const float* from = p.part + i * 4;
-  f32x4 sum = *(const f32x4*)from;
-  for (int k = 1; k < p.parts; ++k) sum += *(const f32x4*)(from + (int64_t)k * 2 * p.n * width);
-  T* to = values ? (T*)p.dv + row * p.ldv + c : (T*)p.dk + row * p.ldk + c;
-  if constexpr (sizeof(T) == 2) {
-    bf16x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (bf16)sum[e];
-    *(bf16x4*)to = v;
-  } else {
-    *(f32x4*)to = sum;
-  }
+// One or two matrices [n, width] as sums of their parts [parts][matrices][n][width], four channels a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_parts_kernel(const float* part, int parts, int64_t n, int width, T* first, int64_t ld_first, T* second, int64_t ld_second) {
+  const int quads = width / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (second ? 2 : 1) * n * quads;
+  if (i >= all) return;
+  f32x4 sum = *(const f32x4*)(part + i * 4);
+  for (int k = 1; k < parts; ++k) sum += *(const f32x4*)(part + (k * all + i) * 4);
+  const int64_t row = i / quads;
+  const int c = (int)(i - row * quads) * 4;
+  store_quad(row < n ? first + row * ld_first + c : second + (row - n) * ld_second + c, sum);
 }
 
 }  // namespace acc

@@ -26,10 +26,12 @@ struct AttnPlan {
   AttnParams p;
   int waves, key_waves;                // of a work-group: over the queries; over the keys (their halves apart)
   AttnGrid queries, keys;
-  size_t minus, delta, part, backward; // workspace
+  int query_parts, key_parts;
+  size_t stats, forward, minus, delta, part, backward;   // workspace
 };
 
-constexpr int64_t kFewGroups = 512, kFewKeyGroups = 512;
+// Work-groups that fill the card: two of the queries' on a compute unit; of the keys' one, and more of them so that the last round is short.
+constexpr int64_t kFewGroups = 512, kFewKeyGroups = 640;
 
 int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   if (!d || (d->flags & ~(uint32_t)ACC_ATTN_CAUSAL)) return ACC_ERR_INVALID_ARG;
@@ -64,21 +66,32 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   p.cap2 = d->cap * kLog2e;
   p.inv_cap = d->cap > 0.f ? p.scale / d->cap : 0.f;
   const bool b16 = d->io_dtype == ACC_BF16;
-  // Work-groups of 64 rows, not of 128, for float, whose products take sixteen times as long as their rows' transfers, and where those of 128
-  // leave compute units idle.
-  plan->waves = b16 && attn_grid(d, seq, 128, p.group).groups >= kFewGroups ? 4 : 2;
-  plan->queries = attn_grid(d, seq, 32 * plan->waves, p.group);
-  plan->key_waves = b16 && attn_grid(d, seq, 128, 1).groups >= kFewKeyGroups ? 4 : 2;
-  // Query heads that share keys are dealt to several work-groups where there are few, and their sums added up by a kernel of its own.
-  p.parts = 1;
-  for (int parts = 2; parts <= p.group; ++parts)
-    if (p.group % parts == 0 && attn_grid(d, seq, 32 * plan->key_waves, p.parts).groups < kFewKeyGroups) p.parts = parts;
-  plan->keys = attn_grid(d, seq, 32 * plan->key_waves, p.parts);
+  const int64_t tile = b16 ? 64 : 32, length = d->docs ? ceil_div(d->n, d->docs) : seq;   // rows of a tile; of a document, on average
+  const int64_t seen = d->window && d->window < length ? d->window : length;
+  // Work-groups of 64 rows, not of 128: for float, whose products take sixteen times as long as their rows' transfers; for short documents, and for
+  // keys of few tokens, where a row's time is its work-group's.
+  plan->waves = b16 && length > 64 ? 4 : 2;
+  plan->key_waves = b16 && d->heads * ceil_div(d->n, 128) >= 128 ? 4 : 2;
+  // Parts: so many that the compute units are filled, of two tiles each at least.
+  auto parts_of = [&](int64_t groups, int64_t tiles, int64_t few) {
+    int64_t parts = (b16 ? few : 2 * few) / groups;
+    if (parts > tiles / 2) parts = tiles / 2;
+    return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+  };
+  plan->query_parts = parts_of(d->heads * ceil_div(d->n, 32 * plan->waves), ceil_div(seen, tile), kFewGroups);
+  plan->key_parts = parts_of(d->kv_heads * ceil_div(d->n, 32 * plan->key_waves), ceil_div(seen, tile) * p.group, kFewKeyGroups);
+  plan->queries = attn_grid(d, seq, 32 * plan->waves, p.group * plan->query_parts);
+  plan->keys = attn_grid(d, seq, 32 * plan->key_waves, plan->key_parts);
   if (plan->queries.groups >= 1 << 24 || plan->keys.groups >= 1 << 24) return ACC_ERR_SHAPE;
+  const int64_t query_floats = plan->query_parts > 1 ? (int64_t)plan->query_parts * d->n * d->heads * d->d : 0;
+  const int64_t key_floats = plan->key_parts > 1 ? (int64_t)plan->key_parts * 2 * d->n * d->kv_heads * d->d : 0;
+  plan->stats = (size_t)round_up(query_floats * 4, 256);
+  plan->forward = plan->stats + (plan->query_parts > 1 ? (size_t)plan->query_parts * 2 * d->heads * d->n * 4 : 0);
   plan->minus = 0;
   plan->delta = (size_t)round_up(d->heads * d->n * 4, 256);
-  plan->part = 2 * plan->delta;
-  plan->backward = plan->part + (p.parts > 1 ? (size_t)p.parts * 2 * d->n * d->kv_heads * d->d * 4 : 0);
+  plan->part = 2 * plan->delta;   // of the queries' gradient, then of the keys'
+  plan->backward = plan->part + (size_t)(query_floats > key_floats ? query_floats : key_floats) * 4;
+  if (plan->backward < plan->forward) plan->backward = plan->forward;
   return ACC_OK;
 }
 
@@ -108,7 +121,8 @@ template <typename T, typename F> void with_waves(int waves, F&& f) {
   f(std::integral_constant<int, 2>{});
 }
 
-void on_grid(AttnParams& p, const AttnGrid& g) {
+void on_grid(AttnParams& p, const AttnGrid& g, int parts) {
+  p.parts = parts;
   p.tiles = g.tiles;
   p.strands = g.strands;
   p.strand_tiles = g.strand_tiles;
@@ -123,8 +137,8 @@ extern "C" {
 
 size_t acc_attn_workspace_bytes(const acc_attn_desc* desc, int is_backward) {
   AttnPlan plan;
-  if (plan_attn(desc, &plan) != ACC_OK || !is_backward) return 0;
-  return plan.backward;
+  if (plan_attn(desc, &plan) != ACC_OK) return 0;
+  return is_backward ? plan.backward : plan.forward;
 }
 
 int acc_attn_fwd(const acc_attn_desc* desc, const void* Q, const void* K, const void* V, const int64_t* starts, const int64_t* prefix,
@@ -135,20 +149,24 @@ int acc_attn_fwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   if (!Q || !K || !V || !O || !lse) return ACC_ERR_INVALID_ARG;
   if ((rc = check_masks(desc, starts, prefix, slopes)) != ACC_OK) return rc;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace)) return ACC_ERR_ALIGN;
-  (void)ws_bytes;
+  if (plan.forward && (!workspace || ws_bytes < plan.forward)) return ACC_ERR_WORKSPACE;
   if ((rc = check_device()) != ACC_OK) return rc;
   Launcher L{(hipStream_t)stream};
   AttnParams p = plan.p;
   p.q = Q; p.k = K; p.v = V; p.o = O; p.lse = lse;
+  p.part = (float*)workspace;
+  p.part_stats = (float*)((char*)workspace + plan.stats);
   p.starts = starts; p.prefix = prefix; p.slopes = slopes;
+  auto quads = [&](int heads) { return dim3((unsigned)ceil_div((int64_t)p.n * heads * p.d / 4, 256)); };
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    on_grid(p, plan.queries);
+    on_grid(p, plan.queries, plan.query_parts);
     with_waves<T>(plan.waves, [&](auto nw) {
       constexpr int NW = decltype(nw)::value;
       L.launch_lds(attn_fwd_kernel<T, DB, NW>, dim3((unsigned)plan.queries.groups), dim3(NW * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
     });
+    if (p.parts > 1) L(attn_join_kernel<T>, quads(p.heads), dim3(256), p);
   });
   return L.status();
 }
@@ -174,21 +192,23 @@ int acc_attn_bwd(const acc_attn_desc* desc, const void* Q, const void* K, const 
   p.delta = (float*)((char*)workspace + plan.delta);
   p.part = (float*)((char*)workspace + plan.part);
   p.starts = starts; p.prefix = prefix; p.slopes = slopes;
+  auto quads = [&](int heads) { return dim3((unsigned)ceil_div((int64_t)p.n * heads * p.d / 4, 256)); };
   with_attn(desc, [&](auto value, auto db) {
     using T = decltype(value);
     constexpr int DB = decltype(db)::value;
-    on_grid(p, plan.queries);
+    on_grid(p, plan.queries, plan.query_parts);
     with_waves<T>(plan.waves, [&](auto nw) {
       constexpr int NW = decltype(nw)::value;
       L.launch_lds(attn_dq_kernel<T, DB, NW>, dim3((unsigned)plan.queries.groups), dim3(NW * 64), (size_t)4 * Tile32<T, DB>::BYTES, p);
     });
-    on_grid(p, plan.keys);
+    if (p.parts > 1) L(attn_parts_kernel<T>, quads(p.heads), dim3(256), p.part, p.parts, (int64_t)p.n, p.heads * p.d, (T*)dQ, p.ldq, (T*)nullptr, (int64_t)0);
+    on_grid(p, plan.keys, plan.key_parts);
     with_waves<T>(plan.key_waves, [&](auto nw) {
       constexpr int KW = decltype(nw)::value;
       using Layout = DkvLayout<T, DB, KW>;
       L.launch_lds(attn_dkv_kernel<T, DB, KW>, dim3((unsigned)plan.keys.groups), dim3(Layout::NW * 64), (size_t)Layout::BYTES, p);
     });
-    if (p.parts > 1) L(attn_parts_kernel<T>, dim3((unsigned)ceil_div((int64_t)2 * p.n * p.kv_heads * p.d / 4, 256)), dim3(256), p);
+    if (p.parts > 1) L(attn_parts_kernel<T>, quads(2 * p.kv_heads), dim3(256), p.part, p.parts, (int64_t)p.n, p.kv_heads * p.d, (T*)dK, p.ldk, (T*)dV, p.ldv);
   });
   return L.status();
 }

@@ -197,6 +197,12 @@ template <typename T, int DB, int NW> struct Tile32Run {
     rest = __builtin_amdgcn_readfirstlane((uint32_t)Loader::bytes(count - (count - 1) / BN * BN, ld, d));
     rsrc = make_rsrc(base + row * ld, count > BN ? whole : rest);
   }
+  __device__ __forceinline__ void skip(int t, int tiles) {
+    const uint64_t at = ((uint64_t)rsrc[1] << 32 | rsrc[0]) + (uint64_t)t * step;
+    rsrc[0] = (uint32_t)at;
+    rsrc[1] = (uint32_t)(at >> 32);
+    rsrc[2] = t + 1 < tiles ? whole : rest;
+  }
   // to tile t of `tiles`, the one behind that it is at
   __device__ __forceinline__ void advance(int t, int tiles) {
     const uint64_t at = ((uint64_t)rsrc[1] << 32 | rsrc[0]) + step;
