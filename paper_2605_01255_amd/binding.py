@@ -6,6 +6,7 @@ built, importing this module raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -494,19 +495,21 @@ def acc_embed_bwd(desc, ids, dY, dW, workspace, stream=None, ws_bytes=None):
     _check(_lib.acc_embed_bwd(ctypes.byref(desc), _ptr(ids), _ptr(dY), _ptr(dW), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
-def _code(t):
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError("gradients are bfloat16 or float32")
-    return ACC_BF16 if t.dtype == torch.bfloat16 else ACC_F32
+_GRAD_CODES = {torch.bfloat16: ACC_BF16, torch.float32: ACC_F32}
 
 
 def make_grad_list(tensors, outs=None):
     """The table of acc_grad_norm and acc_grad_scale: dense tensors and where they go when scaled (None: in place)."""
+    words = []   # of AccGradTensor: src, dst, count, both types (filled as one array: 0.8 us a tensor, 2 by fields)
     for a, b in zip(tensors, tensors if outs is None else outs, strict=True):
-        if not a.is_contiguous() or not b.is_contiguous() or a.numel() != b.numel():
+        count, code = a.numel(), _GRAD_CODES.get(a.dtype)
+        if not a.is_contiguous() or (b is not a and (not b.is_contiguous() or b.numel() != count)):
             raise ValueError("gradients and their outputs must be contiguous and of one size")
-    outs = tensors if outs is None else outs
-    return (AccGradTensor * len(tensors))(*((a.data_ptr(), b.data_ptr(), a.numel(), _code(a), _code(b)) for a, b in zip(tensors, outs)))
+        out = code if b is a else _GRAD_CODES.get(b.dtype)
+        if code is None or out is None:
+            raise TypeError("gradients are bfloat16 or float32")
+        words += a.data_ptr(), b.data_ptr(), count, code | out << 32
+    return (AccGradTensor * len(tensors)).from_buffer(array.array("q", words)) if words else (AccGradTensor * 0)()
 
 
 def make_factor_list(left, gr, flags=0):
@@ -514,12 +517,13 @@ def make_factor_list(left, gr, flags=0):
     rows = []
     for x, g in zip(left, gr, strict=True):
         d_out, r = g.shape if flags & ACC_FLAG_W_OUT_IN else g.shape[::-1]
-        if x.dtype != g.dtype or x.shape[1] != r:
-            raise ValueError("the factors of a gradient have one type and one rank")
+        code = _GRAD_CODES.get(x.dtype)
+        if code is None or x.dtype != g.dtype or x.shape[1] != r:
+            raise ValueError("the factors of a gradient have one type (bfloat16 or float32) and one rank")
         if x.stride(1) != 1 or g.stride(1) != 1:
             raise ValueError("the factors' rows must be contiguous")
         rows.append((x.data_ptr(), g.data_ptr(), x.shape[0], d_out, r, x.stride(0) if x.shape[0] > 1 else 0, g.stride(0) if g.shape[0] > 1 else 0,
-                     _code(x), flags))
+                     code, flags))
     return (AccGradFactors * len(rows))(*rows)
 
 

@@ -77,6 +77,7 @@ static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p)
   const int n = (int)p.n;
   // tokens of the buckets before this one, and of this one
   int before = 0, own = 0;
+#pragma unroll 8
   for (int i = tid; i < n; i += 1024) {
     const int64_t id = p.ids[i];
     const bool word = (uint64_t)id < (uint64_t)p.v;
@@ -108,13 +109,21 @@ static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p)
   int at = before;
   int2* list = p.list;
   if (own) {
+    int64_t ahead[4];
+    auto request = [&](int i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ahead[e] = i + e < n ? p.ids[i + e] : -1;
+    };
+    request(4 * tid);
     for (int i0 = 0, turn = 0; i0 < n; i0 += 4096, turn ^= 1) {
       const int i = i0 + 4 * tid;
       int64_t id[4];
       uint32_t mine = 0;
 #pragma unroll
+      for (int e = 0; e < 4; ++e) id[e] = ahead[e];
+      if (n - i > 4096) request(i + 4096);
+#pragma unroll
       for (int e = 0; e < 4; ++e) {
-        id[e] = i + e < n ? p.ids[i + e] : -1;
         if ((uint64_t)id[e] < (uint64_t)p.v && (int)(id[e] & (kBuckets - 1)) == bucket) mine |= 1u << e;
       }
       const int count = __popc(mine);
@@ -216,13 +225,15 @@ template <typename T, typename TD> __global__ __launch_bounds__(256) void embed_
   typedef T vec __attribute__((ext_vector_type(E)));
   if ((int)blockIdx.x >= p.grad_groups) {
     const int64_t e0 = (int64_t)(blockIdx.x - p.grad_groups) * 32;
-    const int chunks = p.d * (int)sizeof(TD) / 16;
-    for (int e = 0; e < 32; ++e) {
-      if (e0 + e >= (int64_t)kBuckets * p.bins) return;
-      const int b = (int)((e0 + e) / p.bins), key = (int)((e0 + e) - (int64_t)b * p.bins);
-      const int64_t id = ((int64_t)key << kBucketBits) + b;
-      if (id >= p.v || p.rows[e0 + e].y) continue;
-      for (int c = threadIdx.x; c < chunks; c += 256) *(u32x4*)((char*)p.dw + id * p.d * (int64_t)sizeof(TD) + (int64_t)c * 16) = u32x4{0, 0, 0, 0};
+    const int chunks = p.d * (int)sizeof(TD) / 16, lane = threadIdx.x & 63;
+    // (the counts of all 32 at once: one after another their loads took 10 us)
+    const int64_t mine = e0 + (lane & 31);
+    const int b = (int)(mine / p.bins);
+    const int64_t id = ((mine - (int64_t)b * p.bins) << kBucketBits) + b;
+    const bool empty = lane < 32 && mine < (int64_t)kBuckets * p.bins && id < p.v && p.rows[mine].y == 0;
+    for (uint64_t left = __ballot(empty); left; left &= left - 1) {
+      const int64_t word = __shfl(id, __ffsll((unsigned long long)left) - 1);
+      for (int c = threadIdx.x; c < chunks; c += 256) *(u32x4*)((char*)p.dw + word * p.d * (int64_t)sizeof(TD) + (int64_t)c * 16) = u32x4{0, 0, 0, 0};
     }
     return;
   }
@@ -243,6 +254,7 @@ template <typename T, typename TD> __global__ __launch_bounds__(256) void embed_
   };
   for (int q = p0; q < p1; q += 8) {
     int64_t id[8];
+    int2 places[8];
     vec x[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -251,12 +263,14 @@ template <typename T, typename TD> __global__ __launch_bounds__(256) void embed_
       x[k] = *(const vec*)((const T*)p.dy + (int64_t)token * p.ldy + col);
     }
 #pragma unroll
+    for (int k = 0; k < 8; ++k) places[k] = embed_row(p, id[k]);
+#pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (q + k >= p1) break;
       if (id[k] != word) {
         if (word >= 0) finish();
         word = id[k];
-        place = embed_row(p, word);
+        place = places[k];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = to_f32(x[k][e]);
       } else {

@@ -257,15 +257,25 @@ static __global__ __launch_bounds__(256) void gram_sum_kernel(GramSumList l, dou
   int ti = 0, tj = tile;
   while (tj > ti) tj -= ++ti;
   double sum = 0.0;
-  for (int e = threadIdx.x; e < 16 * kGramTile; e += 256) {
-    const int i = rows * 16 + e / kGramTile, j = e % kGramTile;
+  for (int e = threadIdx.x; e < 4 * kGramTile; e += 256) {   // four columns a lane
+    const int i = rows * 16 + e / (kGramTile / 4), j = e % (kGramTile / 4) * 4;
     if (ti * kGramTile + i >= a.r || tj * kGramTile + j >= a.r) continue;
-    auto total = [&](const GramSide& s) {
-      double t = 0.0;
-      for (uint32_t k = 0; k < s.splits; ++k) t += (double)l.g.parts[s.parts + ((int64_t)k * tiles + tile) * kGramTile * kGramTile + i * kGramTile + j];
-      return t;
-    };
-    sum += total(a) * total(b);
+    double one[2][4];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const GramSide& s = side ? b : a;
+      const float* from = l.g.parts + s.parts + (int64_t)tile * kGramTile * kGramTile + i * kGramTile + j;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) one[side][c] = 0.0;
+#pragma unroll 4
+      for (uint32_t k = 0; k < s.splits; ++k) {
+        const f32x4 x = *(const f32x4*)(from + (int64_t)k * tiles * kGramTile * kGramTile);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) one[side][c] += (double)x[c];
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sum += one[0][c] * one[1][c];
   }
   sum = group_sum(ti == tj ? sum : 2.0 * sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
