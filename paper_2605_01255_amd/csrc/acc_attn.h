@@ -426,7 +426,7 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
     const char* ks = smem + (t & 1) * 2 * Tile::BYTES;
     const char* vs = ks + Tile::BYTES;
     const bool masked = k0 < full_lo || k0 + BN > full_hi;
-    f32x16 s[KB], dp[KB], by{};
+    f32x16 s[KB], dp[KB], by;   // by: the cap's slope, where there is one
 #pragma unroll
     for (int b = 0; b < KB; ++b) s[b] = dp[b] = f32x16{};
     typename TransFrag<T>::type sf[2];
@@ -438,7 +438,7 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
     auto gradient = [&](int b, int r) { s[b][r] = here(s[b][r] * (dp[b][r] - delta)); };
     auto pack = [&](auto block) {
       constexpr int b = block.value;
-      if (p.cap2 > 0.f) s[b] *= by;
+      if (p.cap2 > 0.f) s[b] = here(s[b] * by);   // (a branch: sixteen selections otherwise)
       if (masked) {
         const int base = k0 + 32 * b + 4 * h - lo;
         for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) s[b][r] = 0.f; });
@@ -612,7 +612,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
     const bool masked = q0 < full_lo || q0 + QB * 32 > full_hi;
     static_for<0, QB>([&](auto block) {
       constexpr int b = block.value;
-      f32x16 s{}, dp{}, by{};
+      f32x16 s{}, dp{}, by;   // by: the cap's slope, where there is one
       f32x4 minus[4], delta[4];
       using Frag = typename TransFrag<T>::type;
       Frag pf[2], sf[2];
@@ -664,7 +664,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
                 }
                 pf[0] = here(step_operand<T>(s, 0));
                 pf[1] = here(step_operand<T>(s, 1));
-                if (p.cap2 > 0.f) s *= by;
+                if (p.cap2 > 0.f) s = here(s * by);   // (a branch: sixteen selections otherwise)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) delta[g] = *(const f32x4*)(stats + 64 + 32 * b + 8 * g + 4 * h);
               }
