@@ -518,6 +518,9 @@ def clip_grad_norm_(parameters, max_norm: float, modules=()):
     dev = every[0].device
     if any(t.is_sparse or t.dtype not in _CODES for t in every):
         raise TypeError("gradients must be dense, bfloat16 or float32")
+    scaled = [t.data_ptr() for t in grads + [gr for _, gr in pairs] if t.numel()]
+    if len(set(scaled)) < len(scaled):
+        raise ValueError("two parameters share one gradient, which would be scaled twice")
     if not every[0].is_cuda or any(t.device != dev for t in every):
         raise ValueError("all gradients must be on one GPU")
     dense = [g if g.is_contiguous() else g.contiguous() for g in grads]

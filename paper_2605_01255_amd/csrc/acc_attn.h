@@ -563,7 +563,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   Tile32Run<T, DB, NW> qrun((const T*)p.q + (int64_t)head * p.d, q_lo, q_hi - q_lo, p.ldq, p.d), drun((const T*)p.dout + (int64_t)head * p.d, q_lo, q_hi - q_lo, p.ldo, p.d);
   qrun.skip(tile, per_head);
   drun.skip(tile, per_head);
-  u32x4 srows = make_rsrc((wave ? p.delta : p.minus) + (int64_t)head * p.n + q_lo, (q_hi - q_lo) * 4);
+  u32x4 srows = make_rsrc((wave ? p.delta : p.minus) + (int64_t)head * p.n + q_lo, (int64_t)(q_hi - q_lo) * 4);
   uint32_t stage = lds + Layout::KEYS, stats_at = (tile * BQ + lane) * 4;
   // the transfers of the tile of queries behind the one that they are at; the last head's last tile is followed by tiles without rows
   auto next = [&](int tile, int t) {

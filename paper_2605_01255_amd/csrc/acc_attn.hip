@@ -82,7 +82,8 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   plan->key_parts = parts_of(d->kv_heads * ceil_div(d->n, 32 * plan->key_waves), ceil_div(seen, tile) * p.group, kFewKeyGroups);
   plan->queries = attn_grid(d, seq, 32 * plan->waves, p.group * plan->query_parts);
   plan->keys = attn_grid(d, seq, 32 * plan->key_waves, plan->key_parts);
-  if (plan->queries.groups >= 1 << 24 || plan->keys.groups >= 1 << 24) return ACC_ERR_SHAPE;
+  const int64_t key_threads = plan->key_waves * (b16 ? 128 : 64);
+  if (plan->queries.groups * plan->waves * 64 > UINT32_MAX || plan->keys.groups * key_threads > UINT32_MAX) return ACC_ERR_SHAPE;   // of a launch
   const int64_t query_floats = plan->query_parts > 1 ? (int64_t)plan->query_parts * d->n * d->heads * d->d : 0;
   const int64_t key_floats = plan->key_parts > 1 ? (int64_t)plan->key_parts * 2 * d->n * d->kv_heads * d->d : 0;
   plan->stats = (size_t)round_up(query_floats * 4, 256);

@@ -38,11 +38,16 @@ def _bwd(desc, O=0x4000, lse=0x5000, dO=0x7000, dQ=0x8000, dK=0x9000, dV=0xA000,
     (dict(ldv=120), -2), (dict(ldo=504), -2), (dict(ldo=(1 << 18) + 8), -2), (dict(docs=-1), -2), (dict(seq=-1), -2), (dict(window=-1), -1),
     (dict(window=5, flags=0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(cap=-2.0), -1),
     (dict(cap=float("nan")), -1), (dict(cap=float("inf")), -1), (dict(flags=2), -1), (dict(io_dtype=2), -4),
-    (dict(n=1 << 30, seq=1), -2)], ids=str)   # the last: more work-groups than a launch has
+    (dict(n=1 << 30, seq=1), -2), (dict(n=1 << 30, heads=1, kv_heads=1), -2)], ids=str)   # the last two: more threads than a launch has
 def test_descriptors_are_refused(bad, status):
     d = acc.make_attn_desc(**{**OK, **bad})
     assert _fwd(d) == status and _bwd(d) == status
     assert acc.acc_attn_workspace_bytes(d, True) == 0
+
+
+def test_as_many_rows_as_a_launch_has_threads_for():
+    d = acc.make_attn_desc(1 << 29, 1, 1, 8)
+    assert _fwd(d) in FINE and _bwd(d) in FINE
 
 
 def test_masks_that_do_not_go_together_are_refused():

@@ -1,0 +1,80 @@
+"""Attention through the C ABI at the sizes where the work-groups' shape and number change, with offsets beyond 32 bits, and with two captured
+graphs on one workspace; float64 bounds as in the other tests of it."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+from attn_util import Case
+
+
+@pytest.fixture(scope="module")
+def acc():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2605_01255_amd import binding
+    return binding
+
+
+# (sizes, whether the forward pass has each row's keys in parts)
+@pytest.mark.parametrize("kw,parts", [
+    (dict(n=520, heads=72, kv=72, d=40), False),                                          # whole rows, 128 of them a work-group
+    (dict(n=520, heads=72, kv=9, d=40, cap=20.0, bias=True), False),                      # the keys' gradients alone in parts
+    (dict(n=520, heads=72, kv=72, d=40, cuts=[3, 9, 70, 71, 200, 260, 300, 340, 400, 455, 510]), False),   # short documents: 64 rows
+    (dict(n=520, heads=72, kv=72, d=40, dtype="f32"), False),
+    (dict(n=300, heads=72, kv=72, d=40, dtype="f32", causal=False), True),
+    (dict(n=1030, heads=16, kv=16, d=24, window=200), True),
+    (dict(n=1030, heads=16, kv=4, d=24, prefix=[700]), True),
+    (dict(n=2100, heads=1, kv=1, d=128), True),                                           # as many parts as there are
+    (dict(n=2100, heads=1, kv=1, d=128, dtype="f32", cuts=[0, 1, 2099]), True),
+], ids=lambda x: str(x))
+def test_work_groups_of_every_shape_and_number(acc, kw, parts):
+    c = Case(**kw)
+    assert (acc.acc_attn_workspace_bytes(c.desc(acc), False) > 0) == parts
+    c.check(c.run(acc))
+
+
+def test_offsets_beyond_32_bits(acc):
+    """Rows 2^18 elements apart, 4.4 GB from the first to the last: the same bits as from rows one after another."""
+    import torch
+    n, ld = 8400, 1 << 18
+    c = Case(n, 2, 1, 64, cuts=[0, 100, n - 300, n], window=150)
+    dense = c.run(acc)
+    t, out = c.to_gpu(), c.outputs()
+    wide = torch.empty(n, ld, dtype=c.tdt, device="cuda")
+    back = torch.empty(n, ld, dtype=c.tdt, device="cuda")
+    q, k, v = (wide[:, a:b] for a, b in ((0, 128), (ld - 128, ld - 64), (ld - 64, ld)))
+    o, do = wide[:, 1024:1152], wide[:, 4096:4224]
+    for to, x in zip((q, k, v, do), (*c.split(t["qkv"]), t["dO"])):
+        to.copy_(x)
+    dq, dk, dv = (back[:, a:b] for a, b in ((0, 128), (ld - 128, ld - 64), (ld - 64, ld)))
+    desc = acc.make_attn_desc(n, 2, 1, 64, ldq=ld, ldk=ld, ldv=ld, ldo=ld, docs=3, window=150, io_dtype=acc.ACC_BF16, flags=acc.ACC_ATTN_CAUSAL)
+    ws = torch.empty(acc.acc_attn_workspace_bytes(desc, True), dtype=torch.uint8, device="cuda")
+    acc.acc_attn_fwd(desc, q, k, v, t["starts"], None, None, o, out["lse"], ws)
+    acc.acc_attn_bwd(desc, q, k, v, t["starts"], None, None, o, out["lse"], do, dq, dk, dv, ws)
+    assert torch.equal(o, dense["o"]) and torch.equal(out["lse"], dense["lse"])
+    for got, want in zip((dq, dk, dv), c.split(dense["dqkv"])):
+        assert torch.equal(got, want)
+
+
+def test_two_graphs_on_one_workspace(acc):
+    """Nothing is kept there from one call for the next."""
+    import torch
+    cases = [Case(700, 4, 2, 64, cuts=[0, 100, 650]), Case(300, 8, 1, 32, "f32", causal=False, cap=9.0)]
+    want = [c.run(acc) for c in cases]
+    ws = torch.empty(max(acc.acc_attn_workspace_bytes(c.desc(acc), True) for c in cases), dtype=torch.uint8, device="cuda")
+    held, graphs = [(c.to_gpu(), c.outputs()) for c in cases], []
+    for c, (t, out) in zip(cases, held):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.call(acc, t, out, ws)
+    for order in ((0, 1), (1, 0), (0, 0, 1)):
+        for _, out in held:
+            for x in out.values():
+                x.fill_(float("nan"))
+        for k in order:
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        for (_, out), first in zip(held, want):
+            assert all(torch.equal(out[k], first[k]) for k in first)
+        cases[0].run(acc)

@@ -143,6 +143,10 @@ def test_modules_refuse_before_the_gpu():
     p.grad = torch.ones(4)
     with pytest.raises(ValueError):
         ag.clip_grad_norm_(p, 1.0)
+    q = torch.nn.Parameter(torch.zeros(2, 2))
+    q.grad = p.grad.view(2, 2)                            # one gradient of two parameters
+    with pytest.raises(ValueError, match="share one gradient"):
+        ag.clip_grad_norm_([p, q], 1.0)
     p = torch.nn.Parameter(torch.zeros(4, dtype=torch.float64))
     p.grad = torch.ones(4, dtype=torch.float64)
     with pytest.raises(TypeError):
