@@ -30,7 +30,9 @@ struct AttnPlan {
   size_t stats, forward, minus, delta, part, backward;   // workspace
 };
 
-// Work-groups that fill the card: two of the queries' on a compute unit; of the keys' one, and more of them so that the last round is short.
+// Work-groups that fill the card: two of the queries' on a compute unit (float: four, of half the waves); of the keys' one, and more of them so
+// that the last round is short.  (6001 rows with a window of 1000, dK and dV: 153 + 9 us, with half as many 193, with twice as many 165 + 15;
+// one document of 8192 rows, 4 heads, O: 101 + 10, 167, 92 + 17.)
 constexpr int64_t kFewGroups = 512, kFewKeyGroups = 640;
 
 int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
@@ -68,18 +70,27 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   const bool b16 = d->io_dtype == ACC_BF16;
   const int64_t tile = b16 ? 64 : 32, length = d->docs ? ceil_div(d->n, d->docs) : seq;   // rows of a tile; of a document, on average
   const int64_t seen = d->window && d->window < length ? d->window : length;
-  // Work-groups of 64 rows, not of 128: for float, whose products take sixteen times as long as their rows' transfers; for short documents, and for
-  // keys of few tokens, where a row's time is its work-group's.
-  plan->waves = b16 && length > 64 ? 4 : 2;
-  plan->key_waves = b16 && d->heads * ceil_div(d->n, 128) >= 128 ? 4 : 2;
-  // Parts: so many that the compute units are filled, of two tiles each at least.
-  auto parts_of = [&](int64_t groups, int64_t tiles, int64_t few) {
-    int64_t parts = (b16 ? few : 2 * few) / groups;
-    if (parts > tiles / 2) parts = tiles / 2;
-    return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+  // Work-groups of 64 rows, not of 128, which share a tile's transfers among more waves:
+  //   float, whose products take sixteen times as long as their rows' transfers;
+  //   documents of up to 64 rows (8192 rows in 200 of them, 16 heads of 64 channels: forward and dQ 25 + 30 us, of 128 rows 30 + 50);
+  //   fewer than 128 of them with 128 rows (1024 rows, 8 heads of 128: 17 + 19 us and 7 to join parts, of 128 rows 16 + 21 and 11; 4096 rows, 32
+  //   heads: 241 + 280 us, of 128 rows 170 + 206);
+  //   for the keys' gradients heads of up to 64 channels, two work-groups of which fit a compute unit, so that one multiplies while the other
+  //   waits (16 heads of 64, documents of 2048 rows: 199 us, of 128 rows 241; 32 heads of 128, 4096 rows: 355 us, of 128 rows 296).
+  const int64_t whole = d->heads * ceil_div(d->n, 128);
+  plan->waves = b16 && length > 64 && whole >= 128 ? 4 : 2;
+  plan->key_waves = b16 && length > 64 && whole >= 128 && d->d > 64 ? 4 : 2;
+  // Parts: so many that the compute units are filled, of `least` tiles each at least.  A part is written and read as floats, which for the keys
+  // takes the time of seven of its tiles.  (Three float documents of 344 rows, 8 heads: 160 us in all, without parts 305; 2048 rows, 16 heads on
+  // 4 of 128 channels: dK and dV 56 + 8 us in 8 parts, 66 + 11 in 10, 190 in one; 40 documents of 51 rows: 14 us, in two parts 23 + 5.)
+  auto parts_of = [&](int64_t groups, int64_t tiles, int64_t few, int64_t least) {
+    int64_t parts = few / groups;
+    if (parts > tiles / least) parts = tiles / least;
+    if (parts > 16) parts = 16;
+    return (int)(parts < 1 ? 1 : parts);
   };
-  plan->query_parts = parts_of(d->heads * ceil_div(d->n, 32 * plan->waves), ceil_div(seen, tile), kFewGroups);
-  plan->key_parts = parts_of(d->kv_heads * ceil_div(d->n, 32 * plan->key_waves), ceil_div(seen, tile) * p.group, kFewKeyGroups);
+  plan->query_parts = parts_of(d->heads * ceil_div(d->n, 32 * plan->waves), ceil_div(seen, tile), b16 ? kFewGroups : 2 * kFewGroups, b16 ? 4 : 2);
+  plan->key_parts = parts_of(d->kv_heads * ceil_div(d->n, 32 * plan->key_waves), ceil_div(seen, tile) * p.group, kFewKeyGroups, b16 ? 16 : 2);
   plan->queries = attn_grid(d, seq, 32 * plan->waves, p.group * plan->query_parts);
   plan->keys = attn_grid(d, seq, 32 * plan->key_waves, plan->key_parts);
   const int64_t key_threads = plan->key_waves * (b16 ? 128 : 64);

@@ -18,12 +18,15 @@ def acc():
 
 # (sizes, whether the forward pass has each row's keys in parts)
 @pytest.mark.parametrize("kw,parts", [
-    (dict(n=520, heads=72, kv=72, d=40), False),                                          # whole rows, 128 of them a work-group
+    (dict(n=520, heads=72, kv=72, d=72), False),                                          # whole rows, 128 of them a work-group
+    (dict(n=520, heads=72, kv=72, d=40), False),                                          # the keys' gradients: 64 rows
+    (dict(n=520, heads=72, kv=9, d=104, cap=20.0), False),                                # in parts, of 128 rows
     (dict(n=520, heads=72, kv=9, d=40, cap=20.0, bias=True), False),                      # the keys' gradients alone in parts
     (dict(n=520, heads=72, kv=72, d=40, cuts=[3, 9, 70, 71, 200, 260, 300, 340, 400, 455, 510]), False),   # short documents: 64 rows
     (dict(n=520, heads=72, kv=72, d=40, dtype="f32"), False),
     (dict(n=300, heads=72, kv=72, d=40, dtype="f32", causal=False), True),
-    (dict(n=1030, heads=16, kv=16, d=24, window=200), True),
+    (dict(n=1030, heads=16, kv=16, d=24, window=200), False),
+    (dict(n=1030, heads=16, kv=16, d=24, window=600), True),
     (dict(n=1030, heads=16, kv=4, d=24, prefix=[700]), True),
     (dict(n=2100, heads=1, kv=1, d=128), True),                                           # as many parts as there are
     (dict(n=2100, heads=1, kv=1, d=128, dtype="f32", cuts=[0, 1, 2099]), True),
