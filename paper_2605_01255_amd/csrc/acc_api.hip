@@ -26,7 +26,7 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 namespace acc {
 namespace {
 
-constexpr int kVersion = 200;  // 0.2.0
+constexpr int kVersion = 300;  // 0.3.0
 
 SketchParams make_sketch_params(const acc_linear_desc* d) {
   SketchParams sk;

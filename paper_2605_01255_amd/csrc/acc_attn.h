@@ -164,7 +164,10 @@ __device__ __forceinline__ f32x16 shape_scores(const AttnParams& p, f32x16 s, fl
 constexpr float kSlack = 8.f;
 
 // ---- forward -------------------------------------------------------------------------------------------------
-// A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.
+// A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.  Tiles of 64 keys (float 32), two in LDS,
+// leave room for two work-groups on a compute unit.  Bound by power and by the vector instructions beside the matrix ones (six to one, of them
+// one exponential and one maximum a score): 4 x 4096 rows, 32 heads of 128 on 8, 608 to 654 us, 0.84 to 0.90 PFLOP/s, the matrix pipe busy half
+// of the time; on zeros, at the full clock, 490.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;
@@ -323,7 +326,8 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   if (h == 0) p.lse[(int64_t)w.head * p.n + mine] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// O and the log-sum-exps from the parts, four channels a lane.
+// O and the log-sum-exps from the parts, four channels a lane: bound by the parts' bytes (1031 rows, 8 heads of 64, five parts: 7 us; 2048 rows, 16
+// heads of 128, two: 10.6).
 template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
   const int quads = p.d / 4, row_quads = p.heads * quads;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -347,7 +351,10 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(At
 }
 
 // ---- backward: gradient of the queries -----------------------------------------------------------------------
-// As the forward pass; delta = dO . O of this work-group's rows is formed on the way and kept for the keys' gradient.
+// As the forward pass; delta = dO . O of this work-group's rows is formed on the way and kept for the keys' gradient, from O as it is stored: with O
+// in float dQ would be off by 2.4e-3 instead of 2.6e-3 (4096 keys), 2.3e-3 instead of 4.3e-3 (five), at twice the bytes kept of O.  A kernel of
+// its own, which forms scores and dP a second time: sums over work-groups would be atomics, in an order that changes.  Bound as the forward pass,
+// with fewer vector instructions (four to one): 754 to 818 us where that takes 608 to 654, 1.01 to 1.09 PFLOP/s.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;
@@ -497,10 +504,12 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
 }
 
 // ---- backward: gradients of the keys and values --------------------------------------------------------------
-// A work-group has 128 keys of one key head, 32 for each of four waves, and goes over the queries of the heads that share it, so that the sum
-// over them is taken in its accumulators.  bfloat16: eight waves, two for the same keys, which take the two halves of a tile of queries and add
+// A work-group has KW x 32 keys of one key head and goes over the queries of the heads that share it, so that the sum
+// over them is taken in its accumulators.  bfloat16: twice KW waves, two for the same keys, which take the two halves of a tile of queries and add
 // their sums up at the end; the keys' rows stay in LDS.  (Two waves a SIMD need 256 registers each, of which the sums take 128: with the
-// keys' rows in registers too there is one, and nothing runs while it waits.)  float: four waves, the keys' rows in registers.
+// keys' rows in registers too there is one, and nothing runs while it waits: 4 x 4096 rows, 32 heads of 128 on 8, both passes 2.82 ms, so 3.54.)
+// float: the keys' rows in registers.  Where there are few or short rows two waves' keys are a work-group (KW).  The same rows: 1117 to 1193 us,
+// 0.92 to 0.98 PFLOP/s, three vector instructions to a matrix one.
 template <typename T, int DB, int KW> struct DkvLayout {
   using Tile = Tile32<T, DB>;
   static constexpr int HALVES = sizeof(T) == 2 ? 2 : 1, NW = KW * HALVES, BM = 32 * KW, BQ = Tile::BN;
@@ -720,7 +729,8 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   store_row<T, DB>((T*)p.dv + (int64_t)mine * p.ldv + (int64_t)kv * p.d, dv, 1.f, p.d, h);
 }
 
-// One or two matrices [n, width] as sums of their parts [parts][matrices][n][width], four channels a lane.
+// One or two matrices [n, width] as sums of their parts [parts][matrices][n][width], four channels a lane: bound by the parts' bytes (dK and dV of
+// 6001 rows, 4 key heads of 80, three parts: 46 MB in 9 us).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_parts_kernel(const float* part, int parts, int64_t n, int width, T* first, int64_t ld_first, T* second, int64_t ld_second) {
   const int quads = width / 4;

@@ -76,6 +76,7 @@ template <typename T> __device__ __forceinline__ double grad_squares(const T* x,
   return sum[0] + sum[1];
 }
 
+// Bound by HBM: 1.3e9 bfloat16 gradients in 452 us, 5.8 TB/s.
 static __global__ __launch_bounds__(256) void grad_squares_kernel(GradList g, double* partial) {
   const int t = grad_tensor(g, blockIdx.x);
   const int64_t e0 = (int64_t)(blockIdx.x - g.first[t]) * kGradChunk;
@@ -114,7 +115,8 @@ template <typename T, typename TD> __device__ __forceinline__ void grad_scale(co
   for (int i = whole * 8 + threadIdx.x; i < count; i += 256) y[i] = from_f32<TD>(to_f32(x[i]) * by);
 }
 
-// The last work-groups' elements first: those the norm's pass has left in the memory-side cache.
+// The last work-groups' elements first: those the norm's pass has left in the memory-side cache.  1.3e9 bfloat16 gradients in place 972 us, 5.4 TB/s
+// read and written.
 static __global__ __launch_bounds__(256) void grad_scale_kernel(GradList g, const float* factor) {
   const uint32_t group = gridDim.x - 1 - blockIdx.x;
   const int t = grad_tensor(g, group);
@@ -147,7 +149,8 @@ struct GramList {
   float* parts;
 };
 
-// A tile of X^T X over kGramRows of the contracted index: 128 x 128, each of four waves 64 x 64.
+// A tile of X^T X over kGramRows of the contracted index: 128 x 128, each of four waves 64 x 64.  28 pairs of rank 256 (4096 to 14336 rows a side):
+// 54 us, 0.6 PFLOP/s of the three tiles in four that are formed; their bytes take 35, the products 20.
 template <typename T> __global__ __launch_bounds__(256, 1) void gram_kernel(GramList g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, 4>;
@@ -242,7 +245,7 @@ template <typename T> __global__ __launch_bounds__(256, 1) void gram_kernel(Gram
       for_regs([&](int r) { out[(64 * wi + 32 * i + 8 * (r >> 2) + 4 * h + (r & 3)) * kGramTile + 64 * wj + 32 * j + c] = acc[i][j][r]; });
 }
 
-// sum (L^T L) o (G^T G) of pair p (its sides 2 p and 2 p + 1), 16 rows of a tile a work-group; tiles off the diagonal count twice.
+// sum (L^T L) o (G^T G) of pair p (its sides 2 p and 2 p + 1), 16 rows of a tile a work-group; tiles off the diagonal count twice.  8 us for 28 pairs.
 struct GramSumList {
   GramList g;
   uint32_t first[kGradFactors];
