@@ -144,11 +144,19 @@ template <int BN> __device__ __forceinline__ void part_of(int& lo, int& hi, int 
 template <typename T, bool GRAD>
 __device__ __forceinline__ f32x16 shape_scores(const AttnParams& p, f32x16 s, float slope2, int at, int own, f32x16* slope_of_cap) {
   if (p.cap2 > 0.f) {
-    f32x16 x = s * here(p.inv_cap), inv;   // (in a vector register: sixteen copies of a scalar one are kept otherwise)
-    for_regs([&](int r) { inv[r] = __builtin_amdgcn_rcpf(1.f + fast_exp2(x[r] * (2.f * kLog2e))); });   // (1 - tanh x) / 2
-    if constexpr (sizeof(T) == 2) s = here(p.cap2) * (1.f - 2.f * inv);
-    else for_regs([&](int r) { s[r] = p.cap2 * tanhf(x[r]); });
-    if constexpr (GRAD) *slope_of_cap = 4.f * inv * (1.f - inv);
+    const float twice = here(p.inv_cap * (2.f * kLog2e));   // (in a vector register: sixteen copies of a scalar one are kept otherwise)
+    f32x16 inv;
+    if constexpr (GRAD || sizeof(T) == 2) for_regs([&](int r) { inv[r] = __builtin_amdgcn_rcpf(1.f + fast_exp2(s[r] * twice)); });   // (1 - tanh x) / 2
+    if constexpr (sizeof(T) == 2) {
+      const float cap2 = here(p.cap2), minus = here(-2.f * p.cap2);
+      for_regs([&](int r) { s[r] = __builtin_fmaf(inv[r], minus, cap2); });
+    } else {
+      for_regs([&](int r) { s[r] = p.cap2 * tanhf(s[r] * p.inv_cap); });
+    }
+    if constexpr (GRAD) {
+      const f32x16 four = 4.f * inv;
+      for_regs([&](int r) { (*slope_of_cap)[r] = __builtin_fmaf(-four[r], inv[r], four[r]); });
+    }
   } else {
     s *= here(p.c2);
   }

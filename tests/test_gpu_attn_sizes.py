@@ -81,3 +81,43 @@ def test_two_graphs_on_one_workspace(acc):
         for (_, out), first in zip(held, want):
             assert all(torch.equal(out[k], first[k]) for k in first)
         cases[0].run(acc)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_columns_between_the_heads_hold_anything(acc, dtype):
+    """Rows of q, k, v, O and dO whose gaps are not numbers: the same bits as from dense rows."""
+    import torch
+    c = Case(150, 2, 2, 40, dtype, cuts=[0, 90, 150], cap=12.0)
+    dense = c.run(acc)
+    t, lse = c.to_gpu(), torch.empty(2, 150, device="cuda")
+    wide = lambda: torch.full((150, 96), float("nan"), dtype=c.tdt, device="cuda")  # noqa: E731
+    q, k, v, do, o, dq, dk, dv = (wide() for _ in range(8))
+    for to, x in zip((q, k, v, do), (*c.split(t["qkv"]), t["dO"])):
+        to[:, :80] = x
+    desc = acc.make_attn_desc(150, 2, 2, 40, ldq=96, ldk=96, ldv=96, ldo=96, docs=2, cap=12.0, io_dtype=c.desc(acc).io_dtype, flags=acc.ACC_ATTN_CAUSAL)
+    ws = torch.empty(acc.acc_attn_workspace_bytes(desc, True), dtype=torch.uint8, device="cuda")
+    acc.acc_attn_fwd(desc, q, k, v, t["starts"], None, None, o, lse, ws)
+    acc.acc_attn_bwd(desc, q, k, v, t["starts"], None, None, o, lse, do, dq, dk, dv, ws)
+    assert torch.equal(o[:, :80], dense["o"]) and bool(torch.isnan(o[:, 80:]).all()) and torch.equal(lse, dense["lse"])
+    for got, want in zip((dq, dk, dv), c.split(dense["dqkv"])):
+        assert torch.equal(got[:, :80], want) and bool(torch.isnan(got[:, 80:]).all())
+
+
+def test_numbers_of_documents_that_do_not_ascend_stay_inside(acc):
+    """Every first row is brought into [0, n] before it is used: what lies around the tensors is neither read into results nor written."""
+    import torch
+    n = 200
+    c = Case(n, 2, 1, 64, cuts=[0, 60, n])
+    t = c.to_gpu()
+    guard = lambda rows, cols: torch.full((rows + 64, cols), 7.0, dtype=c.tdt, device="cuda")  # noqa: E731
+    for numbers in ([150, 20, 90], [-5, 1 << 40, 30], [0, -(1 << 50), 1 << 50], [200, 200, 0], [199, 0, 400]):
+        starts = torch.tensor(numbers, dtype=torch.int64, device="cuda")
+        o, back, lse = guard(n, 128), guard(n, 256), torch.full((2 * n + 64,), 7.0, device="cuda")
+        desc = c.desc(acc)
+        ws = torch.zeros(acc.acc_attn_workspace_bytes(desc, True), dtype=torch.uint8, device="cuda")
+        masks = starts, None, None
+        acc.acc_attn_fwd(desc, *c.split(t["qkv"]), *masks, o[32:-32], lse[32:-32], ws)
+        acc.acc_attn_bwd(desc, *c.split(t["qkv"]), *masks, o[32:-32], lse[32:-32], t["dO"], *c.split(back[32:-32]), ws)
+        torch.cuda.synchronize()
+        for x in (o, back, lse):
+            assert bool((x[:32] == 7.0).all()) and bool((x[-32:] == 7.0).all()), numbers

@@ -206,3 +206,37 @@ def test_a_decoder_step_of_all_of_them(ag, dtype):
     opt.zero_grad()
     again = loss_of()
     assert math.isfinite(float(again)) and float(again) != before
+
+
+def test_a_captured_step(ag):
+    """Table, attention and clipping in one graph, replayed on other inputs beside the program's own passes over the same weights."""
+    import torch
+    table = ag.Embedding(60, 4 * 32, device="cuda")
+    attend = ag.DocumentAttention(2, 1, cap=15.0, slopes=True, device="cuda")
+    ids, starts = torch.randint(0, 60, (130,), device="cuda"), torch.tensor([0, 50, 130], device="cuda")
+    g = torch.randn(130, 64, device="cuda").to(torch.bfloat16)
+
+    def step():
+        table.weight.grad = None
+        y = attend(table(ids), starts)
+        table.weight.grad, = torch.autograd.grad(y, table.weight, g)
+        norm = ag.clip_grad_norm_(table.parameters(), 0.25)
+        return y.detach(), table.weight.grad, norm
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        ids.copy_(torch.randint(-1, 60, (130,), device="cuda"))
+        starts.copy_(torch.tensor([k, 40 + 20 * k, 130 - k], device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
