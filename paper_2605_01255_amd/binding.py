@@ -6,9 +6,9 @@ built, importing this module raises.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libacc.so")
@@ -500,16 +500,26 @@ _GRAD_CODES = {torch.bfloat16: ACC_BF16, torch.float32: ACC_F32}
 
 def make_grad_list(tensors, outs=None):
     """The table of acc_grad_norm and acc_grad_scale: dense tensors and where they go when scaled (None: in place)."""
-    words = []   # of AccGradTensor: src, dst, count, both types (filled as one array: 0.8 us a tensor, 2 by fields)
-    for a, b in zip(tensors, tensors if outs is None else outs, strict=True):
-        count, code = a.numel(), _GRAD_CODES.get(a.dtype)
-        if not a.is_contiguous() or (b is not a and (not b.is_contiguous() or b.numel() != count)):
-            raise ValueError("gradients and their outputs must be contiguous and of one size")
-        out = code if b is a else _GRAD_CODES.get(b.dtype)
-        if code is None or out is None:
-            raise TypeError("gradients are bfloat16 or float32")
-        words += a.data_ptr(), b.data_ptr(), count, code | out << 32
-    return (AccGradTensor * len(tensors)).from_buffer(array.array("q", words)) if words else (AccGradTensor * 0)()
+    # Filled as one array of AccGradTensor's words (src, dst, count, both types), column by column: 0.7 us a tensor, 1.3 row by row.
+    tensors = list(tensors)
+    count, of = list(map(torch.Tensor.numel, tensors)), torch.Tensor.data_ptr
+    src = dst = list(map(of, tensors))
+    whole = all(map(torch.Tensor.is_contiguous, tensors))
+    try:
+        code = out = [_GRAD_CODES[t.dtype] for t in tensors]
+        if outs is not None:
+            outs = list(outs)
+            whole = whole and all(map(torch.Tensor.is_contiguous, outs)) and count == list(map(torch.Tensor.numel, outs))
+            dst, out = list(map(of, outs)), [_GRAD_CODES[t.dtype] for t in outs]
+    except KeyError:
+        raise TypeError("gradients are bfloat16 or float32") from None
+    if not whole:
+        raise ValueError("gradients and their outputs must be contiguous and of one size")
+    if not tensors:
+        return (AccGradTensor * 0)()
+    words = [0] * (4 * len(tensors))
+    words[0::4], words[1::4], words[2::4], words[3::4] = src, dst, count, [a | b << 32 for a, b in zip(code, out)]
+    return (AccGradTensor * len(tensors)).from_buffer_copy(struct.pack(f"{len(words)}q", *words))
 
 
 def make_factor_list(left, gr, flags=0):

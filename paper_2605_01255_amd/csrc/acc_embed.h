@@ -12,6 +12,7 @@
 namespace acc {
 
 constexpr int kBuckets = 256, kBucketBits = 8, kEmbedBlock = 32;
+constexpr int kWaveList = 256, kListAhead = 16;   // tokens of a wave's list; rows of numbers that it requests together
 constexpr int kEmbedCounters = 16384;   // of a bucket's counting sort: its words times the waves that count apart
 
 struct EmbedParams {
@@ -69,47 +70,59 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// One work-group of 1024 for each bucket: its tokens in p.order, its words' places in p.rows.  LDS: kEmbedCounters ints.  Each reads all numbers
-// twice, from L2: 16 us for 16384 tokens, 21 for 32768, of which counting, the list and the sort are waits one after another.
+// One work-group of 1024 for each bucket: its tokens in p.order, its words' places in p.rows.  LDS: p.bins * p.waves counters, then a list of
+// kWaveList tokens for each wave.  A wave goes over a sixteenth of the numbers and appends its tokens to its list, so the lists one after another
+// are in the tokens' order; where one is too short (a word that most tokens have, very many tokens) the work-group goes over the numbers again,
+// all waves together, and lists its tokens in memory.  12 us for 16384 and 32768 tokens, waits one after another; with a second
+// pass for all of them 16 and 21.
 static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p) {
   extern __shared__ int counter[];
-  __shared__ int sums[2][16], scan[16];
+  __shared__ int sums[2][16], listed[16], scan[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bucket = blockIdx.x;
-  const int n = (int)p.n;
+  const int n = (int)p.n, counters = p.bins * p.waves;
+  int2* lists = (int2*)(counter + (counters + 1) / 2 * 2);
+  for (int i = tid; i < counters; i += 1024) counter[i] = 0;
   // tokens of the buckets before this one, and of this one
   int before = 0, own = 0;
-#pragma unroll 8
-  for (int i = tid; i < n; i += 1024) {
-    const int64_t id = p.ids[i];
-    const bool word = (uint64_t)id < (uint64_t)p.v;
-    const int b = (int)(id & (kBuckets - 1));
-    before += word && b < bucket;
-    own += word && b == bucket;
+  {
+    const int run = (n + 16 * 64 - 1) / (16 * 64) * 64, end = n - wave * run < run ? n : (wave + 1) * run;
+    for (int i0 = wave * run; i0 < end; i0 += 64 * kListAhead) {
+      int64_t id[kListAhead];
+#pragma unroll
+      for (int k = 0; k < kListAhead; ++k) id[k] = i0 + k * 64 + lane < end ? p.ids[i0 + k * 64 + lane] : -1;
+#pragma unroll
+      for (int k = 0; k < kListAhead; ++k) {
+        const bool word = (uint64_t)id[k] < (uint64_t)p.v;
+        const int b = (int)(id[k] & (kBuckets - 1));
+        before += word && b < bucket;
+        const uint64_t mine = __ballot(word && b == bucket);
+        const int at = own + lanes_below(mine);
+        if (word && b == bucket && at < kWaveList) lists[wave * kWaveList + at] = make_int2(i0 + k * 64 + lane, (int)(id[k] >> kBucketBits));
+        own += __popcll(mine);
+      }
+    }
   }
 #pragma unroll
-  for (int s = 32; s; s >>= 1) {
-    before += __shfl_xor(before, s);
-    own += __shfl_xor(own, s);
-  }
+  for (int s = 32; s; s >>= 1) before += __shfl_xor(before, s);
   if (lane == 0) {
     sums[0][wave] = before;
-    sums[1][wave] = own;
+    listed[wave] = own;
   }
-  const int counters = p.bins * p.waves;
-  for (int i = tid; i < counters; i += 1024) counter[i] = 0;
   __syncthreads();
+  bool again = false;
   before = own = 0;
   for (int w = 0; w < 16; ++w) {
     before += sums[0][w];
-    own += sums[1][w];
+    own += listed[w];
+    again |= listed[w] > kWaveList;
   }
   if (bucket == kBuckets - 1 && tid == 0) *p.total = before + own;
-  __syncthreads();
 
   // this bucket's tokens in their order, four neighbours a lane
-  int at = before;
   int2* list = p.list;
-  if (own) {
+  if (again) {
+    __syncthreads();
+    int at = before;
     int64_t ahead[4];
     auto request = [&](int i) {
 #pragma unroll
@@ -122,7 +135,7 @@ static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p)
       uint32_t mine = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) id[e] = ahead[e];
-      if (n - i > 4096) request(i + 4096);
+      request(i + 4096);   // (behind the last number: none)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if ((uint64_t)id[e] < (uint64_t)p.v && (int)(id[e] & (kBuckets - 1)) == bucket) mine |= 1u << e;
@@ -147,14 +160,23 @@ static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p)
       for (int e = 0; e < 4; ++e)
         if (mine >> e & 1) list[to++] = make_int2(i + e, (int)(id[e] >> kBucketBits));
     }
+    __syncthreads();
   }
-  __syncthreads();
   // Counting sort: wave w has a run of the list, counter[word][w] its tokens of a word, then their first place.
-  const int run = (own + p.waves * 64 - 1) / (p.waves * 64) * 64;
-  const int from = before + (wave * run < own ? wave * run : own), until = before + ((wave + 1) * run < own ? (wave + 1) * run : own);
   const bool sorts = wave < p.waves;
-  if (sorts)
-    for (int k = from + lane; k < until; k += 64) atomicAdd(&counter[list[k].y * p.waves + wave], 1);
+  auto pieces = [&](auto&& f) {   // f(tokens and words, their number) for the pieces of this wave's run
+    if (!sorts) return;
+    if (again) {
+      const int run = (own + p.waves * 64 - 1) / (p.waves * 64) * 64;
+      const int from = wave * run < own ? wave * run : own, until = (wave + 1) * run < own ? (wave + 1) * run : own;
+      f(list + before + from, until - from);
+    } else {
+      for (int w = wave * (16 / p.waves); w < (wave + 1) * (16 / p.waves); ++w) f(lists + w * kWaveList, listed[w]);
+    }
+  };
+  pieces([&](const int2* x, int count) {
+    for (int k = lane; k < count; k += 64) atomicAdd(&counter[x[k].y * p.waves + wave], 1);
+  });
   __syncthreads();
   // exclusive sums over the counters, a run of them for each lane
   const int each = (counters + 1023) / 1024, c0 = tid * each < counters ? tid * each : counters, c1 = c0 + each < counters ? c0 + each : counters;
@@ -181,21 +203,22 @@ static __global__ __launch_bounds__(1024) void embed_group_kernel(EmbedParams p)
     p.rows[bucket * p.bins + b] = make_int2(start, end - start);
   }
   __syncthreads();
-  if (!sorts) return;
-  for (int k = from; k < until; k += 64) {
-    const bool there = k + lane < until;
-    const int2 x = there ? list[k + lane] : make_int2(0, 0);
-    uint64_t same = __ballot(there);   // lanes with this lane's word
-    for (int bit = 1; bit < p.bins; bit <<= 1) {
-      const uint64_t m = __ballot((x.y & bit) != 0);
-      same &= x.y & bit ? m : ~m;
+  pieces([&](const int2* from, int count) {
+    for (int k = 0; k < count; k += 64) {
+      const bool there = k + lane < count;
+      const int2 x = there ? from[k + lane] : make_int2(0, 0);
+      uint64_t same = __ballot(there);   // lanes with this lane's word
+      for (int bit = 1; bit < p.bins; bit <<= 1) {
+        const uint64_t m = __ballot((x.y & bit) != 0);
+        same &= x.y & bit ? m : ~m;
+      }
+      const int rank = lanes_below(same), first = there ? __ffsll((unsigned long long)same) - 1 : lane;
+      int to = 0;
+      if (there && first == lane) to = atomicAdd(&counter[x.y * p.waves + wave], __popcll(same));
+      to = __shfl(to, first);
+      if (there) p.order[to + rank] = x.x;
     }
-    const int rank = lanes_below(same), first = there ? __ffsll((unsigned long long)same) - 1 : lane;
-    int to = 0;
-    if (there && first == lane) to = atomicAdd(&counter[x.y * p.waves + wave], __popcll(same));
-    to = __shfl(to, first);
-    if (there) p.order[to + rank] = x.x;
-  }
+  });
 }
 
 template <int E> __device__ __forceinline__ void embed_store(float* to, const float* x, float by, bool add) {

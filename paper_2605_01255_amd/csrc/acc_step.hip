@@ -232,7 +232,7 @@ int acc_embed_bwd(const acc_embed_desc* desc, const int64_t* ids, const void* dY
   p.list = (int2*)(ws + plan.list);
   p.total = (int*)(ws + plan.total);
   p.parts = (float*)(ws + plan.parts);
-  L.launch_lds(embed_group_kernel, dim3(kBuckets), dim3(1024), (size_t)p.bins * p.waves * 4, p);
+  L.launch_lds(embed_group_kernel, dim3(kBuckets), dim3(1024), (size_t)round_up(p.bins * p.waves * 4, 8) + 16 * kWaveList * 8, p);
   const dim3 sums((unsigned)(p.grad_groups + plan.zero_groups)), parts((unsigned)plan.part_groups);
   auto typed = [&](auto value, auto grad) {
     using T = decltype(value);

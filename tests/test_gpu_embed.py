@@ -120,6 +120,16 @@ def test_tables_so_large_that_fewer_waves_sort(acc, v):
     Case(acc, ids, 8, v, "bf16", "bf16").check()
 
 
+@pytest.mark.parametrize("v", [50, 1000, 1 << 21])
+@pytest.mark.parametrize("what", ["one word", "as in text", "a run of one among others", "exactly full lists"])
+def test_words_so_frequent_that_they_are_listed_in_memory(acc, what, v):
+    """Sixteenths of the numbers with more than 256 tokens of one bucket, and with 256."""
+    other = _words(9000, v, seed=3)
+    ids = {"one word": [v - 1] * 9000, "as in text": _words(30001, v), "a run of one among others": other[:4000] + [7] * 5000 + other[4000:],
+           "exactly full lists": ([7] * 256 + [-1] * 256) * 16}[what]
+    Case(acc, ids, 8, v, "bf16", "f32").check()
+
+
 def test_what_is_not_finite_stays_in_its_word(acc):
     import torch
     ids = _words(400, 30)
