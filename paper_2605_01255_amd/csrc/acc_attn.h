@@ -127,6 +127,11 @@ __device__ __forceinline__ int queries_lo(const AttnParams& p, const AttnRows& w
 __device__ __forceinline__ int queries_hi(const AttnParams& p, const AttnRows& w, int j) {
   return p.window && p.window < w.end - j ? j + p.window : w.end;
 }
+// Whether row i as a query sees the key i alone.  Its dS, P (dP - delta) with P = 1, is a difference of two sums that are equal but for their
+// roundings, and is taken as the zero that it is.  (Tiles that hold such a row are never seen whole.)
+__device__ __forceinline__ bool alone(const AttnParams& p, const AttnRows& w, int i) {
+  return p.window == 1 || (i == w.begin && (p.causal ? w.prefix_end <= w.begin + 1 : w.end - w.begin == 1));
+}
 
 __device__ __forceinline__ void store_quad(float* to, f32x4 x) { *(f32x4*)to = x; }
 __device__ __forceinline__ void store_quad(bf16* to, f32x4 x) { *(bf16x4*)to = __builtin_convertvector(x, bf16x4); }
@@ -405,7 +410,7 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
   int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
   part_of<BN>(k_lo, k_hi, part, p.parts);
-  const int lo = keys_lo(p, w, mine), span = keys_hi(p, w, mine) - lo;
+  const int lo = keys_lo(p, w, mine), span = alone(p, w, mine) ? 0 : keys_hi(p, w, mine) - lo;   // of dS
   const int full_lo = keys_lo(p, w, w1), full_hi = keys_hi(p, w, w0);
   const int any_lo = keys_lo(p, w, w0), any_hi = keys_hi(p, w, w1);
   const bool shaped = p.cap2 > 0.f || p.slopes;
@@ -549,7 +554,7 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
   const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
   const int q_lo = queries_lo(p, w, w.first), q_hi = w.dead ? q_lo : queries_hi(p, w, last);
-  const int lo = queries_lo(p, w, mine), span = queries_hi(p, w, mine) - lo;
+  const int lo = queries_lo(p, w, mine), span = queries_hi(p, w, mine) - lo, skip = alone(p, w, mine);   // (the first of them has no dS)
   const int full_lo = queries_lo(p, w, w1), full_hi = queries_hi(p, w, w0);
   const int any_lo = queries_lo(p, w, w0), any_hi = queries_hi(p, w, w1);
   const bool shaped = p.cap2 > 0.f || p.slopes;
@@ -697,8 +702,8 @@ __global__ __launch_bounds__((DkvLayout<T, DB, KW>::NW * 64), (DkvLayout<T, DB, 
               spread<step, steps>([&](int r) { dp[r] = here(s[r] * (dp[r] - delta[r >> 2][r & 3])); });
               if constexpr (step == steps - 1) {
                 if (masked) {   // (a probability of zero does not make what is not finite zero)
-                  const int base = q0 + 32 * b + 4 * h - lo;
-                  for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)span) dp[r] = 0.f; });
+                  const int base = q0 + 32 * b + 4 * h - lo - skip;
+                  for_regs([&](int r) { if ((uint32_t)(base + 8 * (r >> 2) + (r & 3)) >= (uint32_t)(span - skip)) dp[r] = 0.f; });
                 }
                 sf[0] = here(step_operand<T>(dp, 0));
                 sf[1] = here(step_operand<T>(dp, 1));

@@ -121,3 +121,26 @@ def test_numbers_of_documents_that_do_not_ascend_stay_inside(acc):
         torch.cuda.synchronize()
         for x in (o, back, lse):
             assert bool((x[:32] == 7.0).all()) and bool((x[-32:] == 7.0).all()), numbers
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(n=1), dict(n=300, window=1), dict(n=65, seq=1, causal=False), dict(n=140, seq=1, prefix=[1] * 140),
+                                dict(n=130, window=1, cuts=[0, 1, 34, 130]), dict(n=40, cuts=list(range(41)), cap=5.0)], ids=str)
+def test_rows_that_see_one_key_have_no_gradient_of_their_scores(acc, kw, dtype):
+    """Zeros, and not what is left of a difference of two sums."""
+    c = Case(heads=4, kv=2, d=72, dtype=dtype, **kw)
+    out = c.run(acc)
+    c.check(out)
+    dq, dk, _ = c.split(out["dqkv"])
+    assert not dq.any() and not dk.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(n=200), dict(n=200, window=2), dict(n=200, prefix=[1]), dict(n=200, cuts=[0, 1, 90, 91, 200])], ids=str)
+def test_the_first_row_sees_one_key(acc, kw, dtype):
+    c = Case(heads=2, kv=1, d=64, dtype=dtype, **kw)
+    out = c.run(acc)
+    c.check(out)
+    first = [a for a, b in c.documents()]
+    dq = c.split(out["dqkv"])[0]
+    assert not dq[first].any() and bool(dq[first[-1] + 1].any())
