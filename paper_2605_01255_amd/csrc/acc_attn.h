@@ -175,6 +175,7 @@ __device__ __forceinline__ f32x16 shape_scores(const AttnParams& p, f32x16 s, fl
 // How far a score may lie above a row's running maximum, in units of log 2, before the maximum is raised: probabilities reach 2^8 then, which
 // costs float nothing, and a wave seldom rescales its sums (training step's forward 608 us, with 0 here 669).
 constexpr float kSlack = 8.f;
+constexpr int kFewKeys = 64;
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.  Tiles of 64 keys (float 32), two in LDS,
@@ -365,7 +366,9 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(At
 
 // ---- backward: gradient of the queries -----------------------------------------------------------------------
 // As the forward pass; delta = dO . O of this work-group's rows is formed on the way and kept for the keys' gradient, from O as it is stored: with O
-// in float dQ would be off by 2.4e-3 instead of 2.6e-3 (4096 keys), 2.3e-3 instead of 4.3e-3 (five), at twice the bytes kept of O.  A kernel of
+// in float dQ would be off by 2.4e-3 instead of 2.6e-3 (4096 keys), at twice the bytes kept of O.  The fewer keys a row has the more dP and delta
+// cancel (five keys: 2.3e-3 would become 4.3e-3, two 6e-3), so where no row of the work-group has more than kFewKeys delta is the sum of P dP,
+// which it is by definition, in a pass of its own over the one tile or, with a window, the few that there are.  A kernel of
 // its own, which forms scores and dP a second time: sums over work-groups would be atomics, in an order that changes.  Bound as the forward pass,
 // with fewer vector instructions (four to one): 754 to 818 us where that takes 608 to 654, 1.01 to 1.09 PFLOP/s.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
@@ -400,17 +403,12 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const int64_t row = (int64_t)w.head * p.n + mine;
   const float lse = w.dead ? -INFINITY : p.lse[row];
   const float minus = lse == -INFINITY ? -INFINITY : lse * -kLog2e;   // a row without keys has no probabilities
-  if (there && h == 0) {
-    p.delta[row] = delta;
-    p.minus[row] = minus;
-  }
 
   const T* kbase = (const T*)p.k + (int64_t)kv * p.d;
   const T* vbase = (const T*)p.v + (int64_t)kv * p.d;
   const int last = w.first + BM < w.end ? w.first + BM - 1 : w.end - 1;
   int k_lo = keys_lo(p, w, w.first), k_hi = w.dead ? k_lo : keys_hi(p, w, last);
-  part_of<BN>(k_lo, k_hi, part, p.parts);
-  const int lo = keys_lo(p, w, mine), span = alone(p, w, mine) ? 0 : keys_hi(p, w, mine) - lo;   // of dS
+  const int lo = keys_lo(p, w, mine), seen = keys_hi(p, w, mine) - lo, span = alone(p, w, mine) ? 0 : seen;   // span: of dS
   const int full_lo = keys_lo(p, w, w1), full_hi = keys_hi(p, w, w0);
   const int any_lo = keys_lo(p, w, w0), any_hi = keys_hi(p, w, w1);
   const bool shaped = p.cap2 > 0.f || p.slopes;
@@ -420,6 +418,41 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   using KVLoader = Tile32Loader<T, DB, NW>;
   const KVLoader kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
+  if constexpr (sizeof(T) == 2) {
+    const int most = p.window && p.window < k_hi - k_lo ? p.window : k_hi - k_lo;   // keys of a row
+    if (most <= kFewKeys) {
+      delta = 0.f;
+      for (int k0 = k_lo; k0 < k_hi; k0 += BN) {
+        __syncthreads();
+        kload.issue(kbase, k0, k_hi - k0, p.ldk, p.d, lds, wave);
+        vload.issue(vbase, k0, k_hi - k0, p.ldv, p.d, lds + Tile::BYTES, wave);
+        wait_vmcnt0();
+        __syncthreads();
+        static_for<0, KB>([&](auto block) {
+          constexpr int b = block.value;
+          f32x16 s{}, dp{};
+#pragma unroll
+          for (int i = 0; i < Tile::STEPS; ++i) {
+            mma(s, at.row(smem + Tile::block(b), i), qf[i]);
+            mma(dp, at.row(smem + Tile::BYTES + Tile::block(b), i), df[i]);
+          }
+          if (shaped) s = shape_scores<T, false>(p, s, slope2, k0 + 32 * b + 4 * h, mine, nullptr);
+          const int base = k0 + 32 * b + 4 * h - lo;
+          for_regs([&](int r) {
+            const float of = fast_exp2(__builtin_fmaf(s[r], c2, minus)) * dp[r];
+            delta += (uint32_t)(base + 8 * (r >> 2) + (r & 3)) < (uint32_t)seen ? of : 0.f;
+          });
+        });
+      }
+      delta = half_sum(delta);
+      __syncthreads();
+    }
+  }
+  if (there && h == 0) {
+    p.delta[row] = delta;
+    p.minus[row] = minus;
+  }
+  part_of<BN>(k_lo, k_hi, part, p.parts);
   f32x16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{};

@@ -5,7 +5,7 @@ The bounds count roundings (half a step: 2^-8 of the value in bfloat16, 2^-24 in
                and reciprocal to one step each, weighted by at most 1 / 2 and 2), the bias' product and difference
   P            twice the largest error of a row's scores (its own and the log-sum-exp's), the sum over the keys, the exponential
   O            P rounded as an operand (bfloat16), the result rounded: |O| + sum P |V|; the sum in float
-  delta        dO . O with O as rounded: sum |dO| |error of O|
+  delta        dO . O with O as rounded: sum |dO| |error of O|; where no row sees more than 64 keys (bfloat16) sum P dP: P's and dP's errors
   dS           P (dP - delta): P's error, dP's sum over d, delta's error; rounded as an operand (bfloat16)
   dQ, dK, dV   the operands' errors through the product, its sum in float, the result rounded
 """
@@ -93,6 +93,9 @@ class Case:
         dp_err = (d + 4) * u * do.abs() @ v.abs().transpose(1, 2)
         delta = (do * o).sum(2, keepdim=True)
         delta_err = (do.abs() * o_err).sum(2, keepdim=True) + (d + 4) * u * (do * o).abs().sum(2, keepdim=True)
+        longest = max([b - a for a, b in self.documents()], default=0)
+        if self.dtype == "bf16" and min(longest, self.window or longest) <= 64:   # from P and dP, and not from O as rounded
+            delta_err = (p * dp.abs() * (p_rel + 4 * u) + p * dp_err).sum(2, keepdim=True) + sums * (p * dp.abs()).sum(2, keepdim=True)
         ds = p * (dp - delta) * slope
         slope_err = 2.0 ** -20 if self.cap else 0.0
         ds_err = ds.abs() * (p_rel + operand + 8 * u) + p * slope * (dp_err + delta_err) + p * (dp - delta).abs() * slope_err

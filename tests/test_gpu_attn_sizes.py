@@ -144,3 +144,11 @@ def test_the_first_row_sees_one_key(acc, kw, dtype):
     first = [a for a, b in c.documents()]
     dq = c.split(out["dqkv"])[0]
     assert not dq[first].any() and bool(dq[first[-1] + 1].any())
+
+
+@pytest.mark.parametrize("kw", [dict(n=300, seq=2), dict(n=300, seq=3, causal=False), dict(n=256, cuts=sorted({0, 256, *range(0, 256, 5)}), cap=9.0),
+                                dict(n=900, window=2), dict(n=900, window=64, bias=True), dict(n=64), dict(n=512, seq=64, causal=False)], ids=str)
+def test_rows_of_few_keys_have_delta_from_their_probabilities(acc, kw):
+    """Scores of size four, so that dP and delta nearly cancel; bounds without the rounding of O."""
+    c = Case(heads=4, kv=2, d=64, size=2.0, **kw)
+    c.check(c.run(acc))
