@@ -180,7 +180,7 @@ constexpr int kFewKeys = 64;
 // ---- forward -------------------------------------------------------------------------------------------------
 // A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.  Tiles of 64 keys (float 32), two in LDS,
 // leave room for two work-groups on a compute unit.  Bound by power and by the vector instructions beside the matrix ones (six to one, of them
-// one exponential and one maximum a score): 4 x 4096 rows, 32 heads of 128 on 8, 608 to 654 us, 0.84 to 0.90 PFLOP/s, the matrix pipe busy half
+// one exponential and one maximum a score): 4 x 4096 rows, 32 heads of 128 on 8, 597 to 654 us, 0.84 to 0.92 PFLOP/s, the matrix pipe busy half
 // of the time; on zeros, at the full clock, 490.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -370,7 +370,7 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(At
 // cancel (five keys: 2.3e-3 would become 4.3e-3, two 6e-3), so where no row of the work-group has more than kFewKeys delta is the sum of P dP,
 // which it is by definition, in a pass of its own over the one tile or, with a window, the few that there are.  A kernel of
 // its own, which forms scores and dP a second time: sums over work-groups would be atomics, in an order that changes.  Bound as the forward pass,
-// with fewer vector instructions (four to one): 754 to 818 us where that takes 608 to 654, 1.01 to 1.09 PFLOP/s.
+// with fewer vector instructions (four to one): 748 to 818 us where that takes 597 to 654, 1.01 to 1.10 PFLOP/s.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;
@@ -554,8 +554,8 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
 // over them is taken in its accumulators.  bfloat16: twice KW waves, two for the same keys, which take the two halves of a tile of queries and add
 // their sums up at the end; the keys' rows stay in LDS.  (Two waves a SIMD need 256 registers each, of which the sums take 128: with the
 // keys' rows in registers too there is one, and nothing runs while it waits: 4 x 4096 rows, 32 heads of 128 on 8, both passes 2.82 ms, so 3.54.)
-// float: the keys' rows in registers.  Where there are few or short rows two waves' keys are a work-group (KW).  The same rows: 1117 to 1193 us,
-// 0.92 to 0.98 PFLOP/s, three vector instructions to a matrix one.
+// float: the keys' rows in registers.  Where there are few or short rows two waves' keys are a work-group (KW).  The same rows: 1098 to 1193 us,
+// 0.92 to 1.00 PFLOP/s, three vector instructions to a matrix one.
 template <typename T, int DB, int KW> struct DkvLayout {
   using Tile = Tile32<T, DB>;
   static constexpr int HALVES = sizeof(T) == 2 ? 2 : 1, NW = KW * HALVES, BM = 32 * KW, BQ = Tile::BN;
