@@ -72,7 +72,7 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   const int64_t seen = d->window && d->window < length ? d->window : length;
   // Work-groups of 64 rows, not of 128, which share a tile's transfers among more waves:
   //   float, whose products take sixteen times as long as their rows' transfers;
-  //   documents of up to 64 rows (8192 rows in 200 of them, 16 heads of 64 channels: forward and dQ 25 + 30 us, of 128 rows 30 + 50);
+  //   documents of up to 64 rows (8192 rows in 200 of them, 16 heads of 64 channels: forward and dQ 25 + 30 us, of 128 rows 30 + 50, both without delta's own pass);
   //   fewer than 128 of them with 128 rows (1024 rows, 8 heads of 128: 17 + 19 us and 7 to join parts, of 128 rows 16 + 21 and 11; 4096 rows, 32
   //   heads: 241 + 280 us, of 128 rows 170 + 206);
   //   for the keys' gradients heads of up to 64 channels, two work-groups of which fit a compute unit, so that one multiplies while the other
