@@ -382,7 +382,7 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
  *   lse [heads, n]     float, which the backward call reads.
  * What is not finite in a document's rows reaches its own rows only.  bfloat16: products of bfloat16 operands accumulated in float, softmax in
  * float; P and dS are rounded to bfloat16 as operands of the products behind them, O, dQ, dK and dV once; delta is taken from O as it was
- * rounded (where rows have at most 64 keys: as sum P dP), and the cap's tanh is exact to 2^-21.  float: float throughout.  The sums are taken in a fixed order.
+ * rounded (of a row with at most 64 keys: as sum P dP), and the cap's tanh is exact to 2^-21.  float: float throughout.  The sums are taken in a fixed order.
  * Outputs may not overlap inputs.  Of 2^30 rows and more, counted over all heads and each document in whole tiles of 128 (or 64), calls are
  * ACC_ERR_SHAPE: a launch has fewer than 2^32 threads. */
 #define ACC_ATTN_CAUSAL 1u

@@ -367,9 +367,10 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(At
 // ---- backward: gradient of the queries -----------------------------------------------------------------------
 // As the forward pass; delta = dO . O of this work-group's rows is formed on the way and kept for the keys' gradient, from O as it is stored: with O
 // in float dQ would be off by 2.4e-3 instead of 2.6e-3 (4096 keys), at twice the bytes kept of O.  The fewer keys a row has the more dP and delta
-// cancel (five keys: 2.3e-3 would become 4.3e-3, two 6e-3), so where no row of the work-group has more than kFewKeys delta is the sum of P dP,
-// which it is by definition, in a pass of its own over the one tile or, with a window, the few that there are (8192 rows in 200 documents, 16
-// heads of 64: 37 us for 31; for longer rows it would be two of three products again).  A kernel of
+// cancel (five keys: 2.3e-3 would become 4.3e-3, two 6e-3), so of a row with at most kFewKeys keys, the first ones of a long document too, delta is
+// the sum of P dP, which it is by definition, in a pass of its own over the one tile or, with a window, the few that there are (8192 rows in 200
+// documents, 16 heads of 64: 37 us for 31; in 60, 32 heads of 128: 117 for 112; long documents: within 1 %.  For longer rows it would be two of three
+// products again).  A kernel of
 // its own, which forms scores and dP a second time: sums over work-groups would be atomics, in an order that changes.  Bound as the forward pass,
 // with fewer vector instructions (four to one): 748 to 818 us where that takes 597 to 654, 1.01 to 1.10 PFLOP/s.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
@@ -420,15 +421,18 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
   const KVLoader kload(lane, wave, p.ldk, p.d), vload(lane, wave, p.ldv, p.d);
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   if constexpr (sizeof(T) == 2) {
-    const int most = p.window && p.window < k_hi - k_lo ? p.window : k_hi - k_lo;   // keys of a row
-    if (most <= kFewKeys) {
-      delta = 0.f;
-      for (int k0 = k_lo; k0 < k_hi; k0 += BN) {
+    // Rows of few keys are all of them (a window as short, a whole document) or the first ones of a document; their keys end at few_hi.
+    auto few = [&](int i) { return keys_hi(p, w, i) - keys_lo(p, w, i) <= kFewKeys; };
+    const int few_hi = (p.window && p.window <= kFewKeys) || k_hi - w.begin <= kFewKeys ? k_hi : w.begin + kFewKeys;
+    if (!w.dead && few(w.first)) {
+      float sum = 0.f;
+      for (int k0 = k_lo; k0 < few_hi; k0 += BN) {
         __syncthreads();
-        kload.issue(kbase, k0, k_hi - k0, p.ldk, p.d, lds, wave);
-        vload.issue(vbase, k0, k_hi - k0, p.ldv, p.d, lds + Tile::BYTES, wave);
+        kload.issue(kbase, k0, few_hi - k0, p.ldk, p.d, lds, wave);
+        vload.issue(vbase, k0, few_hi - k0, p.ldv, p.d, lds + Tile::BYTES, wave);
         wait_vmcnt0();
         __syncthreads();
+        if (w0 >= w.end || !few(w0)) continue;
         static_for<0, KB>([&](auto block) {
           constexpr int b = block.value;
           f32x16 s{}, dp{};
@@ -441,11 +445,12 @@ template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, size
           const int base = k0 + 32 * b + 4 * h - lo;
           for_regs([&](int r) {
             const float of = fast_exp2(__builtin_fmaf(s[r], c2, minus)) * dp[r];
-            delta += (uint32_t)(base + 8 * (r >> 2) + (r & 3)) < (uint32_t)seen ? of : 0.f;
+            sum += (uint32_t)(base + 8 * (r >> 2) + (r & 3)) < (uint32_t)seen ? of : 0.f;
           });
         });
       }
-      delta = half_sum(delta);
+      sum = half_sum(sum);
+      if (seen <= kFewKeys) delta = sum;
       __syncthreads();
     }
   }
