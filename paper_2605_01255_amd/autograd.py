@@ -418,7 +418,8 @@ class DocumentAttention(torch.nn.Module):
     beginning at the rows `starts` holds (int64, the last number is where the last one ends; rows outside give zeros).  A row sees its
     document's rows up to itself (`causal`), at most `window` of them (0: no limit), and always the document's first `prefix` ones
     (int64, one number per document).  Scores, times `scale` (None: 1 / sqrt(d)), are capped by cap tanh(score / cap) (0: not), and with
-    `slopes` (float32, one per head; True: 2^(-8 h / heads) for h = 1 .. heads) fall by slope times the distance."""
+    `slopes` (float32, one per head, which a cast of the module leaves float32; True: 2^(-8 h / heads) for h = 1 .. heads) fall by slope
+    times the distance."""
 
     def __init__(self, heads: int, kv_heads: Optional[int] = None, causal: bool = True, window: int = 0, cap: float = 0.0, scale: Optional[float] = None,
                  slopes=None, device=None):
@@ -435,10 +436,17 @@ class DocumentAttention(torch.nn.Module):
             slopes = 2.0 ** (-8.0 * torch.arange(1, heads + 1, dtype=torch.float32) / heads)
         self.register_buffer("slopes", None if slopes is None or slopes is False else torch.as_tensor(slopes, dtype=torch.float32).to(device))
 
+    def _apply(self, fn, recurse=True):
+        slopes = self.slopes
+        super()._apply(fn, recurse)
+        if slopes is not None and self.slopes.dtype != torch.float32:   # a cast of the module moves them, and leaves their values
+            self.slopes = slopes.to(self.slopes.device)
+        return self
+
     def forward(self, x, starts=None, prefix=None):
         if prefix is not None and (not self.causal or self.window):
             raise ValueError("a prefix needs causal attention without a window")
-        slopes = None if self.slopes is None else self.slopes.float()   # (a module cast to bfloat16 has cast them too)
+        slopes = None if self.slopes is None else self.slopes.float()
         return DocumentAttentionFunction.apply(x, starts, prefix, slopes, self.heads, self.kv_heads, self.causal, self.window, self.cap,
                                                self.scale or 0.0)
 
