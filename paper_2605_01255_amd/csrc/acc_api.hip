@@ -638,7 +638,7 @@ void gram_matrix(const RsvdPlan& pl, char* ws, int64_t m, int64_t k, const float
 
 // Image of the triangular factor of G [w, w] (row stride ldg), w <= 256.
 void chol_factor(const float* G, int64_t ldg, int64_t w, float* image, const float* scale_ref, float rel_tol, Launcher& L) {
-  auto go = [&](auto kernel, int KB) {  // a kernel's LDS limit is raised once, to what its first launch asks for: always the most
+  auto go = [&](auto kernel, int KB) {  // (the most LDS whatever w is, so that a kernel's limit is raised once)
     L.launch_lds(kernel, dim3(1), dim3((unsigned)chol_threads(KB)), (size_t)chol_lds_bytes(16 * KB), G, image, (int)w, ldg, scale_ref, rel_tol);
   };
   if (w <= 128) go(chol_factor_kernel<8>, 8);

@@ -73,6 +73,7 @@ inline int check_device() {
 }
 
 inline RaisedLimits g_raised;
+inline std::mutex g_raising;
 
 // Enqueues kernels on one stream and remembers the first launch error.
 struct Launcher {
@@ -90,10 +91,13 @@ struct Launcher {
       int dev = 0;
       err = hipGetDevice(&dev);
       if (err != hipSuccess) return;
-      if (!g_raised.has((const void*)kernel, dev)) {
-        err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
-        if (err != hipSuccess) return;
-        g_raised.add((const void*)kernel, dev);
+      if (!g_raised.has((const void*)kernel, dev, (uint32_t)lds_bytes)) {
+        std::lock_guard<std::mutex> lock(g_raising);   // (another thread's smaller limit must not replace a larger one)
+        if (!g_raised.has((const void*)kernel, dev, (uint32_t)lds_bytes)) {
+          err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
+          if (err != hipSuccess) return;
+          g_raised.add((const void*)kernel, dev, (uint32_t)lds_bytes);
+        }
       }
     }
     std::tuple<KArgs...> vals{args...};
