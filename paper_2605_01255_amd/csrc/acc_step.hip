@@ -47,9 +47,7 @@ int plan_embed(const acc_embed_desc* d, EmbedPlan* plan) {
   p.waves = waves;
   plan->zero_groups = p.add ? 0 : ceil_div((int64_t)kBuckets * p.bins, 32);
   plan->part_groups = plan->blocks * ceil_div(d->d, 256);
-  if (ceil_div(d->n, plan->per) >= 1 << 24 || plan->blocks * plan->slices >= 1 << 30 || p.grad_groups + plan->zero_groups >= 1 << 24 ||
-      plan->part_groups >= 1 << 24)
-    return ACC_ERR_SHAPE;
+  if (ceil_div(d->n, plan->per) >= 1 << 24 || plan->blocks * plan->slices >= 1 << 30 || p.grad_groups + plan->zero_groups >= 1 << 24) return ACC_ERR_SHAPE;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t from = at;
@@ -233,12 +231,14 @@ int acc_embed_bwd(const acc_embed_desc* desc, const int64_t* ids, const void* dY
   p.total = (int*)(ws + plan.total);
   p.parts = (float*)(ws + plan.parts);
   L.launch_lds(embed_group_kernel, dim3(kBuckets), dim3(1024), (size_t)round_up(p.bins * p.waves * 4, 8) + 16 * kWaveList * 8, p);
-  const dim3 sums((unsigned)(p.grad_groups + plan.zero_groups)), parts((unsigned)plan.part_groups);
+  const dim3 sums((unsigned)(p.grad_groups + plan.zero_groups));
+  const int64_t most = 1 << 23;   // parts of a launch
   auto typed = [&](auto value, auto grad) {
     using T = decltype(value);
     using TD = decltype(grad);
     L(embed_bwd_kernel<T, TD>, sums, dim3(256), p, plan.across);
-    L(embed_parts_kernel<TD>, parts, dim3(256), p);
+    for (int64_t at = 0; at < plan.part_groups; at += most)
+      L(embed_parts_kernel<TD>, dim3((unsigned)(plan.part_groups - at < most ? plan.part_groups - at : most)), dim3(256), p, (uint32_t)at);
   };
   auto of = [&](auto value) { desc->dw_dtype == ACC_BF16 ? typed(value, bf16{}) : typed(value, float{}); };
   if (desc->io_dtype == ACC_BF16) of(bf16{});
