@@ -72,7 +72,8 @@ int check_tensors(const acc_grad_tensor* t, int64_t count, bool scaled, int64_t*
   for (int64_t i = 0; i < count; ++i) {
     if (!valid_dtype(t[i].dtype) || (scaled && !valid_dtype(t[i].dst_dtype))) return ACC_ERR_DTYPE;
     if (t[i].count < 0 || t[i].count > (int64_t)1 << 39) return ACC_ERR_SHAPE;
-    if (t[i].count && (!t[i].src || (scaled && !t[i].dst))) return ACC_ERR_INVALID_ARG;
+    if (!t[i].count) continue;   // wherever it points
+    if (!t[i].src || (scaled && !t[i].dst)) return ACC_ERR_INVALID_ARG;
     if ((uintptr_t)t[i].src % dtype_size(t[i].dtype) || (scaled && (uintptr_t)t[i].dst % dtype_size(t[i].dst_dtype))) return ACC_ERR_ALIGN;
     if (scaled && t[i].src == t[i].dst && t[i].dtype != t[i].dst_dtype) return ACC_ERR_INVALID_ARG;
     *groups += grad_groups(t[i].count);
