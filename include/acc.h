@@ -398,8 +398,8 @@ typedef struct acc_attn_desc {
   int64_t docs;      /* documents of `starts`; 0: sequences of `seq` rows                    */
   int64_t seq;       /* rows of a sequence, 0 = n; 0 where there are documents               */
   int64_t window;    /* keys that a query sees at most, with ACC_ATTN_CAUSAL; 0 = no limit   */
-  float scale;       /* of the products, not negative; 0 = 1 / sqrt(d)                       */
-  float cap;         /* not negative; 0 = none                                               */
+  float scale;       /* of the products, 0 .. 2^127; 0 = 1 / sqrt(d)                         */
+  float cap;         /* 0 .. 2^126, and scale / cap at most 2^126; 0 = none                  */
   int32_t io_dtype;  /* acc_dtype of Q, K, V, O and their gradients                          */
   uint32_t flags;    /* ACC_ATTN_CAUSAL                                                      */
 } acc_attn_desc;

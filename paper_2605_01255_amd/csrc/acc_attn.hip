@@ -67,6 +67,7 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   p.c2 = p.scale * kLog2e;
   p.cap2 = d->cap * kLog2e;
   p.inv_cap = d->cap > 0.f ? p.scale / d->cap : 0.f;
+  if (!isfinite(p.c2) || !isfinite(2.f * p.cap2) || !isfinite(p.inv_cap * (2.f * kLog2e))) return ACC_ERR_INVALID_ARG;   // (a score of zero would be NaN)
   const bool b16 = d->io_dtype == ACC_BF16;
   const int64_t tile = b16 ? 64 : 32, length = d->docs ? ceil_div(d->n, d->docs) : seq;   // rows of a tile; of a document, on average
   const int64_t seen = d->window && d->window < length ? d->window : length;
