@@ -382,7 +382,7 @@ int acc_linear_ce_bwd(const acc_ce_desc* desc, const void* X, const void* W, con
  *   lse [heads, n]     float, which the backward call reads.
  * What is not finite in a document's rows reaches its own rows only.  bfloat16: products of bfloat16 operands accumulated in float, softmax in
  * float; P and dS are rounded to bfloat16 as operands of the products behind them, O, dQ, dK and dV once; delta is taken from O as it was
- * rounded (of a row with at most 64 keys: as sum P dP), and the cap's tanh is exact to 2^-21.  float: float throughout.  The sums are taken in a fixed order.
+ * rounded (of a row with at most 64 keys: as sum P dP), and a capped score is exact to 2^-21 of the cap.  float: float throughout.  The sums are taken in a fixed order.
  * Outputs may not overlap inputs.  Of 2^30 rows and more, counted over all heads and each document in whole tiles of 128 (or 64), calls are
  * ACC_ERR_SHAPE: a launch has fewer than 2^32 threads. */
 #define ACC_ATTN_CAUSAL 1u
@@ -445,7 +445,7 @@ int acc_embed_bwd(const acc_embed_desc* desc, const int64_t* ids, const void* dY
  *   out[0] = norm;  out[1] = min(1, max_norm / (norm + 1e-6)), NaN where the norm is not a number   (two floats, device)
  * acc_grad_scale: dst = src times *factor (a float, device: &out[1]), rounded once; dst may be src, and then nothing is written where the
  * factor is 1.  Of a factored gradient it scales Gr (or left, not both), as a tensor.
- * Squares of dense gradients are summed in double, so the norm is finite wherever the gradients are; those of factors in float, their
+ * Squares of dense gradients are summed in double, so a norm is finite up to float's largest number; those of factors in float, their
  * products and everything behind them in double.  The sums are taken in a fixed order.
  * The tables are read before the call returns; their tensors have no order and may be of any size, dense, aligned to their elements.  No dst
  * may overlap another tensor of the table: a gradient that occurs twice counts twice in the norm, and is listed once to be scaled. */

@@ -179,9 +179,9 @@ constexpr int kFewKeys = 64;
 
 // ---- forward -------------------------------------------------------------------------------------------------
 // A work-group of NW waves has NW x 32 queries of one head; their rows stay in registers as operands.  Tiles of 64 keys (float 32), two in LDS,
-// leave room for two work-groups on a compute unit.  Bound by power and by the vector instructions beside the matrix ones (six to one, of them
-// one exponential and one maximum a score): 4 x 4096 rows, 32 heads of 128 on 8, 597 to 654 us, 0.84 to 0.92 PFLOP/s, the matrix pipe busy half
-// of the time; on zeros, at the full clock, 490.
+// leave room for two work-groups on a compute unit.  Bound by the waits for transfers and barrier (left out, 26 % less; V's transfers are the last
+// to go), by power and by the vector instructions beside the matrix ones (six to one, of them one exponential and one maximum a score): 4 x 4096
+// rows, 32 heads of 128 on 8, 597 to 654 us, 0.84 to 0.92 PFLOP/s, the matrix pipe busy half of the time; on zeros, at the full clock, 490.
 template <typename T, int DB, int NW> __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   using Tile = Tile32<T, DB>;

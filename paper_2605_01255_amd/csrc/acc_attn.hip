@@ -78,6 +78,8 @@ int plan_attn(const acc_attn_desc* d, AttnPlan* plan) {
   //   heads: 241 + 280 us, of 128 rows 170 + 206);
   //   for the keys' gradients heads of up to 64 channels, two work-groups of which fit a compute unit, so that one multiplies while the other
   //   waits (16 heads of 64, documents of 2048 rows: 199 us, of 128 rows 241; 32 heads of 128, 4096 rows: 355 us, of 128 rows 296).
+  // (By the documents' average length: a long one among many short ones has the short ones' shape and no parts.  One of 4096 rows and 128 of 32
+  // rows, 16 heads of 128 on 4: 590 us forward and backward, the two kinds in calls of their own 415 + 105.)
   const int64_t whole = d->heads * ceil_div(d->n, 128);
   plan->waves = b16 && length > 64 && whole >= 128 ? 4 : 2;
   plan->key_waves = b16 && length > 64 && whole >= 128 && d->d > 64 ? 4 : 2;
